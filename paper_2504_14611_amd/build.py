@@ -22,6 +22,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 # kernels and entry points of users sharing their parameters; heterogeneous users
 SOURCES = [os.path.join(HERE, "csrc", f) for f in ("jdob.hip", "jdob_hetero.hip")]
+# the edge operators (include/jdob_edge.h)
+EDGE_SOURCES = [os.path.join(HERE, "edge_csrc", f) for f in ("norm.hip", "project.hip", "attend.hip")]
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libjdob.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
@@ -34,16 +36,25 @@ FLAGS = [
     "-Wall", "-Wno-unused-function",
 ]
 
+# The edge operators sum long products, whose order the ABI leaves open: multiply and add are fused.
+EDGE_FLAGS = [
+    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
+    "-ffp-contract=fast", "-fno-fast-math",
+    "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
+    "-Wall", "-Wno-unused-function",
+]
+
 
 def build(out: str = LIB, extra=()) -> str:
     """Compiles every source (in parallel) and links libjdob.so."""
     tmp = out + ".tmp%d" % os.getpid()
+    jobs = [(src, FLAGS) for src in SOURCES] + [(src, EDGE_FLAGS) for src in EDGE_SOURCES]
     with tempfile.TemporaryDirectory() as d:
-        objs = [os.path.join(d, os.path.basename(src) + ".o") for src in SOURCES]
-        procs = [subprocess.Popen([HIPCC, *FLAGS, *extra, "-I", INCLUDE, "-c", "-o", obj, src],
+        objs = [os.path.join(d, os.path.basename(src) + ".o") for src, _ in jobs]
+        procs = [subprocess.Popen([HIPCC, *flags, *extra, "-I", INCLUDE, "-c", "-o", obj, src],
                                   stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
-                 for src, obj in zip(SOURCES, objs)]
-        for src, pr in zip(SOURCES, procs):
+                 for (src, flags), obj in zip(jobs, objs)]
+        for (src, _), pr in zip(jobs, procs):
             log = pr.communicate()[0]
             if pr.returncode != 0:
                 sys.stderr.write(log)

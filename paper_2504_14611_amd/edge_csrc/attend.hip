@@ -1,0 +1,549 @@
+// Causal attention of packed sequences of different lengths with grouped heads.
+//
+//   o = sum_j p_j v_j / sum_j p_j,  p_j = exp(scale q.k_j - max),  j <= m - n + i
+//
+// One pass over the keys: a running maximum and sum per row, the output rescaled when the maximum
+// grows.  The products are formed transposed: S^T = K Q^T puts one query row in one lane (twice: the
+// two halves of a wave hold other keys of it), so maxima and sums are the lane's own but for one
+// exchange, and the lane's p are, without any movement, the second operand of O^T = V^T P^T; V's
+// columns come from LDS by transposing reads whose order of keys is that of p.
+//
+// Two kernels.  `prompt_kernel`: many rows, each wave 32 of them, all waves of a workgroup share the
+// staged keys.  `few_kernel`: few rows after a long history, where the rows of all heads that read
+// one key head stand together as 32 columns, each wave takes other keys, and the keys are split
+// over workgroups, whose partial results `join_kernel` puts together.
+#include "edge_common.h"
+
+namespace edge {
+namespace {
+
+struct AttendParams {
+  int sequences, heads, kv_heads, group, dim, max_queries;
+  float scale;  // times log2(e)
+  int64_t query_rows, key_rows;
+  const char *q, *k, *v;
+  char *out;
+  int64_t q_stride, q_head, k_stride, k_head, v_stride, v_head, out_stride, out_head;  // elements
+  const int *query_start;
+  const int64_t *key_start;
+  const int *key_count;
+  int splits, tiles;  // few: splits of the keys, tiles of 32 columns; prompt: tiles of rows
+  float *part;        // few: [sequence][key head][tile][split][32 columns][dim + 2]
+};
+
+template <typename T>
+struct Mma;
+template <>
+struct Mma<__bf16> {
+  typedef bf16x8 frag;
+  __device__ static f32x16 m32(frag a, frag b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+  }
+};
+template <>
+struct Mma<_Float16> {
+  typedef f16x8 frag;
+  __device__ static f32x16 m32(frag a, frag b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+  }
+};
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+// A sequence's rows and keys, kept within the arrays whatever the index arrays hold.
+struct Sequence {
+  int64_t row, key;
+  int rows, keys;
+};
+
+__device__ inline Sequence sequence(const AttendParams &p, int u) {
+  int64_t at = p.query_start[u], end = p.query_start[u + 1];
+  at = at < 0 ? 0 : at < p.query_rows ? at : p.query_rows;
+  end = end < at ? at : end < p.query_rows ? end : p.query_rows;
+  int64_t key = p.key_start[u], count = p.key_count[u];
+  key = key < 0 ? 0 : key < p.key_rows ? key : p.key_rows;
+  count = count < 0 ? 0 : count < p.key_rows - key ? count : p.key_rows - key;
+  return {at, key, (int)(end - at), (int)count};
+}
+
+__device__ const u32x4 attend_zeros = {0, 0, 0, 0};
+
+// Staged keys or values: rows of DP elements, 16-byte chunks exchanged within the row.
+// Keys are read 16 bytes a lane, eight rows' equal chunks at once; values 8 bytes a lane, eight rows'
+// equal pairs of chunks at once.
+template <int DP>
+__device__ inline int key_spot(int r, int c) {
+  return r * (DP * 2) + ((c ^ (r & 7)) << 4);
+}
+template <int DP>
+__device__ inline int value_swap(int r) {
+  return DP >= 128 ? (r & 7) << 1 : (r >> 1 & 3) << 1;
+}
+template <int DP>
+__device__ inline int value_spot(int r, int c) {
+  return r * (DP * 2) + ((c ^ value_swap<DP>(r)) << 4);
+}
+
+// Stages keys first .. first + COUNT - 1 of `count` (zeros behind them, and behind `dim`).
+template <typename T, int DP, bool FAST, bool VALUES, int COUNT, int THREADS>
+__device__ inline void stage(char *dst, const T *base, int64_t stride, int64_t first, int count, int dim) {
+  constexpr int CH = DP / 8;
+#pragma unroll
+  for (int i = 0; i < COUNT * CH / THREADS; ++i) {
+    const int slot = i * THREADS + threadIdx.x, r = slot / CH;
+    const int c = (slot % CH) ^ (VALUES ? value_swap<DP>(r) : r & 7);
+    const bool in = first + r < count && c * 8 < dim;
+    const T *src = base + (first + r) * stride + c * 8;
+    if constexpr (FAST) {
+      const char *from = in ? (const char *)src : (const char *)&attend_zeros;
+      __builtin_amdgcn_global_load_lds(
+          (const __attribute__((address_space(1))) unsigned *)from,
+          (__attribute__((address_space(3))) unsigned *)(dst + (i * THREADS + (threadIdx.x & ~63)) * 16), 16, 0, 0);
+    } else {
+      u32x4 x = {0, 0, 0, 0};
+      if (in) x = __builtin_bit_cast(u32x4, *(const typename Raw<unsigned short, 8>::type *)src);
+      *(u32x4 *)(dst + slot * 16) = x;
+    }
+  }
+}
+
+// The running state of 32 rows in a wave: lane l and l + 32 hold row l % 32.
+template <int DP>
+struct State {
+  float top, sum;           // the maximum so far (log2 units), this half's sum
+  f32x16 out[DP / 32];      // out[d][e]: column 32 d + 8 (e / 4) + 4 half + e % 4
+};
+
+__device__ inline float other_half(float x) { return __shfl_xor(x, 32); }
+
+// The maximum starts below every score that binary32 arithmetic gives real rows, and above -inf, so
+// that masked scores (-inf) give exp2(-inf) = 0 also where nothing has been seen yet.
+constexpr float LOWEST = -1e30f;
+
+constexpr float GROWTH = 8.0f;  // the maximum may lag behind by this much (p up to 2^8) before out is rescaled
+
+// Scores of 32 rows with KT * 32 staged keys, softmax, and the values' sums.  `limit`: the lane's row
+// sees keys first .. limit; `masked`: whether any key of the tile lies behind some row's limit.
+template <typename T, int DP, int KT>
+__device__ inline void attend_tile(State<DP> &s, const typename Mma<T>::frag (&q)[DP / 16], const char *keys,
+                                   const char *values, int64_t first, int64_t limit, bool masked, float scale) {
+  typedef typename Mma<T>::frag frag;
+  const int lane = threadIdx.x % WAVE, l32 = lane % 32, half = lane / 32;
+  f32x16 sc[KT];
+#pragma unroll
+  for (int t = 0; t < KT; ++t) {
+    sc[t] = (f32x16){};
+#pragma unroll
+    for (int c = 0; c < DP / 16; ++c)
+      sc[t] = Mma<T>::m32(*(const frag *)(keys + key_spot<DP>(t * 32 + l32, c * 2 + half)), q[c], sc[t]);
+  }
+  float top = LOWEST;
+  if (masked) {
+    const int64_t sees = limit - first;  // within the tile
+#pragma unroll
+    for (int t = 0; t < KT; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        sc[t][e] = t * 32 + 8 * (e / 4) + 4 * half + e % 4 <= sees ? sc[t][e] : -INFINITY;
+  }
+#pragma unroll
+  for (int t = 0; t < KT; ++t)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) top = fmaxf(top, sc[t][e] * scale);
+  top = fmaxf(top, other_half(top));
+  if (__any(top > s.top + GROWTH)) {
+    // a row's own scores decide for it: what other rows of the wave see does not change its roundings
+    const float next = top > s.top + GROWTH ? top : s.top;
+    // (nothing has been seen yet: out is zero, or holds infinities that are to stay)
+    const float f = s.top == LOWEST ? 1.0f : __builtin_amdgcn_exp2f(s.top - next);
+    s.top = next;
+    s.sum *= f;
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d) s.out[d] *= f;
+  }
+  frag p[KT * 2];
+#pragma unroll
+  for (int t = 0; t < KT; ++t)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const float x = __builtin_amdgcn_exp2f(sc[t][e] * scale - s.top);
+      s.sum += x;
+      p[t * 2 + e / 8][e % 8] = (T)x;
+    }
+  const int l16 = lane % 16, g16 = lane / 16;
+#pragma unroll
+  for (int b = 0; b < KT * 2; ++b)
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d) {
+      const int c0 = d * 4 + (g16 % 2) * 2 + l16 % 4 / 2, r = b * 16 + half * 4 + l16 / 4;
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (__attribute__((address_space(3))) s16x4 *)(values + value_spot<DP>(r, c0) + l16 % 2 * 8));
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (__attribute__((address_space(3))) s16x4 *)(values + value_spot<DP>(r + 8, c0) + l16 % 2 * 8));
+      struct { s16x4 a, b; } both = {lo, hi};
+      s.out[d] = Mma<T>::m32(__builtin_bit_cast(frag, both), p[b], s.out[d]);
+    }
+}
+
+// Whether the wave finds an infinity or a NaN among KEYS staged values.
+template <typename T, int DP, int KEYS>
+__device__ inline bool any_non_finite(const char *values) {
+  const int lane = threadIdx.x % WAVE;
+  constexpr unsigned EXP = sizeof(T) == 2 && __is_same(T, __bf16) ? 0x7f80u : 0x7c00u;
+  bool bad = false;
+  for (int i = lane; i < KEYS * DP / 8; i += WAVE) {
+    const u32x4 x = *(const u32x4 *)(values + i * 16);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) bad |= (x[c] & EXP) == EXP || (x[c] >> 16 & EXP) == EXP;
+  }
+  return __any(bad);
+}
+
+// Replaces the staged values' infinities and NaN by zeros after adding them to the rows that see them
+// (their products with p = 0 of rows that do not would be NaN).  Rare, and slow.
+template <typename T, int DP, int KEYS>
+__device__ inline void take_non_finite(State<DP> &s, char *values, int64_t first, int64_t limit) {
+  constexpr unsigned EXP = __is_same(T, __bf16) ? 0x7f80u : 0x7c00u;
+  const int half = threadIdx.x % WAVE / 32;
+  for (int r = 0; r < KEYS; ++r)
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int at = 32 * d + 8 * (e / 4) + 4 * half + e % 4;
+        const T x = *(const T *)(values + value_spot<DP>(r, at / 8) + at % 8 * 2);
+        const unsigned bits = __builtin_bit_cast(unsigned short, x);
+        if ((bits & EXP) == EXP && first + r <= limit) s.out[d][e] += (float)x;
+      }
+}
+
+template <typename T, int DP, int KEYS, int THREADS>
+__device__ inline void clear_non_finite(char *values) {
+  constexpr unsigned EXP = __is_same(T, __bf16) ? 0x7f80u : 0x7c00u;
+  for (int i = threadIdx.x; i < KEYS * DP; i += THREADS) {
+    unsigned short *x = (unsigned short *)values + i;
+    if ((*x & EXP) == EXP) *x = 0;
+  }
+}
+
+// Eight elements of a query row, zeros behind `dim`.
+template <typename T>
+__device__ inline typename Mma<T>::frag query(const T *row, int c, int dim, bool have) {
+  typename Mma<T>::frag f = {};
+  if (have && c * 8 < dim) f = *(const typename Raw<T, 8>::type *)(row + c * 8);
+  return f;
+}
+
+// ------------------------------------------------------------------ many rows
+
+constexpr int PROMPT_WAVES = 4, PROMPT_ROWS = 32 * PROMPT_WAVES, PROMPT_KEYS = 64;
+
+// Which sequence and which of its tiles of rows a tile index stands for: the sequences' tiles follow
+// each other.  False behind the last one.
+__device__ inline bool find_tile(const AttendParams &p, int tile, int *u, int *t, Sequence *q) {
+  const int lane = threadIdx.x % WAVE;
+  int before = 0;
+  for (int u0 = 0; u0 < p.sequences; u0 += WAVE) {
+    int n = 0;
+    if (u0 + lane < p.sequences) n = (sequence(p, u0 + lane).rows + PROMPT_ROWS - 1) / PROMPT_ROWS;
+    int upto = n;
+#pragma unroll
+    for (int d = 1; d < WAVE; d <<= 1) {
+      const int x = __shfl_up(upto, d);
+      if (lane >= d) upto += x;
+    }
+    const unsigned long long past = __ballot(before + upto > tile);
+    if (past) {
+      const int l = __builtin_ctzll(past);
+      *u = u0 + l;
+      *q = sequence(p, *u);
+      *t = __shfl(n, l) - 1 - (tile - before - __shfl(upto - n, l));  // the last rows see most: first
+      return true;
+    }
+    before += __shfl(upto, WAVE - 1);
+  }
+  return false;
+}
+
+template <typename T, int DP, bool FAST>
+__global__ __launch_bounds__(PROMPT_WAVES *WAVE) void prompt_kernel(AttendParams p) {
+  typedef typename Mma<T>::frag frag;
+  constexpr int THREADS = PROMPT_WAVES * WAVE, BYTES = PROMPT_KEYS * DP * 2;
+  __shared__ __align__(16) char keys[2][BYTES], values[2][BYTES];
+  const int lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE, l32 = lane % 32, half = lane / 32;
+  const int head = blockIdx.x % p.heads, tile = blockIdx.x / p.heads;
+  int u, t;
+  Sequence q;
+  if (!find_tile(p, tile, &u, &t, &q)) return;
+  const int kv = head / p.group;
+  const int row0 = t * PROMPT_ROWS, mine = row0 + wave * 32 + l32;
+  const int shift = q.keys - q.rows;  // row i sees keys 0 .. shift + i
+  const T *const qrow = (const T *)p.q + (q.row + (mine < q.rows ? mine : 0)) * p.q_stride + head * p.q_head;
+  frag qf[DP / 16];
+#pragma unroll
+  for (int c = 0; c < DP / 16; ++c) qf[c] = query<T>(qrow, c * 2 + half, p.dim, mine < q.rows);
+  const T *const k = (const T *)p.k + q.key * p.k_stride + kv * p.k_head;
+  const T *const v = (const T *)p.v + q.key * p.v_stride + kv * p.v_head;
+  const int last_row = (row0 + PROMPT_ROWS < q.rows ? row0 + PROMPT_ROWS : q.rows) - 1;
+  const int seen = shift + last_row + 1;  // keys that some row of the workgroup sees
+  const int tiles = seen > 0 ? (seen + PROMPT_KEYS - 1) / PROMPT_KEYS : 0;
+  State<DP> s;
+  s.top = LOWEST;
+  s.sum = 0.0f;
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d) s.out[d] = (f32x16){};
+  auto load = [&](int b, int kt) {
+    stage<T, DP, FAST, false, PROMPT_KEYS, THREADS>(keys[b], k, p.k_stride, (int64_t)kt * PROMPT_KEYS, q.keys, p.dim);
+    stage<T, DP, FAST, true, PROMPT_KEYS, THREADS>(values[b], v, p.v_stride, (int64_t)kt * PROMPT_KEYS, q.keys, p.dim);
+  };
+  if (tiles > 0) load(0, 0);
+  for (int kt = 0; kt < tiles; ++kt) {
+    const int b = kt & 1;
+    __syncthreads();
+    if (kt + 1 < tiles) load(b ^ 1, kt + 1);
+    const int first = kt * PROMPT_KEYS, limit = shift + mine;
+    // rows of the workgroup that do not see all of the tile
+    const bool edge_tile = first + PROMPT_KEYS - 1 > shift + row0;
+    if (edge_tile) {
+      if (any_non_finite<T, DP, PROMPT_KEYS>(values[b])) {  // the same for all waves
+        take_non_finite<T, DP, PROMPT_KEYS>(s, values[b], first, limit);
+        __syncthreads();
+        clear_non_finite<T, DP, PROMPT_KEYS, THREADS>(values[b]);
+        __syncthreads();
+      }
+    }
+    attend_tile<T, DP, PROMPT_KEYS / 32>(s, qf, keys[b], values[b], first, limit, edge_tile, p.scale);
+  }
+  const float sum = s.sum + other_half(s.sum), f = sum > 0.0f ? 1.0f / sum : sum;
+  if (mine >= q.rows) return;
+  T *const out = (T *)p.out + (q.row + mine) * p.out_stride + head * p.out_head;
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int at = 32 * d + 8 * e + 4 * half;
+      if (at >= p.dim) continue;
+      const float y[4] = {s.out[d][4 * e] * f, s.out[d][4 * e + 1] * f, s.out[d][4 * e + 2] * f, s.out[d][4 * e + 3] * f};
+      store_f32<T, 4>(out + at, y);
+    }
+}
+
+// ------------------------------------------------------------------ few rows
+
+constexpr int FEW_WAVES = 4, FEW_COLUMNS = 32, FEW_KEYS = 32 * FEW_WAVES;
+
+template <typename T, int DP, bool FAST>
+__global__ __launch_bounds__(FEW_WAVES *WAVE) void few_kernel(AttendParams p) {
+  typedef typename Mma<T>::frag frag;
+  constexpr int THREADS = FEW_WAVES * WAVE, BYTES = FEW_KEYS * DP * 2;
+  __shared__ __align__(16) char room[4 * BYTES];
+  __shared__ float tops[FEW_WAVES][32], sums[FEW_WAVES][32];
+  const int lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE, l32 = lane % 32, half = lane / 32;
+  const int split = blockIdx.x % p.splits, kv = blockIdx.x / p.splits % p.kv_heads;
+  const int tile = blockIdx.x / p.splits / p.kv_heads % p.tiles, u = blockIdx.x / p.splits / p.kv_heads / p.tiles;
+  const Sequence q = sequence(p, u);
+  const int rows = q.rows < p.max_queries ? q.rows : p.max_queries;
+  const int columns = rows * p.group, column = tile * FEW_COLUMNS + l32;
+  if (tile * FEW_COLUMNS >= columns) return;
+  const bool have = column < columns;
+  const int row = have ? column / p.group : 0, head = kv * p.group + (have ? column % p.group : 0);
+  const int shift = q.keys - q.rows, limit = have ? shift + row : -1;
+  const T *const qrow = (const T *)p.q + (q.row + row) * p.q_stride + head * p.q_head;
+  frag qf[DP / 16];
+#pragma unroll
+  for (int c = 0; c < DP / 16; ++c) qf[c] = query<T>(qrow, c * 2 + half, p.dim, have);
+  const T *const k = (const T *)p.k + q.key * p.k_stride + kv * p.k_head;
+  const T *const v = (const T *)p.v + q.key * p.v_stride + kv * p.v_head;
+  // this split's tiles of keys
+  const int all = (q.keys + FEW_KEYS - 1) / FEW_KEYS, each = (all + p.splits - 1) / p.splits;
+  const int lo = split * each, hi = lo + each < all ? lo + each : all;
+  const int first_limit = shift + tile * FEW_COLUMNS / p.group;  // of the tile's first row
+  State<DP> s;
+  s.top = LOWEST;
+  s.sum = 0.0f;
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d) s.out[d] = (f32x16){};
+  auto load = [&](int b, int kt) {
+    stage<T, DP, FAST, false, FEW_KEYS, THREADS>(room + b * 2 * BYTES, k, p.k_stride, (int64_t)kt * FEW_KEYS, q.keys, p.dim);
+    stage<T, DP, FAST, true, FEW_KEYS, THREADS>(room + (b * 2 + 1) * BYTES, v, p.v_stride, (int64_t)kt * FEW_KEYS, q.keys, p.dim);
+  };
+  if (lo < hi) load(0, lo);
+  for (int kt = lo; kt < hi; ++kt) {
+    const int b = (kt - lo) & 1;
+    __syncthreads();
+    if (kt + 1 < hi) load(b ^ 1, kt + 1);
+    const int first = kt * FEW_KEYS + wave * 32;
+    const char *const keys = room + b * 2 * BYTES + wave * 32 * DP * 2;
+    char *const values = room + (b * 2 + 1) * BYTES + wave * 32 * DP * 2;
+    const bool masked = first + 31 > first_limit;
+    if (masked && any_non_finite<T, DP, 32>(values)) {
+      take_non_finite<T, DP, 32>(s, values, first, limit);
+      // the wave's own values: its lanes run together, their LDS accesses in order
+      constexpr unsigned EXP = __is_same(T, __bf16) ? 0x7f80u : 0x7c00u;
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      for (int i = lane; i < 32 * DP; i += WAVE) {
+        unsigned short *x = (unsigned short *)values + i;
+        if ((*x & EXP) == EXP) *x = 0;
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    }
+    attend_tile<T, DP, 1>(s, qf, keys, values, first, limit, masked, p.scale);
+  }
+  // the waves' results: each column's maximum, then sums and outputs relative to it
+  s.sum += other_half(s.sum);
+  if (half == 0) {
+    tops[wave][l32] = s.top;
+    sums[wave][l32] = s.sum;
+  }
+  __syncthreads();  // also: the staged keys have been read
+  float top = LOWEST, sum = 0.0f;
+#pragma unroll
+  for (int w = 0; w < FEW_WAVES; ++w) top = fmaxf(top, tops[w][l32]);
+#pragma unroll
+  for (int w = 0; w < FEW_WAVES; ++w) sum += sums[w][l32] * __builtin_amdgcn_exp2f(tops[w][l32] - top);
+  const float f = __builtin_amdgcn_exp2f(s.top - top);
+  float *const mix = (float *)room;  // [wave][column][DP + 4]
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const f32x4 y = {s.out[d][4 * e] * f, s.out[d][4 * e + 1] * f, s.out[d][4 * e + 2] * f, s.out[d][4 * e + 3] * f};
+      *(f32x4 *)(mix + (wave * 32 + l32) * (DP + 4) + 32 * d + 8 * e + 4 * half) = y;
+    }
+  if (wave == 0 && half == 0) sums[0][l32] = sum, tops[0][l32] = top;
+  __syncthreads();
+  for (int i = threadIdx.x; i < 32 * (DP / 4); i += THREADS) {
+    const int c = i / (DP / 4), at = i % (DP / 4) * 4, col = tile * FEW_COLUMNS + c;
+    if (col >= columns || at >= p.dim) continue;
+    f32x4 y = {0, 0, 0, 0};
+#pragma unroll
+    for (int w = 0; w < FEW_WAVES; ++w) y += *(const f32x4 *)(mix + (w * 32 + c) * (DP + 4) + at);
+    if (p.splits == 1) {
+      const float g = sums[0][c] > 0.0f ? 1.0f / sums[0][c] : sums[0][c];
+      const float z[4] = {y[0] * g, y[1] * g, y[2] * g, y[3] * g};
+      T *const out = (T *)p.out + (q.row + col / p.group) * p.out_stride + (kv * p.group + col % p.group) * p.out_head;
+      store_f32<T, 4>(out + at, z);
+    } else {
+      float *const part = p.part + ((((int64_t)u * p.kv_heads + kv) * p.tiles + tile) * p.splits + split) * 32 * (p.dim + 4) + c * (p.dim + 4);
+      *(f32x4 *)(part + at) = y;
+      if (at == 0) part[p.dim] = tops[0][c], part[p.dim + 1] = sums[0][c];
+    }
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(WAVE) void join_kernel(AttendParams p) {
+  const int c = blockIdx.x % 32, kv = blockIdx.x / 32 % p.kv_heads;
+  const int tile = blockIdx.x / 32 / p.kv_heads % p.tiles, u = blockIdx.x / 32 / p.kv_heads / p.tiles;
+  const Sequence q = sequence(p, u);
+  const int rows = q.rows < p.max_queries ? q.rows : p.max_queries, col = tile * FEW_COLUMNS + c;
+  if (col >= rows * p.group) return;
+  const int64_t pitch = p.dim + 4;
+  const float *const part = p.part + (((int64_t)u * p.kv_heads + kv) * p.tiles + tile) * p.splits * 32 * pitch + c * pitch;
+  float top = LOWEST, sum = 0.0f;
+  for (int i = 0; i < p.splits; ++i) top = fmaxf(top, part[i * 32 * pitch + p.dim]);
+  for (int i = 0; i < p.splits; ++i)
+    sum += part[i * 32 * pitch + p.dim + 1] * __builtin_amdgcn_exp2f(part[i * 32 * pitch + p.dim] - top);
+  const float g = sum > 0.0f ? 1.0f / sum : sum;
+  T *const out = (T *)p.out + (q.row + col / p.group) * p.out_stride + (kv * p.group + col % p.group) * p.out_head;
+  for (int at = threadIdx.x; at < p.dim; at += WAVE) {
+    float y = 0.0f;
+    for (int i = 0; i < p.splits; ++i)
+      y += part[i * 32 * pitch + at] * __builtin_amdgcn_exp2f(part[i * 32 * pitch + p.dim] - top);
+    out[at] = (T)(y * g);
+  }
+}
+
+// ------------------------------------------------------------------ host side
+
+int attend_check(const jdob_edge_attend_args *a, bool sizes_only) {
+  if (!a || a->num_sequences < 0 || a->num_heads < 1 || a->num_kv_heads < 1 || a->num_heads % a->num_kv_heads ||
+      a->head_dim < 1 || a->max_queries < 0 || a->max_keys < 0 || a->query_rows < 0 || a->key_rows < 0 ||
+      !(a->scale > 0.0f) || !isfinite(a->scale))
+    return JDOB_ERR_INVALID_ARG;
+  if (a->dtype != JDOB_EDGE_BF16 && a->dtype != JDOB_EDGE_F16) return JDOB_ERR_UNSUPPORTED;
+  if (a->head_dim > JDOB_EDGE_MAX_HEAD_DIM || a->head_dim % 8 || a->num_heads > 1024 ||
+      a->num_sequences > JDOB_EDGE_MAX_SEQUENCES || a->query_rows > 0x7fffffff)
+    return JDOB_ERR_UNSUPPORTED;
+  if (sizes_only || a->num_sequences == 0 || a->query_rows == 0 || a->max_queries == 0) return JDOB_OK;
+  if (!a->q || !a->out || !a->query_start || !a->key_start || !a->key_count || (a->key_rows > 0 && (!a->k || !a->v)))
+    return JDOB_ERR_INVALID_ARG;
+  if (a->q_stride < 0 || a->q_head_stride < 0 || a->k_stride < 0 || a->k_head_stride < 0 || a->v_stride < 0 ||
+      a->v_head_stride < 0 || a->out_stride < 0 || a->out_head_stride < 0)
+    return JDOB_ERR_INVALID_ARG;
+  const int64_t need = jdob_edge_attend_workspace(a);
+  if (need > 0 && (!a->workspace || (uintptr_t)a->workspace % 16 || a->workspace_bytes < need))
+    return JDOB_ERR_INVALID_ARG;
+  return JDOB_OK;
+}
+
+struct FewPlan {
+  bool few;
+  int tiles, splits;
+};
+
+FewPlan few_plan(const jdob_edge_attend_args *a) {
+  const int64_t columns = (int64_t)a->max_queries * (a->num_heads / a->num_kv_heads);
+  const int64_t tiles = (columns + FEW_COLUMNS - 1) / FEW_COLUMNS;
+  const int64_t groups = tiles * a->num_kv_heads * a->num_sequences;
+  if (columns > 128 || groups > (1 << 24)) return {false, 0, 0};
+  int64_t splits = (512 + groups - 1) / groups;
+  const int64_t most = (a->max_keys + 2 * FEW_KEYS - 1) / (2 * FEW_KEYS);
+  splits = splits < most ? splits : most;
+  return {true, (int)tiles, (int)(splits < 1 ? 1 : splits > 128 ? 128 : splits)};
+}
+
+template <typename T, int DP>
+int attend(AttendParams p, bool few, bool fast, hipStream_t stream) {
+  if (few) {
+    const int64_t groups = (int64_t)p.sequences * p.kv_heads * p.tiles;
+    if (groups * p.splits > 0x7fffffff || groups * 32 > 0x7fffffff) return JDOB_ERR_UNSUPPORTED;
+    const dim3 grid((unsigned)(groups * p.splits));
+    const int code = fast ? launch(few_kernel<T, DP, true>, grid, FEW_WAVES * WAVE, stream, p)
+                          : launch(few_kernel<T, DP, false>, grid, FEW_WAVES * WAVE, stream, p);
+    if (code != JDOB_OK || p.splits == 1) return code;
+    return launch(join_kernel<T>, dim3((unsigned)(groups * 32)), WAVE, stream, p);
+  }
+  const int64_t blocks = (int64_t)p.tiles * p.heads;
+  if (blocks > 0x7fffffff) return JDOB_ERR_UNSUPPORTED;
+  return fast ? launch(prompt_kernel<T, DP, true>, dim3((unsigned)blocks), PROMPT_WAVES * WAVE, stream, p)
+              : launch(prompt_kernel<T, DP, false>, dim3((unsigned)blocks), PROMPT_WAVES * WAVE, stream, p);
+}
+
+template <typename T>
+int attend(const AttendParams &p, bool few, bool fast, hipStream_t stream) {
+  return p.dim <= 64 ? attend<T, 64>(p, few, fast, stream) : attend<T, 128>(p, few, fast, stream);
+}
+
+}  // namespace
+}  // namespace edge
+
+extern "C" int64_t jdob_edge_attend_workspace(const jdob_edge_attend_args *a) {
+  using namespace edge;
+  if (attend_check(a, true) != JDOB_OK) return -1;
+  if (a->num_sequences == 0 || a->query_rows == 0 || a->max_queries == 0) return 0;
+  const FewPlan f = few_plan(a);
+  if (!f.few || f.splits == 1) return 0;
+  return (int64_t)a->num_sequences * a->num_kv_heads * f.tiles * f.splits * 32 * (a->head_dim + 4) * (int64_t)sizeof(float);
+}
+
+extern "C" int jdob_edge_attend(const jdob_edge_attend_args *a, void *hip_stream) {
+  using namespace edge;
+  const int code = attend_check(a, false);
+  if (code != JDOB_OK || a->num_sequences == 0 || a->query_rows == 0 || a->max_queries == 0) return code;
+  const FewPlan f = few_plan(a);
+  AttendParams p = {a->num_sequences, a->num_heads, a->num_kv_heads, a->num_heads / a->num_kv_heads, a->head_dim,
+                    a->max_queries, a->scale * 1.44269504088896f, a->query_rows, a->key_rows,
+                    (const char *)a->q, (const char *)a->k, (const char *)a->v, (char *)a->out,
+                    a->q_stride, a->q_head_stride, a->k_stride, a->k_head_stride, a->v_stride, a->v_head_stride,
+                    a->out_stride, a->out_head_stride, a->query_start, a->key_start, a->key_count,
+                    f.splits, f.tiles, (float *)a->workspace};
+  // every sequence's rows fill whole tiles but for one
+  if (!f.few) p.tiles = (int)(a->query_rows / PROMPT_ROWS + a->num_sequences);
+  const bool fast = (uintptr_t)a->k % 16 == 0 && (uintptr_t)a->v % 16 == 0 && a->k_stride % 8 == 0 &&
+                    a->k_head_stride % 8 == 0 && a->v_stride % 8 == 0 && a->v_head_stride % 8 == 0;
+  hipStream_t stream = (hipStream_t)hip_stream;
+  return a->dtype == JDOB_EDGE_BF16 ? attend<__bf16>(p, f.few, fast, stream) : attend<_Float16>(p, f.few, fast, stream);
+}

@@ -1,0 +1,93 @@
+"""jdob_edge_norm against its definition in 64 bits."""
+
+import pytest
+import torch
+
+from paper_2504_14611_amd import edge
+from tests import edge_model as model
+
+pytestmark = pytest.mark.gpu
+BF16, F16, F32 = torch.bfloat16, torch.float16, torch.float32
+
+
+def inputs(rows, dim, dtype, residual, seed=0):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    x = torch.randn(rows, dim, generator=gen, device="cuda").to(dtype)
+    r = torch.randn(rows, dim, generator=gen, device="cuda").mul_(3).to(dtype) if residual else None
+    w = torch.randn(dim, generator=gen, device="cuda").add_(1).to(dtype)
+    return x, r, w
+
+
+def check(r, x, w, eps, residual, label):
+    h, y = model.norm(x, w, eps, residual)
+    if residual is not None:
+        assert torch.equal(r["sum"], (x.float() + residual.float()).to(x.dtype)), label
+    if r["out"] is not None:
+        off = (r["out"].double() - y).abs() - model.norm_bound(y, x.dtype)
+        assert off.max() <= 0, (label, off.max())
+    if r["q"] is not None:
+        top = y.abs().amax(dim=1)
+        assert ((r["scale"].double() - top / 127).abs() <= top / 127 * 100 * model.U32).all(), label
+        step = torch.where(top > 0, top / 127, 1.0)[:, None]
+        # the nearest integer, or its neighbour where y / step lies at the middle to 127 roundings of 100 steps
+        assert ((r["q"].double() - y / step).abs() <= 0.5 + 127 * 101 * model.U32).all(), label
+        assert (r["q"].abs().amax(dim=1)[top > 0] == 127).all(), label
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16, F32], ids=["bf16", "f16", "f32"])
+@pytest.mark.parametrize("rows,dim", [(1, 1), (1, 4096), (3, 7), (5, 64), (2, 513), (33, 1000), (1025, 1031),
+                                      (1500, 512), (1024, 2048), (1030, 4096), (7, 8192), (3, 16384), (2, 12345)])
+def test_norm(rows, dim, dtype):
+    for residual in (False, True):
+        x, r, w = inputs(rows, dim, dtype, residual, rows + dim)
+        for bits8, out16 in ((False, True), (True, False), (True, True)):
+            got = edge.norm(x, w, eps=1e-5, residual=r, bits8=bits8, out16=out16)
+            check(got, x, w, 1e-5, r, (rows, dim, dtype, residual, bits8, out16))
+
+
+@pytest.mark.parametrize("shift", [0, 1, 3])
+def test_norm_strides_offsets_and_in_place(shift):
+    """Rows that start at any element, wider strides, and the sum written over the residual or over x."""
+    rows, dim = 1100, 1024
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    wide = torch.randn(rows, dim + 40, generator=gen, device="cuda").to(BF16)
+    x, (_, r, w) = wide[:, shift:shift + dim], inputs(rows, dim, BF16, True)
+    qs = torch.full((rows, dim + 24), 99, dtype=torch.int8, device="cuda")
+    got = edge.norm(x, w, residual=r, bits8=True, out16=True, into={"q": qs[:, shift:shift + dim]})
+    check(got, x, w, 1e-6, r, shift)
+    assert (qs[:, :shift] == 99).all() and (qs[:, shift + dim:] == 99).all()
+    for target in ("x", "residual"):
+        x2, r2 = wide.clone()[:, shift:shift + dim], r.clone()
+        got2 = edge.norm(x2, w, residual=r2, bits8=True, out16=True, into={"sum": x2 if target == "x" else r2})
+        for key in ("sum", "out", "q", "scale"):
+            assert torch.equal(got2[key], got[key]), (target, key)
+
+
+def test_norm_zero_rows_tiny_rows_and_non_finite_values():
+    x, _, w = inputs(6, 300, F32, False)
+    x[1] = 0
+    x[2] *= 1e-25           # far below eps: y is tiny, but no zero row
+    x[3, 7] = float("nan")
+    x[4, 299] = float("inf")
+    x[5, 0] = -float("inf")
+    got = edge.norm(x, w, eps=1e-6, bits8=True, out16=True)
+    check({k: v[:3] if v is not None else None for k, v in got.items()}, x[:3], w, 1e-6, None, "finite rows")
+    assert got["scale"][1] == 0 and (got["q"][1] == 0).all() and (got["out"][1] == 0).all()
+    assert got["scale"][3:].isnan().all() and got["out"][3].isnan().all()
+    assert got["out"][4, 299].isnan() and (got["out"][4, :299] == 0).all()
+    # eps = 0: a row of zeros is 0 / 0
+    assert edge.norm(torch.zeros(2, 8, device="cuda"), torch.ones(8, device="cuda"), eps=0.0)["out"].isnan().all()
+
+
+def test_norm_one_row_between_others_and_on_another_stream():
+    x, r, w = inputs(40, 4096, F16, True)
+    all_rows = edge.norm(x, w, residual=r, bits8=True)
+    one = edge.norm(x[17:18], w, residual=r[17:18], bits8=True)
+    assert torch.equal(one["q"][0], all_rows["q"][17]) and torch.equal(one["scale"][0], all_rows["scale"][17])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = edge.norm(x, w, residual=r, bits8=True, stream=side.cuda_stream)
+    side.synchronize()
+    for key in ("sum", "q", "scale"):
+        assert torch.equal(got[key], all_rows[key])
+    assert edge.norm(x[:0], w, residual=r[:0], bits8=True)["q"].shape == (0, 4096)
