@@ -45,6 +45,9 @@ __device__ inline void store_f32(T *dst, const float *src) {
   *(typename Raw<T, N>::type *)dst = v;
 }
 
+// The thread's wave, as a value that the compiler knows to be the same for all lanes.
+__device__ inline int wave_index() { return __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE); }
+
 __device__ inline float wave_sum(float x) {
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d);
@@ -58,6 +61,44 @@ __device__ inline unsigned wave_max(unsigned x) {
     x = y > x ? y : x;
   }
   return x;
+}
+
+// Loads 16 bytes a lane from memory to LDS without registers between: lane l's to to + 16 l, where `to`
+// is the same for all lanes of the wave.  The compiler does not count these loads (it would wait for
+// all of them before the next read of any LDS array that it cannot tell from the target): whoever
+// reads the target waits for them with wait_loads and passes a barrier first.  The source is the sum
+// of the wave's own base and a lane's offset of 32 bits, or a lane's own address.  (M0, which holds the
+// target, is not the compiler's to allocate: it writes M0 itself before each instruction that reads it.)
+__device__ inline unsigned lds_address(const void *p) {
+  return (unsigned)(uintptr_t)(const __attribute__((address_space(3))) char *)p;
+}
+__device__ inline void load_to_lds(const void *base, unsigned offset, unsigned to) {
+  const uint64_t b = (uint64_t)base;
+  const uint64_t same = (uint64_t)__builtin_amdgcn_readfirstlane((unsigned)(b >> 32)) << 32 |
+                        (unsigned)__builtin_amdgcn_readfirstlane((unsigned)b);
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+               :
+               : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(offset), "s"(same)
+               : "memory");
+}
+__device__ inline void load_to_lds(const void *from, unsigned to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+               :
+               : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(from)
+               : "memory");
+}
+
+// Waits until at most N of the wave's loads are under way, and none of its LDS accesses.
+template <int N>
+__device__ inline void wait_loads() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "i"(N) : "memory");
+}
+
+// A barrier that waits for nothing but the waves.
+__device__ inline void barrier() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
 }
 
 // Launches a kernel of one parameter struct and returns the status of this launch alone.

@@ -2,9 +2,9 @@
 //
 //   out = x W^T + gain_a ((x A_a^T) B_a^T),  a = the row's adapter (or none)
 //
-// Two kernels.  `down_kernel` forms the low-rank rows v = x A_a^T (binary32, in the workspace);
-// `tile_kernel` forms x W^T tile by tile and, before it stores a tile, multiplies the v of the
-// tile's rows with the B of each adapter among them onto the same accumulators.
+// `down_kernel` forms the low-rank rows gain_a (x A_a^T) in the workspace.  Then either kernel forms
+// x W^T and adds the low-rank rows times B_a^T before it stores: `stream_kernel` for few rows, where
+// reading W is all that counts, `tile_kernel` for many, where the products are.
 #include "edge_common.h"
 
 namespace edge {
@@ -19,8 +19,11 @@ struct ProjectParams {
   const void *down, *up;
   const float *gain;
   const int *rank, *row_adapter;
-  float *v;                        // [splits][rows][rank_pad] partial low-rank rows
-  int rank_pad, splits, split_len; // split_len: elements of the inner dimension, a multiple of 32
+  // The low-rank rows, gain and scales applied, zeros behind the adapter's rank; slabs = ranks / 32.
+  // stream_kernel: binary32 [rows][32 slabs].  tile_kernel: [slab][rows][64] of dtype, the rows' 32
+  // values rounded, then what the rounding left of each.
+  void *v;
+  int slabs, split;                // split: v is in two parts
   void *out;
   int64_t out_stride;
 };
@@ -67,6 +70,11 @@ struct Main<T, true> {
   }
 };
 
+template <int N>
+struct Count {
+  static constexpr int value = N;
+};
+
 // The adapter of a row: -1 for none.
 __device__ inline int adapter_of(const ProjectParams &p, int row) {
   const int a = p.row_adapter[row];
@@ -78,7 +86,62 @@ __device__ inline int rank_of(const ProjectParams &p, int a) {
   return r < 0 ? 0 : r < p.max_rank ? r : p.max_rank;
 }
 
-// ------------------------------------------------------------------ v = x A^T
+// 16 bytes of a row from byte `at` on, zeros from `len` on.
+template <bool X8>
+__device__ inline u32x4 chunk(const char *row, int at, int len) {
+  if (at + 16 <= len) return *(const typename Raw<unsigned, 4>::type *)(row + at);
+  u32x4 v = {0, 0, 0, 0};
+#pragma unroll
+  for (int j = 0; j < 16; j += X8 ? 1 : 2)
+    if (at + j < len)
+      v[j / 4] |= (unsigned)(X8 ? *(const unsigned char *)(row + at + j) : *(const unsigned short *)(row + at + j))
+                  << (j % 4 * 8);
+  return v;
+}
+
+// ------------------------------------------------------------------ rows through registers and LDS
+
+constexpr int SLICE = 128;  // bytes of the inner dimension taken at a time: 64 or 128 elements
+
+// Where 16-byte chunk c of row r of a slice stands in LDS: rows of 128 bytes, chunks exchanged within
+// the row so that eight rows' equal chunks fall on different banks.
+__device__ inline int spot(int r, int c) { return r * SLICE + ((c ^ (r & 7)) << 4); }
+
+// A wave's slices of ROWS rows.  The matrix units want equal lanes in equal rows, memory wants
+// neighbouring lanes in neighbouring bytes (a lane a row makes each lane's 16 bytes a request of
+// their own, and W came at 2.5 TB/s): eight lanes load a row's 128 bytes, and the wave's own corner of
+// LDS hands them to the lanes that need them.
+template <int ROWS>
+struct Rows {
+  const char *at[ROWS / 8];
+  // rows first.., clamped to `last`
+  __device__ Rows(const char *base, int64_t pitch, int first, int last) {
+    const int lane = threadIdx.x % WAVE;
+#pragma unroll
+    for (int i = 0; i < ROWS / 8; ++i) {
+      const int row = first + i * 8 + lane / 8;
+      at[i] = base + (row < last ? row : last) * pitch + lane % 8 * 16;
+    }
+  }
+  __device__ void load(u32x4 (&r)[ROWS / 8], int slice) const {
+#pragma unroll
+    for (int i = 0; i < ROWS / 8; ++i) r[i] = *(const typename Raw<unsigned, 4>::type *)(at[i] + slice * SLICE);
+  }
+  // the last slice, of `len` bytes
+  template <bool X8>
+  __device__ void load_part(u32x4 (&r)[ROWS / 8], int slice, int len) const {
+#pragma unroll
+    for (int i = 0; i < ROWS / 8; ++i)
+      r[i] = chunk<X8>(at[i] + slice * SLICE, 0, len - (int)(threadIdx.x % 8) * 16);
+  }
+  __device__ static void put(char *corner, const u32x4 (&r)[ROWS / 8]) {
+    const int lane = threadIdx.x % WAVE;
+#pragma unroll
+    for (int i = 0; i < ROWS / 8; ++i) *(u32x4 *)(corner + spot(i * 8 + lane / 8, lane % 8)) = r[i];
+  }
+};
+
+// ------------------------------------------------------------------ v = gain x A^T
 
 // Eight elements of a row from element k on, zeros from `len` on.
 template <typename T>
@@ -90,209 +153,458 @@ __device__ inline typename Mma<T>::frag eight(const T *row, int k, int len) {
   return f;
 }
 
-// The same of a row of 8-bit integers, which both 16-bit types hold exactly.
-template <typename T>
-__device__ inline typename Mma<T>::frag eight(const int8_t *row, int k, int len) {
-  typename Mma<T>::frag f;
-  if (k + 8 <= len) {
-    const typename Raw<int8_t, 8>::type c = *(const typename Raw<int8_t, 8>::type *)(row + k);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = (T)(float)c[i];
-    return f;
-  }
-#pragma unroll
-  for (int i = 0; i < 8; ++i) f[i] = k + i < len ? (T)(float)row[k + i] : (T)0.0f;
-  return f;
-}
+constexpr int DOWN_ROWS = 32, DOWN_WAVES = 8;
 
-constexpr int DOWN_ROWS = 32, DOWN_WAVES = 4;
-
-// A workgroup takes 32 rows and one split of the inner dimension, each wave a quarter of the split;
-// RC * 16 ranks at a time.  Of the adapters among its rows it takes every gridDim.z-th.
-template <typename T, typename X, int RC>
+// A workgroup takes 32 rows, each of its waves one contiguous part of the inner dimension, RC * 16
+// ranks at a time.  Of the adapters among its rows it takes every gridDim.y-th.  8-bit rows become
+// 16-bit ones on their way into LDS (both 16-bit types hold them exactly): a slice of them is 64
+// elements too.
+template <typename T, bool X8, int RC>
 __global__ __launch_bounds__(DOWN_WAVES *WAVE) void down_kernel(ProjectParams p) {
-  __shared__ float part[DOWN_WAVES][RC * 2][WAVE][4];
-  const int lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE;
+  constexpr int DEPTH = RC == 4 ? 2 : RC == 2 && X8 ? 3 : 4, RANKS = RC * 16, CORNER = (RANKS + DOWN_ROWS) * SLICE, SUMS = RC * 2 * WAVE * 16;
+  __shared__ __align__(16) char room[DOWN_WAVES * (CORNER > SUMS ? CORNER : SUMS)];
+  const int lane = threadIdx.x % WAVE, wave = wave_index();
   const int row0 = blockIdx.x * DOWN_ROWS, m = lane % 16, q = lane / 16;
-  const int lo = blockIdx.y * p.split_len;
-  const int hi = lo + p.split_len < p.in_dim ? lo + p.split_len : p.in_dim;
-  const X *xr[2];
+  char *const corner = room + wave * CORNER;
+  // x: eight lanes a row and eight elements a lane
+  const char *xr[DOWN_ROWS / 8];
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const int row = row0 + j * 16 + m;
-    xr[j] = (const X *)(p.x + (row < p.rows ? row : p.rows - 1) * p.x_pitch);
+  for (int i = 0; i < DOWN_ROWS / 8; ++i) {
+    const int row = row0 + i * 8 + lane / 8;
+    xr[i] = p.x + (row < p.rows ? row : p.rows - 1) * p.x_pitch + lane % 8 * (X8 ? 8 : 16);
   }
+  typedef typename Raw<unsigned, X8 ? 2 : 4>::type xword;
+  const int full = p.in_dim / 64;  // whole slices; the wave's are those from lo to hi
+  const int lo = full * wave / DOWN_WAVES, hi = full * (wave + 1) / DOWN_WAVES;
   const int mine = lane < DOWN_ROWS && row0 + lane < p.rows ? adapter_of(p, row0 + lane) : -1;
   unsigned long long left = __ballot(mine >= 0);
   for (int n = 0; left; ++n) {
-    const int a = __shfl(mine, __builtin_ctzll(left));
+    const int a = __builtin_amdgcn_readlane(mine, __builtin_ctzll(left));
     const unsigned long long these = __ballot(mine == a);
     left &= ~these;
-    if (n % (int)gridDim.z != (int)blockIdx.z) continue;
+    if (n % (int)gridDim.y != (int)blockIdx.y) continue;
     const int rank = rank_of(p, a);
-    const T *const down = (const T *)p.down + (int64_t)a * p.max_rank * p.in_dim;
-    for (int r0 = 0; r0 < rank; r0 += RC * 16) {
+    const float gain = p.gain[a];
+    const char *const down = (const char *)p.down + (int64_t)a * p.max_rank * p.in_dim * 2;
+    for (int r0 = 0; r0 < p.slabs * 32; r0 += RANKS) {
       f32x4 acc[RC][2];
 #pragma unroll
       for (int c = 0; c < RC; ++c) acc[c][0] = acc[c][1] = (f32x4){0, 0, 0, 0};
-      for (int k = lo + wave * 32 + q * 8; k < ((hi + 31) & ~31); k += DOWN_WAVES * 32) {
-        typename Mma<T>::frag xf[2], af[RC];
+      if (r0 < rank) {
+        // ranks behind the last are its copies here, and zeros in v
+        const Rows<RANKS> ar(down, (int64_t)p.in_dim * 2, r0, rank - 1);
+        u32x4 av[DEPTH][RANKS / 8];
+        xword xv[DEPTH][DOWN_ROWS / 8];
+        auto load = [&](int d, int s) {
+          ar.load(av[d], s);
 #pragma unroll
-        for (int j = 0; j < 2; ++j) xf[j] = eight<T>(xr[j], k, hi);
+          for (int i = 0; i < DOWN_ROWS / 8; ++i) xv[d][i] = *(const xword *)(xr[i] + s * (X8 ? 64 : 128));
+        };
+        auto multiply = [&](int d) {
+          Rows<RANKS>::put(corner, av[d]);
 #pragma unroll
-        for (int c = 0; c < RC; ++c) {
-          const int r = r0 + c * 16 + m;
-          af[c] = eight<T>(down + (int64_t)(r < rank ? r : 0) * p.in_dim, k, r < rank ? hi : 0);
+          for (int i = 0; i < DOWN_ROWS / 8; ++i) {
+            char *const to = corner + RANKS * SLICE + spot(i * 8 + lane / 8, lane % 8);
+            if constexpr (X8) {
+              typedef signed char c8 __attribute__((ext_vector_type(8)));
+              typedef unsigned u2 __attribute__((ext_vector_type(2)));
+              const c8 c = __builtin_bit_cast(c8, (u2)xv[d][i]);
+              typename Mma<T>::frag f;
+#pragma unroll
+              for (int e = 0; e < 8; ++e) f[e] = (T)(float)c[e];
+              *(typename Mma<T>::frag *)to = f;
+            } else {
+              *(u32x4 *)to = xv[d][i];
+            }
+          }
+          typedef typename Mma<T>::frag frag;
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            frag xf[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) xf[j] = *(const frag *)(corner + RANKS * SLICE + spot(j * 16 + m, k * 4 + q));
+#pragma unroll
+            for (int c = 0; c < RC; ++c) {
+              const frag af = *(const frag *)(corner + spot(c * 16 + m, k * 4 + q));
+#pragma unroll
+              for (int j = 0; j < 2; ++j) acc[c][j] = Mma<T>::m16(af, xf[j], acc[c][j]);
+            }
+          }
+        };
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d)
+          if (lo + d < hi) load(d, lo + d);
+        for (int s = lo; s < hi; s += DEPTH) {
+#pragma unroll
+          for (int d = 0; d < DEPTH; ++d) {
+            if (s + d >= hi) break;
+            multiply(d);
+            if (s + d + DEPTH < hi) load(d, s + d + DEPTH);
+          }
         }
+        if (full * 64 < p.in_dim && wave == 0) {
+          const int rest = p.in_dim - full * 64;
+          ar.template load_part<false>(av[0], full, rest * 2);
 #pragma unroll
-        for (int c = 0; c < RC; ++c)
+          for (int i = 0; i < DOWN_ROWS / 8; ++i) {
+            const u32x4 v = chunk<X8>(xr[i] + full * (X8 ? 64 : 128), 0, (rest - lane % 8 * 8) * (X8 ? 1 : 2));
 #pragma unroll
-          for (int j = 0; j < 2; ++j) acc[c][j] = Mma<T>::m16(af[c], xf[j], acc[c][j]);
+            for (int e = 0; e < (X8 ? 2 : 4); ++e) xv[0][i][e] = v[e];
+          }
+          multiply(0);
+        }
       }
-      __syncthreads();  // the previous round's sums have been read
+      __syncthreads();  // the waves' corners have been read
 #pragma unroll
       for (int c = 0; c < RC; ++c)
 #pragma unroll
-        for (int j = 0; j < 2; ++j) *(f32x4 *)part[wave][c * 2 + j][lane] = acc[c][j];
+        for (int j = 0; j < 2; ++j) *(f32x4 *)(room + wave * SUMS + ((c * 2 + j) * WAVE + lane) * 16) = acc[c][j];
       __syncthreads();
-      // entry e = (chunk of ranks, half of the rows): lane's four consecutive ranks of one row
+      // entry e = (chunk of ranks, half of the rows): a lane's four consecutive ranks of one row
       for (int e = wave; e < RC * 2; e += DOWN_WAVES) {
         f32x4 s = (f32x4){0, 0, 0, 0};
 #pragma unroll
-        for (int i = 0; i < DOWN_WAVES; ++i) s += *(const f32x4 *)part[i][e][lane];
-        const int local = (e % 2) * 16 + m, r = r0 + e / 2 * 16 + q * 4;
-        if ((these >> local & 1) && r < p.rank_pad) {
-          float *dst = p.v + ((int64_t)blockIdx.y * p.rows + row0 + local) * p.rank_pad + r;
-          *(f32x4 *)dst = s;
+        for (int i = 0; i < DOWN_WAVES; ++i) s += *(const f32x4 *)(room + i * SUMS + (e * WAVE + lane) * 16);
+        const int local = (e % 2) * 16 + m, r = r0 + e / 2 * 16 + q * 4, row = row0 + local;
+        if (!(these >> local & 1) || r >= p.slabs * 32) continue;
+        s *= X8 ? gain * p.x_scale[row] : gain;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[i] = r + i < rank ? s[i] : 0.0f;
+        if (p.split) {
+          T *const dst = (T *)p.v + ((int64_t)(r / 32) * p.rows + row) * 64 + r % 32;
+          float high[4], low[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            high[i] = (float)(T)s[i];
+            low[i] = s[i] - high[i];
+          }
+          store_f32<T, 4>(dst, high);
+          store_f32<T, 4>(dst + 32, low);
+        } else {
+          *(f32x4 *)((float *)p.v + (int64_t)row * p.slabs * 32 + r) = s;
         }
       }
+      __syncthreads();  // the sums have been read
     }
   }
 }
 
-// v of one row and rank, times the adapter's gain (and the row's scale of 8-bit rows)
-template <bool X8>
-__device__ inline float low_rank(const ProjectParams &p, int row, int a, int r) {
-  float s = 0.0f;
-  for (int i = 0; i < p.splits; ++i) s += p.v[((int64_t)i * p.rows + row) * p.rank_pad + r];
-  s *= p.gain[a];
-  return X8 ? s * p.x_scale[row] : s;
-}
+// ------------------------------------------------------------------ few rows: W streams through
 
-// ------------------------------------------------------------------ out = x W^T + v B^T
-
-__device__ const u32x4 edge_zeros = {0, 0, 0, 0};
-
-constexpr int SLICE = 128;  // bytes of the inner dimension staged at a time: 64 or 128 elements
-
-// Where 16-byte chunk c of row r of a staged slice stands: rows of 128 bytes, chunks exchanged
-// within the row so that eight rows' equal chunks fall on different LDS banks.
-__device__ inline int spot(int r, int c) { return r * SLICE + ((c ^ (r & 7)) << 4); }
-
-template <typename T, bool X8, bool FAST, int BM, int BN, int WM, int WN>
-struct Tile {
-  static constexpr int WAVES = WM * WN, THREADS = WAVES * WAVE;
-  static constexpr int FM = BM / WM / 32, FN = BN / WN / 32;  // 32x32 tiles a wave: rows, columns
-  static constexpr int STAGE = (BM + BN) * SLICE;
-
-  // Stages `count` rows' slice (bytes [at, at + 128) of rows first.., clamped to `last`) at dst.
-  template <int COUNT>
-  __device__ static void stage(char *dst, const char *base, int64_t pitch, int first, int last,
-                               int at, int len) {
-#pragma unroll
-    for (int i = 0; i < COUNT * 8 / THREADS; ++i) {
-      const int slot = i * THREADS + threadIdx.x, r = slot / 8, c = (slot % 8) ^ (r & 7);
-      const int row = first + r < last ? first + r : last;
-      const int byte = at + c * 16;
-      const char *src = base + row * pitch + byte;
-      if constexpr (FAST) {
-        // rows are whole multiples of 16 bytes: a chunk lies within the row or behind it
-        const char *from = byte < len ? src : (const char *)&edge_zeros;
-        __builtin_amdgcn_global_load_lds(
-            (const __attribute__((address_space(1))) unsigned *)from,
-            (__attribute__((address_space(3))) unsigned *)(dst + (i * THREADS + (threadIdx.x & ~63)) * 16),
-            16, 0, 0);
-      } else {
-        u32x4 v = {0, 0, 0, 0};
-        if (byte + 16 <= len) {
-          v = *(const typename Raw<unsigned, 4>::type *)src;
-        } else if (byte < len) {
-          constexpr int E = X8 ? 1 : 2;
-          unsigned char b[16];
-#pragma unroll
-          for (int j = 0; j < 16 / E; ++j) {
-            const bool in = byte + j * E < len;
-            if constexpr (X8) {
-              b[j] = in ? (unsigned char)src[j] : 0;
-            } else {
-              const unsigned short h = in ? ((const unsigned short *)src)[j] : 0;
-              b[2 * j] = (unsigned char)h;
-              b[2 * j + 1] = (unsigned char)(h >> 8);
-            }
-          }
-          __builtin_memcpy(&v, b, 16);
-        }
-        *(u32x4 *)(dst + slot * 16) = v;
-      }
-    }
+// Products of 16 rows of W with 16 of x: 16 bytes a lane of either, 16-bit or 8-bit.
+template <typename T, bool X8>
+struct Small {
+  typedef f32x4 acc;
+  __device__ static acc mma(u32x4 a, u32x4 b, acc c) {
+    typedef typename Mma<T>::frag frag;
+    return Mma<T>::m16(__builtin_bit_cast(frag, a), __builtin_bit_cast(frag, b), c);
+  }
+};
+template <typename T>
+struct Small<T, true> {
+  typedef i32x4 acc;
+  __device__ static acc mma(u32x4 a, u32x4 b, acc c) {
+    return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), c, 0, 0, 0);
   }
 };
 
-// One workgroup: BM rows by BN columns, WM x WN waves.  W's rows are the products' first operand,
-// so a lane holds four consecutive columns of one row.
-template <typename T, bool X8, bool FAST, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(WM *WN *WAVE) void tile_kernel(ProjectParams p) {
-  typedef Tile<T, X8, FAST, BM, BN, WM, WN> K;
-  __shared__ __align__(16) char buf0[K::STAGE], buf1[K::STAGE];
-  __shared__ int ids[BM];
-  const int lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE;
-  const int wm = wave / WN, wn = wave % WN, l32 = lane % 32, half = lane / 32;
-  const int tiles_n = (p.out_dim + BN - 1) / BN;
-  const int row0 = (int)blockIdx.x / tiles_n * BM, col0 = (int)blockIdx.x % tiles_n * BN;
-  const int len = p.in_dim * (X8 ? 1 : 2), slices = (len + SLICE - 1) / SLICE;
+// One row's low-rank part of one column: v . B's row, whole eights of either in registers as far as
+// RANKS goes, which are loaded long before they are used.
+template <typename T, int RANKS>
+struct LowRank {
+  int rank = 0;
+  const float *v;
+  const T *b;
+  f32x4 vf[RANKS / 4];
+  typename Mma<T>::frag bf[RANKS / 8];
 
-  auto stage = [&](char *buf, int s) {
-    K::template stage<BM>(buf, p.x, p.x_pitch, row0, p.rows - 1, s * SLICE, len);
-    K::template stage<BN>(buf + BM * SLICE, p.w, p.w_pitch, col0, p.out_dim - 1, s * SLICE, len);
-  };
-  typename Main<T, X8>::acc acc[K::FM][K::FN] = {};
-  auto multiply = [&](const char *buf) {
+  __device__ void load(const ProjectParams &p, int row, int col) {
+    const int a = row < p.rows && col < p.out_dim ? adapter_of(p, row) : -1;
+    if (a < 0) return;
+    rank = rank_of(p, a);
+    v = (const float *)p.v + (int64_t)row * p.slabs * 32;  // zeros from the rank to a multiple of 32
+    b = (const T *)p.up + ((int64_t)a * p.out_dim + col) * p.max_rank;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {  // 32 bytes of the inner dimension each
-      u32x4 xf[K::FM], wf[K::FN];
+    for (int r = 0; r < RANKS; r += 8)
+      if (r + 8 <= rank) {
+        bf[r / 8] = *(const typename Raw<T, 8>::type *)(b + r);
+        vf[r / 4] = *(const f32x4 *)(v + r);
+        vf[r / 4 + 1] = *(const f32x4 *)(v + r + 4);
+      }
+  }
+  __device__ float value() const {
+    float y = 0.0f;
 #pragma unroll
-      for (int i = 0; i < K::FM; ++i)
-        xf[i] = *(const u32x4 *)(buf + spot((wm * K::FM + i) * 32 + l32, k * 2 + half));
+    for (int r = 0; r < RANKS; r += 8)
+      if (r + 8 <= rank)
 #pragma unroll
-      for (int j = 0; j < K::FN; ++j)
-        wf[j] = *(const u32x4 *)(buf + BM * SLICE + spot((wn * K::FN + j) * 32 + l32, k * 2 + half));
+        for (int k = 0; k < 8; ++k) y += vf[r / 4 + k / 4][k % 4] * (float)bf[r / 8][k];
+    for (int r = rank < RANKS ? rank & ~7 : RANKS; r < rank; r += 8) {
+      const typename Mma<T>::frag f = eight<T>(b, r, rank);
 #pragma unroll
-      for (int i = 0; i < K::FM; ++i)
+      for (int k = 0; k < 8; ++k) y += v[r + k] * (float)f[k];
+    }
+    return y;
+  }
+};
+
+// A workgroup takes 16 columns and all rows (NT * 16); each wave takes one contiguous part of the inner
+// dimension, and their sums meet in LDS.  DW slices of W and DX of x are under way (W comes from
+// memory, x from the cache that all workgroups share).
+template <typename T, bool X8, int NT, int WAVES, int DW, int DX>
+__global__ __launch_bounds__(WAVES *WAVE) void stream_kernel(ProjectParams p) {
+  typedef typename Small<T, X8>::acc acc_t;
+  static_assert(DW % DX == 0, "rings");
+  constexpr int THREADS = WAVES * WAVE, OUTPUTS = NT * 256, EACH = (OUTPUTS + THREADS - 1) / THREADS;
+  constexpr int CORNER = (1 + NT) * 16 * SLICE;
+  __shared__ __align__(16) char room[WAVES * CORNER];
+  const int lane = threadIdx.x % WAVE, wave = wave_index(), m = lane % 16, q = lane / 16;
+  const int col0 = blockIdx.x * 16, len = p.in_dim * (X8 ? 1 : 2);
+  const Rows<16> wr(p.w, p.w_pitch, col0, p.out_dim - 1);
+  const Rows<NT * 16> xr(p.x, p.x_pitch, 0, p.rows - 1);
+  const int full = len / SLICE;  // whole slices; the wave's are those from lo to hi
+  const int lo = full * wave / WAVES, hi = full * (wave + 1) / WAVES;
+  u32x4 w[DW][2], x[DX][NT * 2];
 #pragma unroll
-        for (int j = 0; j < K::FN; ++j) acc[i][j] = Main<T, X8>::mma(wf[j], xf[i], acc[i][j]);
+  for (int d = 0; d < DW; ++d)
+    if (lo + d < hi) wr.load(w[d], lo + d);
+#pragma unroll
+  for (int d = 0; d < DX; ++d)
+    if (lo + d < hi) xr.load(x[d], lo + d);
+  // the thread's outputs: row (e * THREADS + threadIdx.x) / 16, column col0 + threadIdx.x % 16
+  LowRank<T, 16> low[EACH];
+  if (p.num_adapters > 0) {
+#pragma unroll
+    for (int e = 0; e < EACH; ++e)
+      low[e].load(p, (e * THREADS + (int)threadIdx.x) / 16, col0 + threadIdx.x % 16);
+  }
+  acc_t acc[NT] = {};
+  char *const corner = room + wave * CORNER;
+  auto multiply = [&](const u32x4 (&wv)[2], const u32x4 (&xv)[NT * 2]) {
+    Rows<16>::put(corner, wv);
+    Rows<NT * 16>::put(corner + 16 * SLICE, xv);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const u32x4 wf = *(const u32x4 *)(corner + spot(m, h * 4 + q));
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+        acc[t] = Small<T, X8>::mma(wf, *(const u32x4 *)(corner + 16 * SLICE + spot(t * 16 + m, h * 4 + q)), acc[t]);
     }
   };
-  stage(buf0, 0);
-  for (int s = 0; s < slices; s += 2) {
+  for (int s = lo; s < hi; s += DW) {
+#pragma unroll
+    for (int d = 0; d < DW; ++d) {
+      if (s + d >= hi) break;
+      multiply(w[d], x[d % DX]);
+      if (s + d + DW < hi) wr.load(w[d], s + d + DW);
+      if (s + d + DX < hi) xr.load(x[d % DX], s + d + DX);
+    }
+  }
+  if (full * SLICE < len && wave == 0) {
+    wr.template load_part<X8>(w[0], full, len - full * SLICE);
+    xr.template load_part<X8>(x[0], full, len - full * SLICE);
+    multiply(w[0], x[0]);
+  }
+  __syncthreads();  // the waves' corners have been read
+#pragma unroll
+  for (int t = 0; t < NT; ++t) *(acc_t *)(room + ((wave * NT + t) * WAVE + lane) * 16) = acc[t];
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < EACH; ++e) {
+    const int o = e * THREADS + threadIdx.x, row = o / 16, c = o % 16;
+    if (o >= OUTPUTS || row >= p.rows || col0 + c >= p.out_dim) continue;
+    auto part = [&](int w) { return (*(const acc_t *)(room + ((w * NT + row / 16) * WAVE + c / 4 * 16 + row % 16) * 16))[c % 4]; };
+    auto sum = part(0);
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) sum += part(w);
+    float y = (float)sum;
+    if constexpr (X8) y *= p.x_scale[row] * p.w_scale[col0 + c];
+    if (p.num_adapters > 0) y += low[e].value();
+    ((T *)p.out)[row * p.out_stride + col0 + c] = (T)y;
+  }
+}
+
+// ------------------------------------------------------------------ many rows: tiles
+
+__device__ const u32x4 edge_zeros = {0, 0, 0, 0};
+
+// Stages COUNT rows' slice (bytes [at, at + 128) of rows first.., clamped to `last`) at dst.  DIRECT:
+// memory to LDS, without registers between; needs chunks that lie within the row or behind it.
+template <bool X8, bool DIRECT, int COUNT, int THREADS>
+__device__ inline void stage(char *dst, const char *base, int64_t pitch, int first, int last, int at, int len) {
+  static_assert(COUNT * 8 % THREADS == 0, "whole rounds");
+  const char *const tile = base + first * pitch + at;
+  auto each = [&](auto one) {
+#pragma unroll
+    for (int i = 0; i < COUNT * 8 / THREADS; ++i) {
+      const int slot = i * THREADS + threadIdx.x, r = slot / 8, c = (slot % 8) ^ (r & 7);
+      one(i * THREADS, first + r < last ? r : last - first, c * 16);
+    }
+  };
+  const unsigned to = lds_address(dst) + wave_index() * WAVE * 16;
+  if constexpr (!DIRECT) {
+    each([&](int s0, int r, int byte) {
+      *(u32x4 *)(dst + (s0 + threadIdx.x) * 16) = chunk<X8>(tile + r * pitch + byte, 0, len - at - byte);
+    });
+  } else if (at + SLICE <= len) {
+    each([&](int s0, int r, int byte) { load_to_lds(tile, (unsigned)r * (unsigned)pitch + byte, to + s0 * 16); });
+  } else {
+    each([&](int s0, int r, int byte) {
+      load_to_lds(at + byte < len ? tile + r * pitch + byte : (const char *)&edge_zeros, to + s0 * 16);
+    });
+  }
+}
+
+template <typename T, bool X8, bool DIRECT, int BM, int BN, int WM, int WN, int STAGES>
+struct Tile {
+  static constexpr int THREADS = WM * WN * WAVE;
+  static constexpr int FM = BM / WM / 32, FN = BN / WN / 32;  // 32x32 tiles a wave: rows, columns
+  static constexpr int STAGE = (BM + BN) * SLICE;             // bytes
+  static constexpr int LOADS = STAGE / 16 / THREADS;          // a thread's, each stage
+  static constexpr int OUT = BM * BN * 2;
+  static constexpr int ROOM = STAGES * STAGE > OUT ? STAGES * STAGE : OUT;
+};
+
+// One workgroup: BM rows by BN columns, WM x WN waves.  W's rows are the products' first operand,
+// so a lane holds four consecutive columns of one row.  STAGES - 1 slices are under way while one
+// is multiplied.  Behind the slices of the inner dimension come those of the low-rank part: for each
+// adapter among the tile's rows, 32 ranks at a time, the rows' two-part v and the columns' B twice.
+// Their product is added to the adapter's own rows only (zeros times an infinity are not zero), so
+// other rows' v may be anything.  ROWWISE: few rows with many adapters, where each output's low-rank
+// part is computed by itself.
+template <typename T, bool X8, bool DIRECT, int BM, int BN, int WM, int WN, int STAGES, bool ROWWISE>
+__global__ __launch_bounds__(WM *WN *WAVE) void tile_kernel(ProjectParams p) {
+  typedef Tile<T, X8, DIRECT, BM, BN, WM, WN, STAGES> K;
+  typedef typename Mma<T>::frag frag;
+  __shared__ __align__(16) char room[K::ROOM];
+  __shared__ int ids[BM], list[BM], listed;
+  const int lane = threadIdx.x % WAVE, wave = wave_index();
+  const int wm = wave / WN, wn = wave % WN, l32 = lane % 32, half = lane / 32;
+  const int tiles_m = (p.rows + BM - 1) / BM, tiles_n = (p.out_dim + BN - 1) / BN;
+  // Workgroups go to the chip's eight dies in turn: each die takes a contiguous run of tiles, in
+  // groups of eight tiles of rows, so that what its cache holds serves several tiles.
+  const int total = tiles_m * tiles_n, die = blockIdx.x % 8, slot = blockIdx.x / 8;
+  const int tile = die * (total / 8) + (die < total % 8 ? die : total % 8) + slot;
+  const int group = tile / (8 * tiles_n), high = tiles_m - group * 8 < 8 ? tiles_m - group * 8 : 8;
+  const int in_group = tile - group * 8 * tiles_n;
+  const int row0 = (group * 8 + in_group % high) * BM, col0 = in_group / high * BN;
+  const int len = p.in_dim * (X8 ? 1 : 2), slices = (len + SLICE - 1) / SLICE;
+
+  // the dies start at different places of the inner dimension and do not all ask for the same ones
+  const int turn = slices * die / 8;
+  auto load = [&](int t) {
+    char *const buf = room + t % STAGES * K::STAGE;
+    const int s = t + turn < slices ? t + turn : t + turn - slices;
+    stage<X8, DIRECT, BM, K::THREADS>(buf, p.x, p.x_pitch, row0, p.rows - 1, s * SLICE, len);
+    stage<X8, DIRECT, BN, K::THREADS>(buf + BM * SLICE, p.w, p.w_pitch, col0, p.out_dim - 1, s * SLICE, len);
+  };
+  // slice n of the low-rank part, which is slice slices + n of all
+  auto load_low = [&](int n) {
+    char *const buf = room + (slices + n) % STAGES * K::STAGE;
+    const int a = __builtin_amdgcn_readfirstlane(list[n / p.slabs]), slab = n % p.slabs;
+    stage<false, true, BM, K::THREADS>(buf, (const char *)p.v + (int64_t)slab * p.rows * SLICE, SLICE, row0,
+                                       p.rows - 1, 0, SLICE);
+    const int left = rank_of(p, a) - slab * 32;
+    const T *const up = (const T *)p.up + ((int64_t)a * p.out_dim + col0) * p.max_rank + slab * 32;
+    const bool direct = (left % 8 == 0 || left >= 32) && p.max_rank % 8 == 0 && (uintptr_t)p.up % 16 == 0;
+    const unsigned to = lds_address(buf + BM * SLICE) + wave * WAVE * 16;
+#pragma unroll
+    for (int i = 0; i < BN * 8 / K::THREADS; ++i) {
+      const int e = i * K::THREADS + threadIdx.x, c = e / 8, r = ((e % 8) ^ (c & 7)) % 4 * 8;
+      const bool in = col0 + c < p.out_dim && r < left;
+      const T *const from = up + (in ? (int64_t)c * p.max_rank + r : 0);
+      if (direct) {
+        load_to_lds(in ? (const void *)from : (const void *)&edge_zeros, to + i * K::THREADS * 16);
+      } else {
+        frag f = {};
+        if (in) f = eight<T>(from, 0, left - r);
+        *(frag *)(buf + BM * SLICE + e * 16) = f;
+      }
+    }
+  };
+  typename Main<T, X8>::acc acc[K::FM][K::FN] = {};
+#pragma unroll
+  for (int s = 0; s < STAGES - 1; ++s)
+    if (s < slices) load(s);
+  int behind = 0;  // slices of the low-rank part
+  if (!ROWWISE && p.num_adapters > 0) {
+    for (int r0 = wave * WAVE; r0 < BM; r0 += K::THREADS) {
+      const int r = r0 + lane, a = r < BM && row0 + r < p.rows ? adapter_of(p, row0 + r) : -1;
+      if (r < BM) ids[r] = a;
+    }
     __syncthreads();
-    if (s + 1 < slices) stage(buf1, s + 1);
-    multiply(buf0);
-    if (s + 1 < slices) {
-      __syncthreads();
-      if (s + 2 < slices) stage(buf0, s + 2);
-      multiply(buf1);
+    if (wave == 0) {  // the adapters, each once
+      int n = 0;
+      for (int r0 = 0; r0 < BM; r0 += WAVE) {
+        int a = r0 + lane < BM ? ids[r0 + lane] : -1;
+        for (int i = 0; i < n; ++i) a = a == list[i] ? -1 : a;
+        unsigned long long left = __ballot(a >= 0);
+        while (left) {
+          const int b = __builtin_amdgcn_readlane(a, __builtin_ctzll(left));
+          left &= ~__ballot(a == b);
+          if (lane == 0) list[n] = b;
+          ++n;
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      }
+      if (lane == 0) listed = n;
+    }
+    __syncthreads();
+    behind = __builtin_amdgcn_readfirstlane(listed) * p.slabs;
+#pragma unroll
+    for (int s = 0; s < STAGES - 1; ++s)
+      if (s >= slices && s - slices < behind) load_low(s - slices);
+  }
+  // this slice has landed and the slice before it has been read, by all waves; the next one is on its way
+  auto advance = [&](int s) {
+    if (DIRECT && s + STAGES - 2 < slices) {
+      wait_loads<(STAGES - 2) * K::LOADS>();
+    } else {
+      wait_loads<0>();
+    }
+    barrier();
+    const int next = s + STAGES - 1;
+    if (next < slices) {
+      load(next);
+    } else if (next - slices < behind) {
+      load_low(next - slices);
+    }
+  };
+  for (int s = 0; s < slices; ++s) {
+    advance(s);
+    const char *const buf = room + s % STAGES * K::STAGE;
+    u32x4 xf[2][K::FM], wf[2][K::FN];
+    auto fetch = [&](int b, int k) {  // 32 bytes of the inner dimension
+#pragma unroll
+      for (int i = 0; i < K::FM; ++i)
+        xf[b][i] = *(const u32x4 *)(buf + spot((wm * K::FM + i) * 32 + l32, k * 2 + half));
+#pragma unroll
+      for (int j = 0; j < K::FN; ++j)
+        wf[b][j] = *(const u32x4 *)(buf + BM * SLICE + spot((wn * K::FN + j) * 32 + l32, k * 2 + half));
+    };
+    fetch(0, 0);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (k < 3) fetch((k + 1) & 1, k + 1);
+#pragma unroll
+      for (int i = 0; i < K::FM; ++i)
+#pragma unroll
+        for (int j = 0; j < K::FN; ++j) acc[i][j] = Main<T, X8>::mma(wf[k & 1][j], xf[k & 1][i], acc[i][j]);
     }
   }
 
   // to binary32, with the scales of 8-bit rows and columns
   f32x16 sum[K::FM][K::FN];
 #pragma unroll
-  for (int i = 0; i < K::FM; ++i)
+  for (int i = 0; i < K::FM; ++i) {
+    float xs = 1.0f;
+    if constexpr (X8) {
+      const int row = row0 + (wm * K::FM + i) * 32 + l32;
+      xs = p.x_scale[row < p.rows ? row : p.rows - 1];
+    }
 #pragma unroll
     for (int j = 0; j < K::FN; ++j) {
       if constexpr (X8) {
-        const int row = row0 + (wm * K::FM + i) * 32 + l32;
-        const float xs = p.x_scale[row < p.rows ? row : p.rows - 1];
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           const int col = col0 + (wn * K::FN + j) * 32 + 8 * (e / 4) + 4 * half + e % 4;
@@ -302,103 +614,85 @@ __global__ __launch_bounds__(WM *WN *WAVE) void tile_kernel(ProjectParams p) {
         sum[i][j] = acc[i][j];
       }
     }
-
-  if (p.num_adapters > 0) {
-    // For each adapter among the tile's rows, 32 ranks at a time: the rows' v (zeros for rows of
-    // other adapters) as two 16-bit parts whose sum is v to 16 (22) bits, and the columns' B.
-    // The product is added to the adapter's own rows only: zeros times an infinity are not zero.
-    char *const vbuf = buf0, *const bbuf = buf0 + BM * SLICE;
-    __syncthreads();
-    for (int r = threadIdx.x; r < BM; r += K::THREADS)
-      ids[r] = row0 + r < p.rows ? adapter_of(p, row0 + r) : -1;
-    __syncthreads();
-    int done = 0;  // rows before it belong to adapters that have been applied
-    while (true) {
-      while (done < BM) {
-        const int a = ids[done];
-        bool seen = a < 0;
-        for (int r = 0; r < done && !seen; ++r) seen = ids[r] == a;
-        if (!seen) break;
-        ++done;
+  }
+  for (int n = 0; n < behind; ++n) {
+    advance(slices + n);
+    const char *const buf = room + (slices + n) % STAGES * K::STAGE;
+    const int a = __builtin_amdgcn_readfirstlane(list[n / p.slabs]);
+#pragma unroll
+    for (int i = 0; i < K::FM; ++i) {
+      const int r = (wm * K::FM + i) * 32 + l32;
+      const bool mine = ids[r] == a;
+      if (!__any(mine)) continue;
+      frag v[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = *(const frag *)(buf + spot(r, k * 2 + half));
+#pragma unroll
+      for (int j = 0; j < K::FN; ++j) {
+        f32x16 more = {};
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          more = Mma<T>::m32(*(const frag *)(buf + BM * SLICE + spot((wn * K::FN + j) * 32 + l32, k * 2 + half)), v[k], more);
+        if (mine) sum[i][j] += more;
       }
-      if (done >= BM) break;
-      const int a = ids[done++], rank = rank_of(p, a);
-      const T *const up = (const T *)p.up + (int64_t)a * p.out_dim * p.max_rank;
-      for (int r0 = 0; r0 < rank; r0 += 32) {
-        __syncthreads();
-        for (int e = threadIdx.x; e < BM * 32; e += K::THREADS) {
-          const int r = e / 32, k = e % 32;
-          const float v = ids[r] == a && r0 + k < rank ? low_rank<X8>(p, row0 + r, a, r0 + k) : 0.0f;
-          const T high = (T)v, low = (T)(v - (float)high);
-          *(T *)(vbuf + spot(r, k / 8) + k % 8 * 2) = high;
-          *(T *)(vbuf + spot(r, 4 + k / 8) + k % 8 * 2) = low;
-        }
-        for (int e = threadIdx.x; e < BN * 32; e += K::THREADS) {
-          const int c = e / 32, k = e % 32;
-          const bool in = col0 + c < p.out_dim && r0 + k < rank;
-          *(T *)(bbuf + spot(c, k / 8) + k % 8 * 2) =
-              in ? up[(int64_t)(col0 + c) * p.max_rank + r0 + k] : (T)0.0f;
-        }
-        __syncthreads();
-        typedef typename Mma<T>::frag frag;
+    }
+  }
+  if constexpr (ROWWISE) {
+    if (p.num_adapters > 0) {
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
+      for (int i = 0; i < K::FM; ++i) {
+        const int row = row0 + (wm * K::FM + i) * 32 + l32;
 #pragma unroll
-          for (int j = 0; j < K::FN; ++j) {
-            const frag b = *(const frag *)(bbuf + spot((wn * K::FN + j) * 32 + l32, k * 2 + half));
+        for (int j = 0; j < K::FN; ++j)
 #pragma unroll
-            for (int i = 0; i < K::FM; ++i) {
-              const int r = (wm * K::FM + i) * 32 + l32;
-              const frag h = *(const frag *)(vbuf + spot(r, k * 2 + half));
-              const frag l = *(const frag *)(vbuf + spot(r, 4 + k * 2 + half));
-              const f32x16 more = Mma<T>::m32(b, l, Mma<T>::m32(b, h, (f32x16){}));
-              if (ids[r] == a) sum[i][j] += more;
-            }
+          for (int e = 0; e < 16; e += 8) {
+            LowRank<T, 8> low[8];
+#pragma unroll
+            for (int c = 0; c < 8; ++c)
+              low[c].load(p, row, col0 + (wn * K::FN + j) * 32 + 8 * ((e + c) / 4) + 4 * half + c % 4);
+#pragma unroll
+            for (int c = 0; c < 8; ++c) sum[i][j][e + c] += low[c].value();
           }
       }
     }
   }
+  wait_loads<0>();
+  __syncthreads();  // all slices have been read
 
-  T *const out = (T *)p.out;
+  // The tile goes through LDS, so that rows are stored in runs of 16 bytes a lane: chunks of eight
+  // columns, exchanged within the row so that 32 rows' equal chunks fall on different banks.
+  constexpr int CHUNKS = BN / 8, SWAP = CHUNKS < 32 ? CHUNKS - 1 : 31;
 #pragma unroll
   for (int i = 0; i < K::FM; ++i) {
-    const int row = row0 + (wm * K::FM + i) * 32 + l32;
-    if (row >= p.rows) continue;
+    const int r = (wm * K::FM + i) * 32 + l32;
 #pragma unroll
     for (int j = 0; j < K::FN; ++j)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int col = col0 + (wn * K::FN + j) * 32 + 8 * e + 4 * half;
-        T *dst = out + row * p.out_stride + col;
-        float y[4] = {sum[i][j][4 * e], sum[i][j][4 * e + 1], sum[i][j][4 * e + 2], sum[i][j][4 * e + 3]};
-        if (col + 4 <= p.out_dim) {
-          store_f32<T, 4>(dst, y);
-        } else {
-#pragma unroll
-          for (int c = 0; c < 4; ++c)
-            if (col + c < p.out_dim) dst[c] = (T)y[c];
-        }
+        const int c = (wn * K::FN + j) * 4 + e;
+        const float y[4] = {sum[i][j][4 * e], sum[i][j][4 * e + 1], sum[i][j][4 * e + 2], sum[i][j][4 * e + 3]};
+        store_f32<T, 4>((T *)(room + r * (BN * 2) + ((c ^ (r & SWAP)) << 4) + half * 8), y);
       }
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < BM * CHUNKS; e += K::THREADS) {
+    const int r = e / CHUNKS, c = e % CHUNKS, col = col0 + c * 8;
+    if (row0 + r >= p.rows || col >= p.out_dim) continue;
+    const typename Mma<T>::frag y = *(const typename Mma<T>::frag *)(room + r * (BN * 2) + ((c ^ (r & SWAP)) << 4));
+    T *const dst = (T *)p.out + (row0 + r) * p.out_stride + col;
+    if (col + 8 <= p.out_dim) {
+      *(typename Raw<T, 8>::type *)dst = y;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (col + i < p.out_dim) dst[i] = y[i];
+    }
   }
 }
 
 // ------------------------------------------------------------------ host side
 
-struct DownPlan {
-  int rank_pad, splits, split_len;
-};
-
-// Splits of the inner dimension for v: enough workgroups for the chip at few rows, none shorter
-// than 256 elements.
-DownPlan down_plan(int rows, int in_dim, int max_rank) {
-  const int groups = (rows + DOWN_ROWS - 1) / DOWN_ROWS;
-  int splits = 512 / groups;
-  const int most = (in_dim + 255) / 256;
-  splits = splits < 1 ? 1 : splits > most ? most : splits;
-  splits = splits > 16 ? 16 : splits;
-  const int each = (in_dim + splits - 1) / splits, len = (each + 31) & ~31;
-  return {(max_rank + 15) & ~15, (in_dim + len - 1) / len, len};
-}
+constexpr int STREAM_ROWS = 64;  // up to here W streams through
 
 int project_check(const jdob_edge_project_args *a, bool sizes_only) {
   if (!a || a->rows < 0 || a->in_dim < 1 || a->out_dim < 1 || a->num_adapters < 0 ||
@@ -421,35 +715,62 @@ int project_check(const jdob_edge_project_args *a, bool sizes_only) {
   return JDOB_OK;
 }
 
-template <typename T, typename X>
+template <typename T, bool X8>
 int launch_down(const ProjectParams &p, hipStream_t stream) {
   const int groups = (p.rows + DOWN_ROWS - 1) / DOWN_ROWS;
   // few rows may all have adapters of their own: those are dealt to several workgroups
-  const dim3 grid((unsigned)groups, (unsigned)p.splits, groups <= 4 ? 8 : 1);
+  const dim3 grid((unsigned)groups, groups <= 4 ? (p.num_adapters < 32 ? p.num_adapters : 32) : 1);
   constexpr int threads = DOWN_WAVES * WAVE;
-  if (p.max_rank <= 16) return launch(down_kernel<T, X, 1>, grid, threads, stream, p);
-  if (p.max_rank <= 32) return launch(down_kernel<T, X, 2>, grid, threads, stream, p);
-  return launch(down_kernel<T, X, 4>, grid, threads, stream, p);
+  if (p.max_rank <= 16) return launch(down_kernel<T, X8, 1>, grid, threads, stream, p);
+  if (p.max_rank <= 32) return launch(down_kernel<T, X8, 2>, grid, threads, stream, p);
+  return launch(down_kernel<T, X8, 4>, grid, threads, stream, p);
 }
 
-template <typename T, bool X8, bool FAST, int BM, int BN, int WM, int WN>
+template <typename T, bool X8, int NT, int WAVES, int DW, int DX>
+int launch_stream(const ProjectParams &p, hipStream_t stream) {
+  return launch(stream_kernel<T, X8, NT, WAVES, DW, DX>, dim3((unsigned)((p.out_dim + 15) / 16)), WAVES * WAVE,
+                stream, p);
+}
+
+template <typename T, bool X8, bool DIRECT, int BM, int BN, int WM, int WN, int STAGES, bool ROWWISE = false>
 int launch_tile(const ProjectParams &p, hipStream_t stream) {
   const int64_t tiles = (int64_t)((p.rows + BM - 1) / BM) * ((p.out_dim + BN - 1) / BN);
   if (tiles > 0x7fffffff) return JDOB_ERR_UNSUPPORTED;
-  return launch(tile_kernel<T, X8, FAST, BM, BN, WM, WN>, dim3((unsigned)tiles), WM * WN * WAVE,
+  return launch(tile_kernel<T, X8, DIRECT, BM, BN, WM, WN, STAGES, ROWWISE>, dim3((unsigned)tiles), WM * WN * WAVE,
                 stream, p);
 }
+
+// Few rows with many adapters: the low-rank part output by output.
+bool rowwise(int rows, int num_adapters) { return rows <= 512 && num_adapters * 16 >= rows; }
 
 template <typename T, bool X8>
 int project(const ProjectParams &p, hipStream_t stream) {
   if (p.num_adapters > 0) {
-    const int code = X8 ? launch_down<T, int8_t>(p, stream) : launch_down<T, T>(p, stream);
+    const int code = launch_down<T, X8>(p, stream);
     if (code != JDOB_OK) return code;
   }
-  const bool fast = (uintptr_t)p.x % 16 == 0 && (uintptr_t)p.w % 16 == 0 && p.x_pitch % 16 == 0 &&
-                    p.w_pitch % 16 == 0 && p.in_dim * (X8 ? 1 : 2) % 16 == 0;
-  if (!fast) return launch_tile<T, X8, false, 128, 128, 2, 2>(p, stream);
-  return launch_tile<T, X8, true, 128, 128, 2, 2>(p, stream);
+  if (p.rows <= 16) return launch_stream<T, X8, 1, 8, 4, 4>(p, stream);
+  if (p.rows <= 32) return launch_stream<T, X8, 2, 8, 4, 4>(p, stream);
+  if (p.rows <= STREAM_ROWS) return launch_stream<T, X8, 4, 8, 4, 2>(p, stream);
+  const bool direct = (uintptr_t)p.x % 16 == 0 && (uintptr_t)p.w % 16 == 0 && p.x_pitch % 16 == 0 &&
+                      p.w_pitch % 16 == 0 && p.x_pitch < (1 << 22) && p.w_pitch < (1 << 22) &&
+                      p.in_dim * (X8 ? 1 : 2) % 16 == 0;
+  const bool rw = rowwise(p.rows, p.num_adapters);
+  if (!direct)
+    return rw ? launch_tile<T, X8, false, 64, 64, 2, 2, 2, true>(p, stream)
+              : launch_tile<T, X8, false, 128, 128, 2, 2, 2>(p, stream);
+  if (rw) return launch_tile<T, X8, true, 64, 64, 2, 2, 4, true>(p, stream);
+  // The tile that takes least time by a count of rounds: a slice of 128 bytes takes a round of 256
+  // workgroups 1.87 us with tiles of 256 x 256 (one a compute unit), a round of 512 1.10 us with
+  // 128 x 128 and 0.46 us with 64 x 64 (two a compute unit), measured at 8192 x 4096 x 4096.
+  auto rounds = [&](int side, int at_once) {
+    const int64_t tiles = (int64_t)((p.rows + side - 1) / side) * ((p.out_dim + side - 1) / side);
+    return (double)((tiles + at_once - 1) / at_once);
+  };
+  const double t256 = 1.87 * rounds(256, 256), t128 = 1.10 * rounds(128, 512), t64 = 0.46 * rounds(64, 512);
+  if (t64 <= t128 && t64 <= t256) return launch_tile<T, X8, true, 64, 64, 2, 2, 4>(p, stream);
+  if (t128 <= t256) return launch_tile<T, X8, true, 128, 128, 2, 2, 2>(p, stream);
+  return launch_tile<T, X8, true, 256, 256, 2, 4, 2>(p, stream);
 }
 
 }  // namespace
@@ -459,8 +780,8 @@ extern "C" int64_t jdob_edge_project_workspace(const jdob_edge_project_args *a) 
   using namespace edge;
   if (project_check(a, true) != JDOB_OK) return -1;
   if (a->num_adapters == 0 || a->rows == 0) return 0;
-  const DownPlan d = down_plan(a->rows, a->in_dim, a->max_rank);
-  return (int64_t)d.splits * a->rows * d.rank_pad * (int64_t)sizeof(float);
+  // 32 ranks of a row: binary32, or two 16-bit parts
+  return (int64_t)a->rows * ((a->max_rank + 31) / 32) * 128;
 }
 
 extern "C" int jdob_edge_project(const jdob_edge_project_args *a, void *hip_stream) {
@@ -468,16 +789,10 @@ extern "C" int jdob_edge_project(const jdob_edge_project_args *a, void *hip_stre
   const int code = project_check(a, false);
   if (code != JDOB_OK || a->rows == 0) return code;
   const int size = a->bits8 ? 1 : 2;
-  ProjectParams p = {a->rows, a->in_dim, a->out_dim, (const char *)a->x, (const char *)a->weight,
+  const ProjectParams p = {a->rows, a->in_dim, a->out_dim, (const char *)a->x, (const char *)a->weight,
                      a->x_stride * size, a->weight_stride * size, a->x_scale, a->weight_scale,
                      a->num_adapters, a->max_rank, a->down, a->up, a->gain, a->rank,
-                     a->row_adapter, (float *)a->workspace, 0, 0, 0, a->out, a->out_stride};
-  if (a->num_adapters > 0) {
-    const DownPlan d = down_plan(a->rows, a->in_dim, a->max_rank);
-    p.rank_pad = d.rank_pad;
-    p.splits = d.splits;
-    p.split_len = d.split_len;
-  }
+                     a->row_adapter, a->workspace, (a->max_rank + 31) / 32, a->rows > STREAM_ROWS && !rowwise(a->rows, a->num_adapters), a->out, a->out_stride};
   hipStream_t stream = (hipStream_t)hip_stream;
   if (a->dtype == JDOB_EDGE_BF16)
     return a->bits8 ? project<__bf16, true>(p, stream) : project<__bf16, false>(p, stream);
