@@ -27,7 +27,8 @@ struct AttendParams {
   const int *query_start;
   const int64_t *key_start;
   const int *key_count;
-  int splits, tiles;  // few: splits of the keys, tiles of 32 columns; prompt: tiles of rows
+  int splits, each;   // few: splits of the keys, keys of one
+  int tiles;          // few: tiles of 32 columns of a sequence; prompt: tiles of rows of all
   float *part;        // few: [sequence][key head][tile][split][32 columns][dim + 2]
 };
 
@@ -84,26 +85,37 @@ __device__ inline int value_spot(int r, int c) {
   return r * (DP * 2) + ((c ^ value_swap<DP>(r)) << 4);
 }
 
-// Stages keys first .. first + COUNT - 1 of `count` (zeros behind them, and behind `dim`).
-template <typename T, int DP, bool FAST, bool VALUES, int COUNT, int THREADS>
-__device__ inline void stage(char *dst, const T *base, int64_t stride, int64_t first, int count, int dim) {
+// Stages keys first .. first + COUNT - 1 of `count` by THREADS threads, of which this is number `t` and
+// its wave's first is t0 (zeros behind the last key, and behind `dim` where keys are staged: queries are
+// zero there, but a key's infinity times zero is not).  DIRECT: memory to LDS, without registers between.
+template <typename T, int DP, bool DIRECT, bool VALUES, int COUNT, int THREADS>
+__device__ inline void stage(char *dst, const T *base, int64_t stride, int64_t first, int count, int dim, int t, int t0) {
   constexpr int CH = DP / 8;
+  const T *const tile = base + first * stride;
+  auto each = [&](auto one) {
 #pragma unroll
-  for (int i = 0; i < COUNT * CH / THREADS; ++i) {
-    const int slot = i * THREADS + threadIdx.x, r = slot / CH;
-    const int c = (slot % CH) ^ (VALUES ? value_swap<DP>(r) : r & 7);
-    const bool in = first + r < count && c * 8 < dim;
-    const T *src = base + (first + r) * stride + c * 8;
-    if constexpr (FAST) {
-      const char *from = in ? (const char *)src : (const char *)&attend_zeros;
-      __builtin_amdgcn_global_load_lds(
-          (const __attribute__((address_space(1))) unsigned *)from,
-          (__attribute__((address_space(3))) unsigned *)(dst + (i * THREADS + (threadIdx.x & ~63)) * 16), 16, 0, 0);
-    } else {
-      u32x4 x = {0, 0, 0, 0};
-      if (in) x = __builtin_bit_cast(u32x4, *(const typename Raw<unsigned short, 8>::type *)src);
-      *(u32x4 *)(dst + slot * 16) = x;
+    for (int i = 0; i < COUNT * CH / THREADS; ++i) {
+      const int slot = i * THREADS + t, r = slot / CH;
+      one(i * THREADS, r, (slot % CH) ^ (VALUES ? value_swap<DP>(r) : r & 7));
     }
+  };
+  const unsigned to = lds_address(dst) + t0 * 16;
+  if constexpr (!DIRECT) {
+    each([&](int s0, int r, int c) {
+      u32x4 x = {0, 0, 0, 0};
+      if (first + r < count && c * 8 < dim)
+        x = __builtin_bit_cast(u32x4, *(const typename Raw<unsigned short, 8>::type *)(tile + r * stride + c * 8));
+      *(u32x4 *)(dst + (s0 + t) * 16) = x;
+    });
+  } else if (first + COUNT <= count && dim == DP) {
+    each([&](int s0, int r, int c) {
+      load_to_lds(tile, (unsigned)r * (unsigned)(stride * 2) + c * 16, to + s0 * 16);
+    });
+  } else {
+    each([&](int s0, int r, int c) {
+      const bool in = first + r < count && c * 8 < dim;
+      load_to_lds(in ? (const void *)(tile + r * stride + c * 8) : (const void *)&attend_zeros, to + s0 * 16);
+    });
   }
 }
 
@@ -114,7 +126,10 @@ struct State {
   f32x16 out[DP / 32];      // out[d][e]: column 32 d + 8 (e / 4) + 4 half + e % 4
 };
 
-__device__ inline float other_half(float x) { return __shfl_xor(x, 32); }
+__device__ inline float other_half(float x) {
+  const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(threadIdx.x % WAVE < 32 ? both[1] : both[0]);
+}
 
 // The maximum starts below every score that binary32 arithmetic gives real rows, and above -inf, so
 // that masked scores (-inf) give exp2(-inf) = 0 also where nothing has been seen yet.
@@ -122,35 +137,56 @@ constexpr float LOWEST = -1e30f;
 
 constexpr float GROWTH = 8.0f;  // the maximum may lag behind by this much (p up to 2^8) before out is rescaled
 
-// Scores of 32 rows with KT * 32 staged keys, softmax, and the values' sums.  `limit`: the lane's row
-// sees keys first .. limit; `masked`: whether any key of the tile lies behind some row's limit.
-template <typename T, int DP, int KT>
+// Scores of 32 rows with KT * 32 staged keys, softmax, and the values' sums.  The lane's row sees the
+// tile's keys 0 .. sees; MASKED: some key of the tile lies behind that for some row.
+// LDS is read well before its use, a group at a time: left to itself the compiler reads each operand
+// right before its product and waits for it.
+template <typename T, int DP, int KT, bool MASKED>
 __device__ inline void attend_tile(State<DP> &s, const typename Mma<T>::frag (&q)[DP / 16], const char *keys,
-                                   const char *values, int64_t first, int64_t limit, bool masked, float scale) {
+                                   const char *values, int sees, float scale) {
   typedef typename Mma<T>::frag frag;
-  const int lane = threadIdx.x % WAVE, l32 = lane % 32, half = lane / 32;
+  const int lane = threadIdx.x % WAVE, l32 = lane % 32, half = lane / 32, l16 = lane % 16, g16 = lane / 16;
+  frag kf[KT][DP / 16];
+#pragma unroll
+  for (int t = 0; t < KT; ++t)
+#pragma unroll
+    for (int c = 0; c < DP / 16; ++c) kf[t][c] = *(const frag *)(keys + key_spot<DP>(t * 32 + l32, c * 2 + half));
+  __builtin_amdgcn_sched_barrier(0);
   f32x16 sc[KT];
 #pragma unroll
-  for (int t = 0; t < KT; ++t) {
-    sc[t] = (f32x16){};
+  for (int t = 0; t < KT; ++t) sc[t] = (f32x16){};
 #pragma unroll
-    for (int c = 0; c < DP / 16; ++c)
-      sc[t] = Mma<T>::m32(*(const frag *)(keys + key_spot<DP>(t * 32 + l32, c * 2 + half)), q[c], sc[t]);
-  }
-  float top = LOWEST;
-  if (masked) {
-    const int64_t sees = limit - first;  // within the tile
+  for (int t = 0; t < KT; ++t)
+#pragma unroll
+    for (int c = 0; c < DP / 16; ++c) sc[t] = Mma<T>::m32(kf[t][c], q[c], sc[t]);
+  // columns 32 d .. 32 d + 31 of 16 keys: the transposing reads give a lane four keys of one column
+  struct Pair { s16x4 lo, hi; };
+  auto fetch = [&](Pair (&vf)[DP / 32], int b) {
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d) {
+      const int c = d * 4 + (g16 % 2) * 2 + l16 % 4 / 2, r = b * 16 + half * 4 + l16 / 4;
+      vf[d].lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (__attribute__((address_space(3))) s16x4 *)(values + value_spot<DP>(r, c) + l16 % 2 * 8));
+      vf[d].hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (__attribute__((address_space(3))) s16x4 *)(values + value_spot<DP>(r + 8, c) + l16 % 2 * 8));
+    }
+  };
+  Pair vf[2][DP / 32];
+  fetch(vf[0], 0);
+  __builtin_amdgcn_sched_barrier(0);
+  if constexpr (MASKED) {
 #pragma unroll
     for (int t = 0; t < KT; ++t)
 #pragma unroll
       for (int e = 0; e < 16; ++e)
         sc[t][e] = t * 32 + 8 * (e / 4) + 4 * half + e % 4 <= sees ? sc[t][e] : -INFINITY;
   }
+  float top = LOWEST;
 #pragma unroll
   for (int t = 0; t < KT; ++t)
 #pragma unroll
-    for (int e = 0; e < 16; ++e) top = fmaxf(top, sc[t][e] * scale);
-  top = fmaxf(top, other_half(top));
+    for (int e = 0; e < 16; ++e) top = fmaxf(top, sc[t][e]);
+  top = fmaxf(top, other_half(top)) * scale;
   if (__any(top > s.top + GROWTH)) {
     // a row's own scores decide for it: what other rows of the wave see does not change its roundings
     const float next = top > s.top + GROWTH ? top : s.top;
@@ -170,19 +206,13 @@ __device__ inline void attend_tile(State<DP> &s, const typename Mma<T>::frag (&q
       s.sum += x;
       p[t * 2 + e / 8][e % 8] = (T)x;
     }
-  const int l16 = lane % 16, g16 = lane / 16;
 #pragma unroll
-  for (int b = 0; b < KT * 2; ++b)
+  for (int b = 0; b < KT * 2; ++b) {
+    if (b + 1 < KT * 2) fetch(vf[(b + 1) & 1], b + 1);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int d = 0; d < DP / 32; ++d) {
-      const int c0 = d * 4 + (g16 % 2) * 2 + l16 % 4 / 2, r = b * 16 + half * 4 + l16 / 4;
-      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-          (__attribute__((address_space(3))) s16x4 *)(values + value_spot<DP>(r, c0) + l16 % 2 * 8));
-      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-          (__attribute__((address_space(3))) s16x4 *)(values + value_spot<DP>(r + 8, c0) + l16 % 2 * 8));
-      struct { s16x4 a, b; } both = {lo, hi};
-      s.out[d] = Mma<T>::m32(__builtin_bit_cast(frag, both), p[b], s.out[d]);
-    }
+    for (int d = 0; d < DP / 32; ++d) s.out[d] = Mma<T>::m32(__builtin_bit_cast(frag, vf[b & 1][d]), p[b], s.out[d]);
+  }
 }
 
 // Whether the wave finds an infinity or a NaN among KEYS staged values.
@@ -202,7 +232,7 @@ __device__ inline bool any_non_finite(const char *values) {
 // Replaces the staged values' infinities and NaN by zeros after adding them to the rows that see them
 // (their products with p = 0 of rows that do not would be NaN).  Rare, and slow.
 template <typename T, int DP, int KEYS>
-__device__ inline void take_non_finite(State<DP> &s, char *values, int64_t first, int64_t limit) {
+__device__ inline void take_non_finite(State<DP> &s, char *values, int first, int limit) {
   constexpr unsigned EXP = __is_same(T, __bf16) ? 0x7f80u : 0x7c00u;
   const int half = threadIdx.x % WAVE / 32;
   for (int r = 0; r < KEYS; ++r)
@@ -265,17 +295,18 @@ __device__ inline bool find_tile(const AttendParams &p, int tile, int *u, int *t
   return false;
 }
 
-template <typename T, int DP, bool FAST>
-__global__ __launch_bounds__(PROMPT_WAVES *WAVE) void prompt_kernel(AttendParams p) {
+template <typename T, int DP, bool DIRECT>
+__global__ __launch_bounds__(PROMPT_WAVES *WAVE, 2) void prompt_kernel(AttendParams p) {
   typedef typename Mma<T>::frag frag;
   constexpr int THREADS = PROMPT_WAVES * WAVE, BYTES = PROMPT_KEYS * DP * 2;
   __shared__ __align__(16) char keys[2][BYTES], values[2][BYTES];
-  const int lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE, l32 = lane % 32, half = lane / 32;
-  const int head = blockIdx.x % p.heads, tile = blockIdx.x / p.heads;
+  const int lane = threadIdx.x % WAVE, wave = wave_index(), l32 = lane % 32, half = lane / 32;
+  // Workgroups go to the chip's eight dies in turn: heads that read one key head should share a die's cache.
+  const int kv = blockIdx.x % p.heads % p.kv_heads, head = kv * p.group + blockIdx.x % p.heads / p.kv_heads;
+  const int tile = blockIdx.x / p.heads;
   int u, t;
   Sequence q;
   if (!find_tile(p, tile, &u, &t, &q)) return;
-  const int kv = head / p.group;
   const int row0 = t * PROMPT_ROWS, mine = row0 + wave * 32 + l32;
   const int shift = q.keys - q.rows;  // row i sees keys 0 .. shift + i
   const T *const qrow = (const T *)p.q + (q.row + (mine < q.rows ? mine : 0)) * p.q_stride + head * p.q_head;
@@ -293,26 +324,36 @@ __global__ __launch_bounds__(PROMPT_WAVES *WAVE) void prompt_kernel(AttendParams
 #pragma unroll
   for (int d = 0; d < DP / 32; ++d) s.out[d] = (f32x16){};
   auto load = [&](int b, int kt) {
-    stage<T, DP, FAST, false, PROMPT_KEYS, THREADS>(keys[b], k, p.k_stride, (int64_t)kt * PROMPT_KEYS, q.keys, p.dim);
-    stage<T, DP, FAST, true, PROMPT_KEYS, THREADS>(values[b], v, p.v_stride, (int64_t)kt * PROMPT_KEYS, q.keys, p.dim);
+    stage<T, DP, DIRECT, false, PROMPT_KEYS, THREADS>(keys[b], k, p.k_stride, (int64_t)kt * PROMPT_KEYS, q.keys, p.dim,
+                                                      threadIdx.x, wave * WAVE);
+    stage<T, DP, DIRECT, true, PROMPT_KEYS, THREADS>(values[b], v, p.v_stride, (int64_t)kt * PROMPT_KEYS, q.keys, p.dim,
+                                                     threadIdx.x, wave * WAVE);
   };
   if (tiles > 0) load(0, 0);
-  for (int kt = 0; kt < tiles; ++kt) {
-    const int b = kt & 1;
-    __syncthreads();
-    if (kt + 1 < tiles) load(b ^ 1, kt + 1);
-    const int first = kt * PROMPT_KEYS, limit = shift + mine;
-    // rows of the workgroup that do not see all of the tile
-    const bool edge_tile = first + PROMPT_KEYS - 1 > shift + row0;
-    if (edge_tile) {
-      if (any_non_finite<T, DP, PROMPT_KEYS>(values[b])) {  // the same for all waves
-        take_non_finite<T, DP, PROMPT_KEYS>(s, values[b], first, limit);
-        __syncthreads();
-        clear_non_finite<T, DP, PROMPT_KEYS, THREADS>(values[b]);
-        __syncthreads();
-      }
+  const int limit = shift + mine;
+  // keys that all rows of the workgroup see
+  const int whole = shift + row0 < 0 ? 0 : (shift + row0 + 1) / PROMPT_KEYS;
+  auto advance = [&](int kt) {
+    wait_loads<0>();
+    barrier();
+    if (kt + 1 < tiles) load((kt + 1) & 1, kt + 1);
+  };
+  int kt = 0;
+  for (; kt < whole; ++kt) {
+    advance(kt);
+    attend_tile<T, DP, PROMPT_KEYS / 32, false>(s, qf, keys[kt & 1], values[kt & 1], 0, p.scale);
+  }
+  for (; kt < tiles; ++kt) {
+    advance(kt);
+    const int first = kt * PROMPT_KEYS;
+    char *const v_now = values[kt & 1];
+    if (any_non_finite<T, DP, PROMPT_KEYS>(v_now)) {  // the same for all waves
+      take_non_finite<T, DP, PROMPT_KEYS>(s, v_now, first, limit);
+      __syncthreads();
+      clear_non_finite<T, DP, PROMPT_KEYS, THREADS>(v_now);
+      __syncthreads();
     }
-    attend_tile<T, DP, PROMPT_KEYS / 32>(s, qf, keys[b], values[b], first, limit, edge_tile, p.scale);
+    attend_tile<T, DP, PROMPT_KEYS / 32, true>(s, qf, keys[kt & 1], v_now, limit - first, p.scale);
   }
   const float sum = s.sum + other_half(s.sum), f = sum > 0.0f ? 1.0f / sum : sum;
   if (mine >= q.rows) return;
@@ -330,21 +371,28 @@ __global__ __launch_bounds__(PROMPT_WAVES *WAVE) void prompt_kernel(AttendParams
 
 // ------------------------------------------------------------------ few rows
 
-constexpr int FEW_WAVES = 4, FEW_COLUMNS = 32, FEW_KEYS = 32 * FEW_WAVES;
+constexpr int FEW_WAVES = 2, FEW_COLUMNS = 32, FEW_KEYS = 32;
 
-template <typename T, int DP, bool FAST>
+// A workgroup takes 32 columns (rows times the heads of one key head) and `each` keys of them; its
+// waves take 32 keys in turn, each staged in the wave's own two buffers, so that no wave waits for
+// another before the end.
+template <typename T, int DP, bool DIRECT>
 __global__ __launch_bounds__(FEW_WAVES *WAVE) void few_kernel(AttendParams p) {
   typedef typename Mma<T>::frag frag;
-  constexpr int THREADS = FEW_WAVES * WAVE, BYTES = FEW_KEYS * DP * 2;
-  __shared__ __align__(16) char room[4 * BYTES];
+  constexpr int THREADS = FEW_WAVES * WAVE, BYTES = FEW_KEYS * DP * 2, CORNER = 4 * BYTES;
+  constexpr int LOADS = 2 * BYTES / (WAVE * 16), MIX = FEW_WAVES * 32 * (DP + 4) * 4;
+  __shared__ __align__(16) char room[FEW_WAVES * CORNER > MIX ? FEW_WAVES * CORNER : MIX];
   __shared__ float tops[FEW_WAVES][32], sums[FEW_WAVES][32];
-  const int lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE, l32 = lane % 32, half = lane / 32;
-  const int split = blockIdx.x % p.splits, kv = blockIdx.x / p.splits % p.kv_heads;
-  const int tile = blockIdx.x / p.splits / p.kv_heads % p.tiles, u = blockIdx.x / p.splits / p.kv_heads / p.tiles;
+  const int lane = threadIdx.x % WAVE, wave = wave_index(), l32 = lane % 32, half = lane / 32;
+  const int kv = blockIdx.x % p.kv_heads, split = blockIdx.x / p.kv_heads % p.splits;
+  const int tile = blockIdx.x / p.kv_heads / p.splits % p.tiles, u = blockIdx.x / p.kv_heads / p.splits / p.tiles;
   const Sequence q = sequence(p, u);
   const int rows = q.rows < p.max_queries ? q.rows : p.max_queries;
   const int columns = rows * p.group, column = tile * FEW_COLUMNS + l32;
   if (tile * FEW_COLUMNS >= columns) return;
+  // this split's keys; the last split takes what the others leave (max_keys may be too small)
+  const int from = split * p.each, until = split + 1 < p.splits && from + p.each < q.keys ? from + p.each : q.keys;
+  if (from >= until && split > 0) return;
   const bool have = column < columns;
   const int row = have ? column / p.group : 0, head = kv * p.group + (have ? column % p.group : 0);
   const int shift = q.keys - q.rows, limit = have ? shift + row : -1;
@@ -354,42 +402,48 @@ __global__ __launch_bounds__(FEW_WAVES *WAVE) void few_kernel(AttendParams p) {
   for (int c = 0; c < DP / 16; ++c) qf[c] = query<T>(qrow, c * 2 + half, p.dim, have);
   const T *const k = (const T *)p.k + q.key * p.k_stride + kv * p.k_head;
   const T *const v = (const T *)p.v + q.key * p.v_stride + kv * p.v_head;
-  // this split's tiles of keys
-  const int all = (q.keys + FEW_KEYS - 1) / FEW_KEYS, each = (all + p.splits - 1) / p.splits;
-  const int lo = split * each, hi = lo + each < all ? lo + each : all;
   const int first_limit = shift + tile * FEW_COLUMNS / p.group;  // of the tile's first row
   State<DP> s;
   s.top = LOWEST;
   s.sum = 0.0f;
 #pragma unroll
   for (int d = 0; d < DP / 32; ++d) s.out[d] = (f32x16){};
-  auto load = [&](int b, int kt) {
-    stage<T, DP, FAST, false, FEW_KEYS, THREADS>(room + b * 2 * BYTES, k, p.k_stride, (int64_t)kt * FEW_KEYS, q.keys, p.dim);
-    stage<T, DP, FAST, true, FEW_KEYS, THREADS>(room + (b * 2 + 1) * BYTES, v, p.v_stride, (int64_t)kt * FEW_KEYS, q.keys, p.dim);
+  char *const corner = room + wave * CORNER;
+  auto load = [&](int b, int first) {
+    stage<T, DP, DIRECT, false, FEW_KEYS, WAVE>(corner + b * 2 * BYTES, k, p.k_stride, first, q.keys, p.dim, lane, 0);
+    stage<T, DP, DIRECT, true, FEW_KEYS, WAVE>(corner + (b * 2 + 1) * BYTES, v, p.v_stride, first, q.keys, p.dim, lane, 0);
   };
-  if (lo < hi) load(0, lo);
-  for (int kt = lo; kt < hi; ++kt) {
-    const int b = (kt - lo) & 1;
-    __syncthreads();
-    if (kt + 1 < hi) load(b ^ 1, kt + 1);
-    const int first = kt * FEW_KEYS + wave * 32;
-    const char *const keys = room + b * 2 * BYTES + wave * 32 * DP * 2;
-    char *const values = room + (b * 2 + 1) * BYTES + wave * 32 * DP * 2;
-    const bool masked = first + 31 > first_limit;
-    if (masked && any_non_finite<T, DP, 32>(values)) {
-      take_non_finite<T, DP, 32>(s, values, first, limit);
+  int first = from + wave * FEW_KEYS, b = 0;
+  if (first < until) load(0, first);
+  for (; first < until; first += FEW_WAVES * FEW_KEYS, b ^= 1) {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the other buffer has been read
+    if (first + FEW_WAVES * FEW_KEYS < until) {
+      load(b ^ 1, first + FEW_WAVES * FEW_KEYS);
+      if constexpr (DIRECT) wait_loads<LOADS>();
+    } else if constexpr (DIRECT) {
+      wait_loads<0>();
+    }
+    const char *const keys = corner + b * 2 * BYTES;
+    char *const values = corner + (b * 2 + 1) * BYTES;
+    const bool masked = first + FEW_KEYS - 1 > first_limit || first + FEW_KEYS > until;
+    // keys behind `until` are the next split's (or none)
+    const int last = limit < until - 1 ? limit : until - 1;
+    if (masked && any_non_finite<T, DP, FEW_KEYS>(values)) {
+      take_non_finite<T, DP, FEW_KEYS>(s, values, first, last);
       // the wave's own values: its lanes run together, their LDS accesses in order
       constexpr unsigned EXP = __is_same(T, __bf16) ? 0x7f80u : 0x7c00u;
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-      for (int i = lane; i < 32 * DP; i += WAVE) {
+      for (int i = lane; i < FEW_KEYS * DP; i += WAVE) {
         unsigned short *x = (unsigned short *)values + i;
         if ((*x & EXP) == EXP) *x = 0;
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      __builtin_amdgcn_wave_barrier();
     }
-    attend_tile<T, DP, 1>(s, qf, keys, values, first, limit, masked, p.scale);
+    if (masked) {
+      attend_tile<T, DP, 1, true>(s, qf, keys, values, last - first, p.scale);
+    } else {
+      attend_tile<T, DP, 1, false>(s, qf, keys, values, 0, p.scale);
+    }
   }
   // the waves' results: each column's maximum, then sums and outputs relative to it
   s.sum += other_half(s.sum);
@@ -412,6 +466,7 @@ __global__ __launch_bounds__(FEW_WAVES *WAVE) void few_kernel(AttendParams p) {
       const f32x4 y = {s.out[d][4 * e] * f, s.out[d][4 * e + 1] * f, s.out[d][4 * e + 2] * f, s.out[d][4 * e + 3] * f};
       *(f32x4 *)(mix + (wave * 32 + l32) * (DP + 4) + 32 * d + 8 * e + 4 * half) = y;
     }
+  __syncthreads();  // also: the waves' maxima and sums have been read
   if (wave == 0 && half == 0) sums[0][l32] = sum, tops[0][l32] = top;
   __syncthreads();
   for (int i = threadIdx.x; i < 32 * (DP / 4); i += THREADS) {
@@ -426,33 +481,62 @@ __global__ __launch_bounds__(FEW_WAVES *WAVE) void few_kernel(AttendParams p) {
       T *const out = (T *)p.out + (q.row + col / p.group) * p.out_stride + (kv * p.group + col % p.group) * p.out_head;
       store_f32<T, 4>(out + at, z);
     } else {
-      float *const part = p.part + ((((int64_t)u * p.kv_heads + kv) * p.tiles + tile) * p.splits + split) * 32 * (p.dim + 4) + c * (p.dim + 4);
+      const int64_t group = ((int64_t)u * p.kv_heads + kv) * p.tiles + tile, pitch = p.dim + 4;
+      float *const part = p.part + ((group * p.splits + split) * 32 + c) * pitch;
       *(f32x4 *)(part + at) = y;
       if (at == 0) part[p.dim] = tops[0][c], part[p.dim + 1] = sums[0][c];
     }
   }
 }
 
+constexpr int MAX_SPLITS = 256, JOIN_THREADS = 256;
+
+// A workgroup puts one column's partial results together.
 template <typename T>
-__global__ __launch_bounds__(WAVE) void join_kernel(AttendParams p) {
-  const int c = blockIdx.x % 32, kv = blockIdx.x / 32 % p.kv_heads;
-  const int tile = blockIdx.x / 32 / p.kv_heads % p.tiles, u = blockIdx.x / 32 / p.kv_heads / p.tiles;
+__global__ __launch_bounds__(JOIN_THREADS) void join_kernel(AttendParams p) {
+  __shared__ float weight[MAX_SPLITS], mix[8][128];
+  const int columns_each = p.tiles * FEW_COLUMNS < p.max_queries * p.group ? p.tiles * FEW_COLUMNS : p.max_queries * p.group;
+  const int kv = blockIdx.x % p.kv_heads, col = blockIdx.x / p.kv_heads % columns_each;
+  const int u = blockIdx.x / p.kv_heads / columns_each, tile = col / FEW_COLUMNS;
   const Sequence q = sequence(p, u);
-  const int rows = q.rows < p.max_queries ? q.rows : p.max_queries, col = tile * FEW_COLUMNS + c;
+  const int rows = q.rows < p.max_queries ? q.rows : p.max_queries;
   if (col >= rows * p.group) return;
-  const int64_t pitch = p.dim + 4;
-  const float *const part = p.part + (((int64_t)u * p.kv_heads + kv) * p.tiles + tile) * p.splits * 32 * pitch + c * pitch;
-  float top = LOWEST, sum = 0.0f;
-  for (int i = 0; i < p.splits; ++i) top = fmaxf(top, part[i * 32 * pitch + p.dim]);
-  for (int i = 0; i < p.splits; ++i)
-    sum += part[i * 32 * pitch + p.dim + 1] * __builtin_amdgcn_exp2f(part[i * 32 * pitch + p.dim] - top);
-  const float g = sum > 0.0f ? 1.0f / sum : sum;
-  T *const out = (T *)p.out + (q.row + col / p.group) * p.out_stride + (kv * p.group + col % p.group) * p.out_head;
-  for (int at = threadIdx.x; at < p.dim; at += WAVE) {
-    float y = 0.0f;
-    for (int i = 0; i < p.splits; ++i)
-      y += part[i * 32 * pitch + at] * __builtin_amdgcn_exp2f(part[i * 32 * pitch + p.dim] - top);
-    out[at] = (T)(y * g);
+  const int64_t pitch = p.dim + 4, step = 32 * pitch;
+  const float *const part = p.part + (((int64_t)u * p.kv_heads + kv) * p.tiles + tile) * p.splits * step + col % FEW_COLUMNS * pitch;
+  const int used = q.keys > 0 ? (q.keys + p.each - 1) / p.each : 1, splits = used < p.splits ? used : p.splits;
+  const int t = threadIdx.x, lane = t % WAVE;
+  // every wave for itself: the maximum, the weights, their sum
+  float tops[MAX_SPLITS / WAVE], top = LOWEST, sum = 0.0f;
+#pragma unroll
+  for (int i = 0; i < MAX_SPLITS / WAVE; ++i) {
+    tops[i] = i * WAVE + lane < splits ? part[(i * WAVE + lane) * step + p.dim] : LOWEST;
+    top = fmaxf(top, tops[i]);
+  }
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+#pragma unroll
+  for (int i = 0; i < MAX_SPLITS / WAVE; ++i)
+    if (i * WAVE + lane < splits) {
+      const float w = __builtin_amdgcn_exp2f(tops[i] - top);
+      sum += w * part[(i * WAVE + lane) * step + p.dim + 1];
+      if (t < WAVE) weight[i * WAVE + lane] = w;
+    }
+  sum = wave_sum(sum);
+  __syncthreads();
+  const int at = t % 32 * 4, g = t / 32;
+  f32x4 y = {0, 0, 0, 0};
+  if (at < p.dim) {
+#pragma unroll 4
+    for (int i = g; i < splits; i += 8) y += *(const f32x4 *)(part + i * step + at) * weight[i];
+    *(f32x4 *)(mix[g] + at) = y;
+  }
+  __syncthreads();
+  if (t < p.dim) {
+    float z = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) z += mix[i][t];
+    T *const out = (T *)p.out + (q.row + col / p.group) * p.out_stride + (kv * p.group + col % p.group) * p.out_head;
+    out[t] = (T)(z * (sum > 0.0f ? 1.0f / sum : sum));
   }
 }
 
@@ -481,40 +565,47 @@ int attend_check(const jdob_edge_attend_args *a, bool sizes_only) {
 
 struct FewPlan {
   bool few;
-  int tiles, splits;
+  int tiles, splits, each;
 };
 
 FewPlan few_plan(const jdob_edge_attend_args *a) {
   const int64_t columns = (int64_t)a->max_queries * (a->num_heads / a->num_kv_heads);
   const int64_t tiles = (columns + FEW_COLUMNS - 1) / FEW_COLUMNS;
   const int64_t groups = tiles * a->num_kv_heads * a->num_sequences;
-  if (columns > 128 || groups > (1 << 24)) return {false, 0, 0};
-  int64_t splits = (512 + groups - 1) / groups;
-  const int64_t most = (a->max_keys + 2 * FEW_KEYS - 1) / (2 * FEW_KEYS);
-  splits = splits < most ? splits : most;
-  return {true, (int)tiles, (int)(splits < 1 ? 1 : splits > 128 ? 128 : splits)};
+  if (columns > 128 || groups > (1 << 24)) return {false, 0, 0, 0};
+  // about four workgroups for each place that the chip has for one (two a compute unit), whose
+  // sequences may be of very different lengths, but no fewer than 512 keys each
+  int64_t each = (a->max_keys * groups + 2047) / 2048;
+  each = each < 512 ? 512 : (each + 63) & ~63;
+  int64_t splits = (a->max_keys + each - 1) / each;
+  if (splits > MAX_SPLITS) {
+    each = ((a->max_keys + MAX_SPLITS - 1) / MAX_SPLITS + 63) & ~63;
+    splits = (a->max_keys + each - 1) / each;
+  }
+  return {true, (int)tiles, (int)(splits < 1 ? 1 : splits), (int)each};
 }
 
 template <typename T, int DP>
-int attend(AttendParams p, bool few, bool fast, hipStream_t stream) {
+int attend(AttendParams p, bool few, bool direct, hipStream_t stream) {
   if (few) {
     const int64_t groups = (int64_t)p.sequences * p.kv_heads * p.tiles;
-    if (groups * p.splits > 0x7fffffff || groups * 32 > 0x7fffffff) return JDOB_ERR_UNSUPPORTED;
+    const int64_t columns = (int64_t)p.sequences * p.kv_heads * p.max_queries * p.group;
+    if (groups * p.splits > 0x7fffffff || columns > 0x7fffffff) return JDOB_ERR_UNSUPPORTED;
     const dim3 grid((unsigned)(groups * p.splits));
-    const int code = fast ? launch(few_kernel<T, DP, true>, grid, FEW_WAVES * WAVE, stream, p)
+    const int code = direct ? launch(few_kernel<T, DP, true>, grid, FEW_WAVES * WAVE, stream, p)
                           : launch(few_kernel<T, DP, false>, grid, FEW_WAVES * WAVE, stream, p);
     if (code != JDOB_OK || p.splits == 1) return code;
-    return launch(join_kernel<T>, dim3((unsigned)(groups * 32)), WAVE, stream, p);
+    return launch(join_kernel<T>, dim3((unsigned)columns), JOIN_THREADS, stream, p);
   }
   const int64_t blocks = (int64_t)p.tiles * p.heads;
   if (blocks > 0x7fffffff) return JDOB_ERR_UNSUPPORTED;
-  return fast ? launch(prompt_kernel<T, DP, true>, dim3((unsigned)blocks), PROMPT_WAVES * WAVE, stream, p)
+  return direct ? launch(prompt_kernel<T, DP, true>, dim3((unsigned)blocks), PROMPT_WAVES * WAVE, stream, p)
               : launch(prompt_kernel<T, DP, false>, dim3((unsigned)blocks), PROMPT_WAVES * WAVE, stream, p);
 }
 
 template <typename T>
-int attend(const AttendParams &p, bool few, bool fast, hipStream_t stream) {
-  return p.dim <= 64 ? attend<T, 64>(p, few, fast, stream) : attend<T, 128>(p, few, fast, stream);
+int attend(const AttendParams &p, bool few, bool direct, hipStream_t stream) {
+  return p.dim <= 64 ? attend<T, 64>(p, few, direct, stream) : attend<T, 128>(p, few, direct, stream);
 }
 
 }  // namespace
@@ -539,11 +630,11 @@ extern "C" int jdob_edge_attend(const jdob_edge_attend_args *a, void *hip_stream
                     (const char *)a->q, (const char *)a->k, (const char *)a->v, (char *)a->out,
                     a->q_stride, a->q_head_stride, a->k_stride, a->k_head_stride, a->v_stride, a->v_head_stride,
                     a->out_stride, a->out_head_stride, a->query_start, a->key_start, a->key_count,
-                    f.splits, f.tiles, (float *)a->workspace};
+                    f.splits, f.each, f.tiles, (float *)a->workspace};
   // every sequence's rows fill whole tiles but for one
   if (!f.few) p.tiles = (int)(a->query_rows / PROMPT_ROWS + a->num_sequences);
-  const bool fast = (uintptr_t)a->k % 16 == 0 && (uintptr_t)a->v % 16 == 0 && a->k_stride % 8 == 0 &&
-                    a->k_head_stride % 8 == 0 && a->v_stride % 8 == 0 && a->v_head_stride % 8 == 0;
+  const bool direct = (uintptr_t)a->k % 16 == 0 && (uintptr_t)a->v % 16 == 0 && a->k_stride % 8 == 0 &&
+                    a->k_head_stride % 8 == 0 && a->v_stride % 8 == 0 && a->v_head_stride % 8 == 0 && a->k_stride < (1 << 24) && a->v_stride < (1 << 24);
   hipStream_t stream = (hipStream_t)hip_stream;
-  return a->dtype == JDOB_EDGE_BF16 ? attend<__bf16>(p, f.few, fast, stream) : attend<_Float16>(p, f.few, fast, stream);
+  return a->dtype == JDOB_EDGE_BF16 ? attend<__bf16>(p, f.few, direct, stream) : attend<_Float16>(p, f.few, direct, stream);
 }
