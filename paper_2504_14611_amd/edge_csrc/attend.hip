@@ -69,16 +69,21 @@ __device__ inline Sequence sequence(const AttendParams &p, int u) {
 
 __device__ const u32x4 attend_zeros = {0, 0, 0, 0};
 
-// Staged keys or values: rows of DP elements, 16-byte chunks exchanged within the row.
-// Keys are read 16 bytes a lane, eight rows' equal chunks at once; values 8 bytes a lane, eight rows'
-// equal pairs of chunks at once.
+// Staged keys or values: rows of DP elements, 16-byte chunks exchanged within the row so that what is
+// read at once falls on different LDS banks: of keys eight rows' equal chunks (16 bytes a lane), of
+// values eight rows' equal pairs of chunks (8 bytes a lane).  Rows of 96 elements start on other banks
+// already, and chunks stay within their group of four.
 template <int DP>
-__device__ inline int key_spot(int r, int c) {
-  return r * (DP * 2) + ((c ^ (r & 7)) << 4);
+__device__ inline int key_swap(int r) {
+  return DP == 96 ? r >> 1 & 3 : r & 7;
 }
 template <int DP>
 __device__ inline int value_swap(int r) {
-  return DP >= 128 ? (r & 7) << 1 : (r >> 1 & 3) << 1;
+  return DP == 96 ? (r >> 2 & 1) << 1 : DP == 128 ? (r & 7) << 1 : (r >> 1 & 3) << 1;
+}
+template <int DP>
+__device__ inline int key_spot(int r, int c) {
+  return r * (DP * 2) + ((c ^ key_swap<DP>(r)) << 4);
 }
 template <int DP>
 __device__ inline int value_spot(int r, int c) {
@@ -86,17 +91,19 @@ __device__ inline int value_spot(int r, int c) {
 }
 
 // Stages keys first .. first + COUNT - 1 of `count` by THREADS threads, of which this is number `t` and
-// its wave's first is t0 (zeros behind the last key, and behind `dim` where keys are staged: queries are
-// zero there, but a key's infinity times zero is not).  DIRECT: memory to LDS, without registers between.
+// its wave's first is t0: zeros behind the last key.  Behind `dim`, where queries are zero and the output
+// is not stored, stand zeros, or unless `careful` any of the row's own elements (their product with zero
+// is zero but for infinities and NaN).  DIRECT: memory to LDS, without registers between.
 template <typename T, int DP, bool DIRECT, bool VALUES, int COUNT, int THREADS>
-__device__ inline void stage(char *dst, const T *base, int64_t stride, int64_t first, int count, int dim, int t, int t0) {
+__device__ inline void stage(char *dst, const T *base, int64_t stride, int64_t first, int count, int dim, bool careful,
+                             int t, int t0) {
   constexpr int CH = DP / 8;
   const T *const tile = base + first * stride;
   auto each = [&](auto one) {
 #pragma unroll
     for (int i = 0; i < COUNT * CH / THREADS; ++i) {
       const int slot = i * THREADS + t, r = slot / CH;
-      one(i * THREADS, r, (slot % CH) ^ (VALUES ? value_swap<DP>(r) : r & 7));
+      one(i * THREADS, r, (slot % CH) ^ (VALUES ? value_swap<DP>(r) : key_swap<DP>(r)));
     }
   };
   const unsigned to = lds_address(dst) + t0 * 16;
@@ -107,9 +114,9 @@ __device__ inline void stage(char *dst, const T *base, int64_t stride, int64_t f
         x = __builtin_bit_cast(u32x4, *(const typename Raw<unsigned short, 8>::type *)(tile + r * stride + c * 8));
       *(u32x4 *)(dst + (s0 + t) * 16) = x;
     });
-  } else if (first + COUNT <= count && dim == DP) {
+  } else if (first + COUNT <= count && !careful) {
     each([&](int s0, int r, int c) {
-      load_to_lds(tile, (unsigned)r * (unsigned)(stride * 2) + c * 16, to + s0 * 16);
+      load_to_lds(tile, (unsigned)r * (unsigned)(stride * 2) + (c * 8 < dim ? c * 16 : 0), to + s0 * 16);
     });
   } else {
     each([&](int s0, int r, int c) {
@@ -124,6 +131,16 @@ template <int DP>
 struct State {
   float top, sum;           // the maximum so far (log2 units), this half's sum
   f32x16 out[DP / 32];      // out[d][e]: column 32 d + 8 (e / 4) + 4 half + e % 4
+
+  __device__ void clear();
+  __device__ bool has_nan() const {
+    bool bad = sum != sum;
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) bad |= out[d][e] != out[d][e];
+    return bad;
+  }
 };
 
 __device__ inline float other_half(float x) {
@@ -135,30 +152,49 @@ __device__ inline float other_half(float x) {
 // that masked scores (-inf) give exp2(-inf) = 0 also where nothing has been seen yet.
 constexpr float LOWEST = -1e30f;
 
+template <int DP>
+__device__ void State<DP>::clear() {
+  top = LOWEST;
+  sum = 0.0f;
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d) out[d] = (f32x16){};
+}
+
 constexpr float GROWTH = 8.0f;  // the maximum may lag behind by this much (p up to 2^8) before out is rescaled
 
 // Scores of 32 rows with KT * 32 staged keys, softmax, and the values' sums.  The lane's row sees the
 // tile's keys 0 .. sees; MASKED: some key of the tile lies behind that for some row.
 // LDS is read well before its use, a group at a time: left to itself the compiler reads each operand
 // right before its product and waits for it.
-template <typename T, int DP, int KT, bool MASKED>
+template <typename T, int DP, int KT, bool MASKED, int GROUP = 4>
 __device__ inline void attend_tile(State<DP> &s, const typename Mma<T>::frag (&q)[DP / 16], const char *keys,
                                    const char *values, int sees, float scale) {
   typedef typename Mma<T>::frag frag;
   const int lane = threadIdx.x % WAVE, l32 = lane % 32, half = lane / 32, l16 = lane % 16, g16 = lane / 16;
-  frag kf[KT][DP / 16];
-#pragma unroll
-  for (int t = 0; t < KT; ++t)
-#pragma unroll
-    for (int c = 0; c < DP / 16; ++c) kf[t][c] = *(const frag *)(keys + key_spot<DP>(t * 32 + l32, c * 2 + half));
-  __builtin_amdgcn_sched_barrier(0);
+  constexpr int N = KT * DP / 16, G = N % GROUP == 0 ? GROUP : 3;  // operands in all, and in a group
+  static_assert(N % G == 0, "whole groups");
   f32x16 sc[KT];
 #pragma unroll
   for (int t = 0; t < KT; ++t) sc[t] = (f32x16){};
+  frag kf[2][G];
+  auto fetch_keys = [&](int g) {
 #pragma unroll
-  for (int t = 0; t < KT; ++t)
+    for (int i = 0; i < G; ++i) {
+      const int t = (g * G + i) % KT, c = (g * G + i) / KT;
+      kf[g & 1][i] = *(const frag *)(keys + key_spot<DP>(t * 32 + l32, c * 2 + half));
+    }
+  };
+  fetch_keys(0);
 #pragma unroll
-    for (int c = 0; c < DP / 16; ++c) sc[t] = Mma<T>::m32(kf[t][c], q[c], sc[t]);
+  for (int g = 0; g < N / G; ++g) {
+    if (g + 1 < N / G) fetch_keys(g + 1);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < G; ++i) {
+      const int t = (g * G + i) % KT, c = (g * G + i) / KT;
+      sc[t] = Mma<T>::m32(kf[g & 1][i], q[c], sc[t]);
+    }
+  }
   // columns 32 d .. 32 d + 31 of 16 keys: the transposing reads give a lane four keys of one column
   struct Pair { s16x4 lo, hi; };
   auto fetch = [&](Pair (&vf)[DP / 32], int b) {
@@ -248,9 +284,9 @@ __device__ inline void take_non_finite(State<DP> &s, char *values, int first, in
 }
 
 template <typename T, int DP, int KEYS, int THREADS>
-__device__ inline void clear_non_finite(char *values) {
+__device__ inline void clear_non_finite(char *values, int t) {
   constexpr unsigned EXP = __is_same(T, __bf16) ? 0x7f80u : 0x7c00u;
-  for (int i = threadIdx.x; i < KEYS * DP; i += THREADS) {
+  for (int i = t; i < KEYS * DP; i += THREADS) {
     unsigned short *x = (unsigned short *)values + i;
     if ((*x & EXP) == EXP) *x = 0;
   }
@@ -268,14 +304,19 @@ __device__ inline typename Mma<T>::frag query(const T *row, int c, int dim, bool
 
 constexpr int PROMPT_WAVES = 4, PROMPT_ROWS = 32 * PROMPT_WAVES, PROMPT_KEYS = 64;
 
-// Which sequence and which of its tiles of rows a tile index stands for: the sequences' tiles follow
-// each other.  False behind the last one.
-__device__ inline bool find_tile(const AttendParams &p, int tile, int *u, int *t, Sequence *q) {
+__device__ inline int64_t lane_of(int64_t x, int lane) {
+  return (int64_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32 | (unsigned)__builtin_amdgcn_readlane((int)x, lane);
+}
+
+// Which sequence and which of its tiles a tile index stands for: the sequences' tiles follow each
+// other.  False behind the last one.
+__device__ inline bool find_tile(const AttendParams &p, int tile, int *t, Sequence *q) {
   const int lane = threadIdx.x % WAVE;
   int before = 0;
   for (int u0 = 0; u0 < p.sequences; u0 += WAVE) {
-    int n = 0;
-    if (u0 + lane < p.sequences) n = (sequence(p, u0 + lane).rows + PROMPT_ROWS - 1) / PROMPT_ROWS;
+    Sequence mine = {0, 0, 0, 0};
+    if (u0 + lane < p.sequences) mine = sequence(p, u0 + lane);
+    const int n = (mine.rows + PROMPT_ROWS - 1) / PROMPT_ROWS;
     int upto = n;
 #pragma unroll
     for (int d = 1; d < WAVE; d <<= 1) {
@@ -285,12 +326,12 @@ __device__ inline bool find_tile(const AttendParams &p, int tile, int *u, int *t
     const unsigned long long past = __ballot(before + upto > tile);
     if (past) {
       const int l = __builtin_ctzll(past);
-      *u = u0 + l;
-      *q = sequence(p, *u);
-      *t = __shfl(n, l) - 1 - (tile - before - __shfl(upto - n, l));  // the last rows see most: first
+      *q = {lane_of(mine.row, l), lane_of(mine.key, l), __builtin_amdgcn_readlane(mine.rows, l),
+            __builtin_amdgcn_readlane(mine.keys, l)};
+      *t = before + __builtin_amdgcn_readlane(upto, l) - 1 - tile;  // the last rows see most: first
       return true;
     }
-    before += __shfl(upto, WAVE - 1);
+    before += __builtin_amdgcn_readlane(upto, WAVE - 1);
   }
   return false;
 }
@@ -304,56 +345,71 @@ __global__ __launch_bounds__(PROMPT_WAVES *WAVE, 2) void prompt_kernel(AttendPar
   // Workgroups go to the chip's eight dies in turn: heads that read one key head should share a die's cache.
   const int kv = blockIdx.x % p.heads % p.kv_heads, head = kv * p.group + blockIdx.x % p.heads / p.kv_heads;
   const int tile = blockIdx.x / p.heads;
-  int u, t;
+  int t;
   Sequence q;
-  if (!find_tile(p, tile, &u, &t, &q)) return;
-  const int row0 = t * PROMPT_ROWS, mine = row0 + wave * 32 + l32;
+  if (!find_tile(p, tile, &t, &q)) return;
+  const int row0 = t * PROMPT_ROWS, wave_row = row0 + wave * 32, mine = wave_row + l32;
   const int shift = q.keys - q.rows;  // row i sees keys 0 .. shift + i
-  const T *const qrow = (const T *)p.q + (q.row + (mine < q.rows ? mine : 0)) * p.q_stride + head * p.q_head;
-  frag qf[DP / 16];
-#pragma unroll
-  for (int c = 0; c < DP / 16; ++c) qf[c] = query<T>(qrow, c * 2 + half, p.dim, mine < q.rows);
   const T *const k = (const T *)p.k + q.key * p.k_stride + kv * p.k_head;
   const T *const v = (const T *)p.v + q.key * p.v_stride + kv * p.v_head;
   const int last_row = (row0 + PROMPT_ROWS < q.rows ? row0 + PROMPT_ROWS : q.rows) - 1;
   const int seen = shift + last_row + 1;  // keys that some row of the workgroup sees
   const int tiles = seen > 0 ? (seen + PROMPT_KEYS - 1) / PROMPT_KEYS : 0;
-  State<DP> s;
-  s.top = LOWEST;
-  s.sum = 0.0f;
-#pragma unroll
-  for (int d = 0; d < DP / 32; ++d) s.out[d] = (f32x16){};
-  auto load = [&](int b, int kt) {
-    stage<T, DP, DIRECT, false, PROMPT_KEYS, THREADS>(keys[b], k, p.k_stride, (int64_t)kt * PROMPT_KEYS, q.keys, p.dim,
-                                                      threadIdx.x, wave * WAVE);
-    stage<T, DP, DIRECT, true, PROMPT_KEYS, THREADS>(values[b], v, p.v_stride, (int64_t)kt * PROMPT_KEYS, q.keys, p.dim,
-                                                     threadIdx.x, wave * WAVE);
-  };
-  if (tiles > 0) load(0, 0);
-  const int limit = shift + mine;
-  // keys that all rows of the workgroup see
+  // tiles that all rows of the workgroup see
   const int whole = shift + row0 < 0 ? 0 : (shift + row0 + 1) / PROMPT_KEYS;
+  // the last key that the wave's last row sees (-1: it has no rows, or they see nothing)
+  const int wave_last = wave_row + 31 < last_row ? wave_row + 31 : last_row;
+  const int wave_any = wave_row <= last_row ? shift + wave_last : -1;
+  const int limit = shift + mine;
+  bool careful = false;
+  auto load = [&](int kt) {
+    const int b = kt & 1;
+    stage<T, DP, DIRECT, false, PROMPT_KEYS, THREADS>(keys[b], k, p.k_stride, (int64_t)kt * PROMPT_KEYS, q.keys, p.dim,
+                                                      careful, threadIdx.x, wave * WAVE);
+    stage<T, DP, DIRECT, true, PROMPT_KEYS, THREADS>(values[b], v, p.v_stride, (int64_t)kt * PROMPT_KEYS, q.keys, p.dim,
+                                                     careful, threadIdx.x, wave * WAVE);
+  };
   auto advance = [&](int kt) {
     wait_loads<0>();
     barrier();
-    if (kt + 1 < tiles) load((kt + 1) & 1, kt + 1);
+    if (kt + 1 < tiles) load(kt + 1);
   };
+  if (tiles > 0) load(0);
+  const T *const qrow = (const T *)p.q + (q.row + (mine < q.rows ? mine : 0)) * p.q_stride + head * p.q_head;
+  frag qf[DP / 16];
+#pragma unroll
+  for (int c = 0; c < DP / 16; ++c) qf[c] = query<T>(qrow, c * 2 + half, p.dim, mine < q.rows);
+  State<DP> s;
+  s.clear();
   int kt = 0;
   for (; kt < whole; ++kt) {
     advance(kt);
-    attend_tile<T, DP, PROMPT_KEYS / 32, false>(s, qf, keys[kt & 1], values[kt & 1], 0, p.scale);
+    if (wave_row <= last_row)
+      attend_tile<T, DP, PROMPT_KEYS / 32, false>(s, qf, keys[kt & 1], values[kt & 1], 0, p.scale);
   }
   for (; kt < tiles; ++kt) {
     advance(kt);
     const int first = kt * PROMPT_KEYS;
-    char *const v_now = values[kt & 1];
-    if (any_non_finite<T, DP, PROMPT_KEYS>(v_now)) {  // the same for all waves
-      take_non_finite<T, DP, PROMPT_KEYS>(s, v_now, first, limit);
-      __syncthreads();
-      clear_non_finite<T, DP, PROMPT_KEYS, THREADS>(v_now);
-      __syncthreads();
+    if (first > wave_any) continue;  // the wave's rows see nothing of this tile
+    attend_tile<T, DP, PROMPT_KEYS / 32, true>(s, qf, keys[kt & 1], values[kt & 1], limit - first, p.scale);
+  }
+  // A NaN may come from a value that its row does not see (p = 0 times an infinity): once more, with care.
+  if (__syncthreads_or(mine < q.rows && s.has_nan())) {
+    careful = true;
+    s.clear();
+    if (tiles > 0) load(0);
+    for (kt = 0; kt < tiles; ++kt) {
+      advance(kt);
+      const int first = kt * PROMPT_KEYS;
+      char *const v_now = values[kt & 1];
+      if (any_non_finite<T, DP, PROMPT_KEYS>(v_now)) {  // the same for all waves
+        take_non_finite<T, DP, PROMPT_KEYS>(s, v_now, first, limit);
+        __syncthreads();
+        clear_non_finite<T, DP, PROMPT_KEYS, THREADS>(v_now, threadIdx.x);
+        __syncthreads();
+      }
+      attend_tile<T, DP, PROMPT_KEYS / 32, true>(s, qf, keys[kt & 1], v_now, limit - first, p.scale);
     }
-    attend_tile<T, DP, PROMPT_KEYS / 32, true>(s, qf, keys[kt & 1], v_now, limit - first, p.scale);
   }
   const float sum = s.sum + other_half(s.sum), f = sum > 0.0f ? 1.0f / sum : sum;
   if (mine >= q.rows) return;
@@ -404,47 +460,45 @@ __global__ __launch_bounds__(FEW_WAVES *WAVE) void few_kernel(AttendParams p) {
   const T *const v = (const T *)p.v + q.key * p.v_stride + kv * p.v_head;
   const int first_limit = shift + tile * FEW_COLUMNS / p.group;  // of the tile's first row
   State<DP> s;
-  s.top = LOWEST;
-  s.sum = 0.0f;
-#pragma unroll
-  for (int d = 0; d < DP / 32; ++d) s.out[d] = (f32x16){};
   char *const corner = room + wave * CORNER;
-  auto load = [&](int b, int first) {
-    stage<T, DP, DIRECT, false, FEW_KEYS, WAVE>(corner + b * 2 * BYTES, k, p.k_stride, first, q.keys, p.dim, lane, 0);
-    stage<T, DP, DIRECT, true, FEW_KEYS, WAVE>(corner + (b * 2 + 1) * BYTES, v, p.v_stride, first, q.keys, p.dim, lane, 0);
-  };
-  int first = from + wave * FEW_KEYS, b = 0;
-  if (first < until) load(0, first);
-  for (; first < until; first += FEW_WAVES * FEW_KEYS, b ^= 1) {
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the other buffer has been read
-    if (first + FEW_WAVES * FEW_KEYS < until) {
-      load(b ^ 1, first + FEW_WAVES * FEW_KEYS);
-      if constexpr (DIRECT) wait_loads<LOADS>();
-    } else if constexpr (DIRECT) {
-      wait_loads<0>();
-    }
-    const char *const keys = corner + b * 2 * BYTES;
-    char *const values = corner + (b * 2 + 1) * BYTES;
-    const bool masked = first + FEW_KEYS - 1 > first_limit || first + FEW_KEYS > until;
-    // keys behind `until` are the next split's (or none)
-    const int last = limit < until - 1 ? limit : until - 1;
-    if (masked && any_non_finite<T, DP, FEW_KEYS>(values)) {
-      take_non_finite<T, DP, FEW_KEYS>(s, values, first, last);
-      // the wave's own values: its lanes run together, their LDS accesses in order
-      constexpr unsigned EXP = __is_same(T, __bf16) ? 0x7f80u : 0x7c00u;
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      for (int i = lane; i < FEW_KEYS * DP; i += WAVE) {
-        unsigned short *x = (unsigned short *)values + i;
-        if ((*x & EXP) == EXP) *x = 0;
+  auto keys_of = [&](bool careful) {
+    s.clear();
+    auto load = [&](int b, int first) {
+      stage<T, DP, DIRECT, false, FEW_KEYS, WAVE>(corner + b * 2 * BYTES, k, p.k_stride, first, q.keys, p.dim, careful, lane, 0);
+      stage<T, DP, DIRECT, true, FEW_KEYS, WAVE>(corner + (b * 2 + 1) * BYTES, v, p.v_stride, first, q.keys, p.dim, careful,
+                                                 lane, 0);
+    };
+    int first = from + wave * FEW_KEYS, b = 0;
+    if (first < until) load(0, first);
+    for (; first < until; first += FEW_WAVES * FEW_KEYS, b ^= 1) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the other buffer has been read
+      if (first + FEW_WAVES * FEW_KEYS < until) {
+        load(b ^ 1, first + FEW_WAVES * FEW_KEYS);
+        if constexpr (DIRECT) wait_loads<LOADS>();
+      } else if constexpr (DIRECT) {
+        wait_loads<0>();
       }
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    }
-    if (masked) {
+      const char *const keys = corner + b * 2 * BYTES;
+      char *const values = corner + (b * 2 + 1) * BYTES;
+      // keys behind `until` are the next split's (or none)
+      const int last = limit < until - 1 ? limit : until - 1;
+      if (first + FEW_KEYS - 1 <= first_limit && first + FEW_KEYS <= until && !careful) {
+        attend_tile<T, DP, 1, false>(s, qf, keys, values, 0, p.scale);
+        continue;
+      }
+      if (careful && any_non_finite<T, DP, FEW_KEYS>(values)) {
+        take_non_finite<T, DP, FEW_KEYS>(s, values, first, last);
+        // the wave's own values: its lanes run together, their LDS accesses in order
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        clear_non_finite<T, DP, FEW_KEYS, WAVE>(values, lane);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      }
       attend_tile<T, DP, 1, true>(s, qf, keys, values, last - first, p.scale);
-    } else {
-      attend_tile<T, DP, 1, false>(s, qf, keys, values, 0, p.scale);
     }
-  }
+  };
+  keys_of(false);
+  // A NaN may come from a value that its row does not see (p = 0 times an infinity): once more, with care.
+  if (__any(have && s.has_nan())) keys_of(true);
   // the waves' results: each column's maximum, then sums and outputs relative to it
   s.sum += other_half(s.sum);
   if (half == 0) {
@@ -495,7 +549,7 @@ constexpr int MAX_SPLITS = 256, JOIN_THREADS = 256;
 template <typename T>
 __global__ __launch_bounds__(JOIN_THREADS) void join_kernel(AttendParams p) {
   __shared__ float weight[MAX_SPLITS], mix[8][128];
-  const int columns_each = p.tiles * FEW_COLUMNS < p.max_queries * p.group ? p.tiles * FEW_COLUMNS : p.max_queries * p.group;
+  const int columns_each = p.max_queries * p.group;
   const int kv = blockIdx.x % p.kv_heads, col = blockIdx.x / p.kv_heads % columns_each;
   const int u = blockIdx.x / p.kv_heads / columns_each, tile = col / FEW_COLUMNS;
   const Sequence q = sequence(p, u);
@@ -572,7 +626,11 @@ FewPlan few_plan(const jdob_edge_attend_args *a) {
   const int64_t columns = (int64_t)a->max_queries * (a->num_heads / a->num_kv_heads);
   const int64_t tiles = (columns + FEW_COLUMNS - 1) / FEW_COLUMNS;
   const int64_t groups = tiles * a->num_kv_heads * a->num_sequences;
-  if (columns > 128 || groups > (1 << 24)) return {false, 0, 0, 0};
+  // Many rows take prompt_kernel, whose workgroups stage each key once for 128 rows of one head, unless
+  // that gives the chip too few workgroups for the keys there are.
+  const int64_t prompts = (a->query_rows / PROMPT_ROWS + a->num_sequences) * a->num_heads;
+  const bool long_keys = prompts < 256 && a->max_keys >= 1024 && columns <= 4096;
+  if ((columns > 128 && !long_keys) || groups > (1 << 24)) return {false, 0, 0, 0};
   // about four workgroups for each place that the chip has for one (two a compute unit), whose
   // sequences may be of very different lengths, but no fewer than 512 keys each
   int64_t each = (a->max_keys * groups + 2047) / 2048;
@@ -605,7 +663,8 @@ int attend(AttendParams p, bool few, bool direct, hipStream_t stream) {
 
 template <typename T>
 int attend(const AttendParams &p, bool few, bool direct, hipStream_t stream) {
-  return p.dim <= 64 ? attend<T, 64>(p, few, direct, stream) : attend<T, 128>(p, few, direct, stream);
+  if (p.dim <= 64) return attend<T, 64>(p, few, direct, stream);
+  return p.dim <= 96 ? attend<T, 96>(p, few, direct, stream) : attend<T, 128>(p, few, direct, stream);
 }
 
 }  // namespace
