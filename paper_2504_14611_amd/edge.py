@@ -12,11 +12,21 @@ current stream of the tensors' device).  Refused arguments raise jdob.JdobError 
 
 from __future__ import annotations
 
-import contextlib
 import ctypes as C
 from typing import Dict, Optional
 
+import torch
+
 from . import jdob
+
+try:  # a call's overhead on the host counts with few rows: these take a tenth of the public calls' time
+    from torch._C import _cuda_getCurrentRawStream as _raw_stream, _cuda_getDevice as _current_device
+except ImportError:
+    def _raw_stream(index):
+        return torch.cuda.current_stream(index).cuda_stream
+
+    def _current_device():
+        return torch.cuda.current_device()
 
 EDGE_BF16, EDGE_F16, EDGE_F32 = 0, 1, 2
 MAX_NORM_DIM, MAX_RANK, MAX_HEAD_DIM, MAX_SEQUENCES = 16384, 256, 128, 65535
@@ -68,59 +78,52 @@ def load():
     return _lib
 
 
+_CODES = {torch.bfloat16: EDGE_BF16, torch.float16: EDGE_F16, torch.float32: EDGE_F32}
+
+
 def _refuse(where: str, why: str, code: int = jdob.JDOB_ERR_INVALID_ARG):
     raise jdob.JdobError(code, f"{where}: {why}")
 
 
 def _dtype(t, where: str) -> int:
-    import torch
-    code = {torch.bfloat16: EDGE_BF16, torch.float16: EDGE_F16, torch.float32: EDGE_F32}.get(t)
+    code = _CODES.get(t)
     if code is None:
         _refuse(where, f"type {t}", jdob.JDOB_ERR_UNSUPPORTED)
     return code
 
 
-def _need(ok: bool, where: str, why: str):
-    if not ok:
-        _refuse(where, why)
-
-
 def _array(t, where: str, name: str, shape, dtype, device):
     """A tensor whose shape, type and device the kernels take as given, with its innermost dimension contiguous."""
-    if t.dtype != dtype or t.device != device or tuple(t.shape) != tuple(shape):
+    if t.dtype is not dtype or t.shape != shape or t.device != device:
         _refuse(where, f"{name} is {tuple(t.shape)} {t.dtype} on {t.device}, "
                        f"expected {tuple(shape)} {dtype} on {device}")
-    if t.dim() and t.shape[-1] > 1 and t.stride(-1) != 1:
+    if t.stride(-1) != 1 and t.shape[-1] > 1:
         _refuse(where, f"{name}'s last dimension is not contiguous")
+    return t.data_ptr()
 
 
 def _dense(t, where: str, name: str, shape, dtype, device):
-    _array(t, where, name, shape, dtype, device)
-    _need(t.is_contiguous(), where, f"{name} is not contiguous")
-
-
-def _on(device, stream):
-    """The device's allocations and launches go to `stream` (a raw handle), or to torch's current stream."""
-    import torch
-    if device.type != "cuda":
-        return contextlib.nullcontext()
-    if stream is not None:
-        return torch.cuda.stream(torch.cuda.ExternalStream(stream, device=device))
-    if device.index is not None and device.index != torch.cuda.current_device():
-        return torch.cuda.device(device)
-    return contextlib.nullcontext()
-
-
-def _handle(device, stream) -> Optional[int]:
-    import torch
-    if stream is not None or device.type != "cuda":
-        return stream
-    return torch.cuda.current_stream(device).cuda_stream
+    if t.dtype is not dtype or t.shape != shape or t.device != device or not t.is_contiguous():
+        _array(t, where, name, shape, dtype, device)
+        _refuse(where, f"{name} is not contiguous")
+    return t.data_ptr()
 
 
 def _row_stride(t, width: int) -> int:
     # a single row's stride is never used, whatever torch says it is
-    return t.stride(0) if t.shape[0] > 1 else max(width, t.stride(0))
+    stride = t.stride(0)
+    return stride if stride > width or t.shape[0] > 1 else width
+
+
+def _enter(device, stream):
+    """The raw stream of a call on `device`, and the context (or None) in which its outputs are allocated and its
+    kernels launched: `stream`'s, or the device's where it is not torch's current one."""
+    if device.type != "cuda":
+        return stream, None
+    if stream is not None:
+        return stream, torch.cuda.stream(torch.cuda.ExternalStream(stream, device=device))
+    index = device.index
+    return _raw_stream(index), None if index == _current_device() else torch.cuda.device(index)
 
 
 def norm(x, weight, eps: float = 1e-6, residual=None, bits8: bool = False, out16: Optional[bool] = None,
@@ -128,39 +131,60 @@ def norm(x, weight, eps: float = 1e-6, residual=None, bits8: bool = False, out16
     """jdob_edge_norm of x [rows, dim]: a dict with `sum` (x + residual, None without a residual), `out` (the
     normalised rows in x's type; with bits8 only where out16 is true) and, with bits8, `q` and `scale`.
     `into` holds the caller's own buffers for any of them; `sum` may be x or residual itself."""
-    import torch
     where = "jdob_edge_norm"
-    _need(x.dim() == 2, where, "x has rows and columns")
-    rows, dim = x.shape
-    code, dev = _dtype(x.dtype, where), x.device
-    _array(x, where, "x", (rows, dim), x.dtype, dev)
-    _dense(weight, where, "weight", (dim,), x.dtype, dev)
+    if x.dim() != 2:
+        _refuse(where, "x has rows and columns")
+    shape, dtype, dev = x.shape, x.dtype, x.device
+    rows, dim = shape
+    if out16 is None:
+        out16 = not bits8
+    if not (bits8 or out16):
+        _refuse(where, "neither output is asked for")
+    a = NormArgs(rows, dim, _dtype(dtype, where), eps, _array(x, where, "x", shape, dtype, dev), _row_stride(x, dim))
+    a.weight = _dense(weight, where, "weight", (dim,), dtype, dev)
     if residual is not None:
-        _array(residual, where, "residual", (rows, dim), x.dtype, dev)
-    want16 = (not bits8) if out16 is None else out16
-    _need(bits8 or want16, where, "neither output is asked for")
-    r = dict.fromkeys(("sum", "out", "q", "scale"))
-    into = into or {}
-    with _on(dev, stream):
-        for key, wanted, shape, dtype in (("sum", residual is not None, (rows, dim), x.dtype),
-                                          ("out", want16, (rows, dim), x.dtype), ("q", bits8, (rows, dim), torch.int8),
-                                          ("scale", bits8, (rows,), torch.float32)):
-            if not wanted:
-                continue
-            t = into.get(key)
-            if t is None:
-                t = torch.empty(shape, dtype=dtype, device=dev)
-            else:
-                (_dense if key == "scale" else _array)(t, where, key, shape, dtype, dev)
-            r[key] = t
-        a = NormArgs(rows, dim, code, eps, x.data_ptr(), _row_stride(x, dim) if rows else dim,
-                     *((residual.data_ptr(), _row_stride(residual, dim)) if residual is not None and rows else (None, 0)),
-                     weight.data_ptr(), *[y for key in ("sum", "out", "q") for y in
-                                          ((r[key].data_ptr(), _row_stride(r[key], dim))
-                                           if r[key] is not None and rows else (None, 0))],
-                     r["scale"].data_ptr() if bits8 else None)
-        jdob._check(load().jdob_edge_norm(C.byref(a), _handle(dev, stream)), where)
-    return r
+        a.residual = _array(residual, where, "residual", shape, dtype, dev)
+        a.residual_stride = _row_stride(residual, dim)
+    handle, context = _enter(dev, stream)
+    if context is not None:
+        with context:
+            return _norm(a, where, x, bits8, out16, into, handle)
+    return _norm(a, where, x, bits8, out16, into, handle)
+
+
+def _norm(a, where, x, bits8, out16, into, handle):
+    shape, dtype, dev, dim = x.shape, x.dtype, x.device, a.dim
+    total = out = q = scale = None
+    if a.residual_stride:
+        total = into and into.get("sum")
+        if total is None:
+            total = torch.empty_like(x, memory_format=torch.contiguous_format)
+            a.sum, a.sum_stride = total.data_ptr(), dim
+        else:
+            a.sum, a.sum_stride = _array(total, where, "sum", shape, dtype, dev), _row_stride(total, dim)
+    if out16:
+        out = into and into.get("out")
+        if out is None:
+            out = torch.empty_like(x, memory_format=torch.contiguous_format)
+            a.out, a.out_stride = out.data_ptr(), dim
+        else:
+            a.out, a.out_stride = _array(out, where, "out", shape, dtype, dev), _row_stride(out, dim)
+    if bits8:
+        q, scale = (into.get("q"), into.get("scale")) if into else (None, None)
+        if q is None:
+            q = torch.empty_like(x, dtype=torch.int8, memory_format=torch.contiguous_format)
+            a.q, a.q_stride = q.data_ptr(), dim
+        else:
+            a.q, a.q_stride = _array(q, where, "q", shape, torch.int8, dev), _row_stride(q, dim)
+        if scale is None:
+            scale = torch.empty(shape[:1], dtype=torch.float32, device=dev)
+            a.scale = scale.data_ptr()
+        else:
+            a.scale = _dense(scale, where, "scale", shape[:1], torch.float32, dev)
+    code = (_lib or load()).jdob_edge_norm(C.byref(a), handle)
+    if code:
+        jdob._check(code, where)
+    return {"sum": total, "out": out, "q": q, "scale": scale}
 
 
 def project(x, weight, x_scale=None, weight_scale=None, adapters: Optional[dict] = None, row_adapter=None,
@@ -170,61 +194,74 @@ def project(x, weight, x_scale=None, weight_scale=None, adapters: Optional[dict]
     x and weight are of the output's type, or int8 with x_scale [rows] and weight_scale [out] (dtype then names
     the output's type, default bfloat16).  adapters: {"down" [n, r, in], "up" [n, out, r], "gain" [n], optionally
     "rank" [n] int32} with row_adapter [rows] int32 (outside [0, n): none).  Returns out [rows, out]."""
-    import torch
     where = "jdob_edge_project"
-    _need(x.dim() == 2 and weight.dim() == 2, where, "x and weight have rows and columns")
-    (rows, i), o, dev = x.shape, weight.shape[0], x.device
-    bits8 = x.dtype == torch.int8
+    if x.dim() != 2 or weight.dim() != 2:
+        _refuse(where, "x and weight have rows and columns")
+    rows, i = x.shape
+    o, dev = weight.shape[0], x.device
+    kind = x.dtype
+    bits8 = kind is torch.int8
     if dtype is None:
-        dtype = torch.bfloat16 if bits8 else x.dtype
-    code = _dtype(dtype, where)
-    _array(x, where, "x", (rows, i), torch.int8 if bits8 else dtype, dev)
-    _array(weight, where, "weight", (o, i), x.dtype, dev)
-    _need((x_scale is not None and weight_scale is not None) == bits8 and
-          (x_scale is None) == (weight_scale is None), where, "scales belong to 8-bit x and weight")
+        dtype = torch.bfloat16 if bits8 else kind
+    elif not bits8 and kind is not dtype:
+        _refuse(where, f"x is {kind}, expected {dtype} or int8")
+    a = ProjectArgs(rows, i, o, _dtype(dtype, where), bits8, _array(x, where, "x", x.shape, kind, dev),
+                    _row_stride(x, i), None, _array(weight, where, "weight", (o, i), kind, dev), _row_stride(weight, i))
     if bits8:
-        _dense(x_scale, where, "x_scale", (rows,), torch.float32, dev)
-        _dense(weight_scale, where, "weight_scale", (o,), torch.float32, dev)
-    _need((adapters is None) == (row_adapter is None), where, "adapters and row_adapter go together")
-    a = ProjectArgs(rows=rows, in_dim=i, out_dim=o, dtype=code, bits8=bits8, x=x.data_ptr(), weight=weight.data_ptr(),
-                    x_stride=_row_stride(x, i) if rows else i, weight_stride=_row_stride(weight, i) if o else i)
-    if bits8:
-        a.x_scale, a.weight_scale = x_scale.data_ptr(), weight_scale.data_ptr()
+        if x_scale is None or weight_scale is None:
+            _refuse(where, "8-bit x and weight have scales")
+        a.x_scale = _dense(x_scale, where, "x_scale", (rows,), torch.float32, dev)
+        a.weight_scale = _dense(weight_scale, where, "weight_scale", (o,), torch.float32, dev)
+    elif x_scale is not None or weight_scale is not None:
+        _refuse(where, "scales belong to 8-bit x and weight")
+    if (adapters is None) != (row_adapter is None):
+        _refuse(where, "adapters and row_adapter go together")
     if adapters is not None:
-        down, up, gain, rank = adapters["down"], adapters["up"], adapters["gain"], adapters.get("rank")
-        _need(down.dim() == 3, where, "down is [adapters, rank, in]")
+        down, rank = adapters["down"], adapters.get("rank")
+        if down.dim() != 3:
+            _refuse(where, "down is [adapters, rank, in]")
         n, most = down.shape[:2]
-        _dense(down, where, "down", (n, most, i), dtype, dev)
-        _dense(up, where, "up", (n, o, most), dtype, dev)
-        _dense(gain, where, "gain", (n,), torch.float32, dev)
-        _dense(row_adapter, where, "row_adapter", (rows,), torch.int32, dev)
-        a.num_adapters, a.max_rank, a.row_adapter = n, most, row_adapter.data_ptr()
-        a.down, a.up, a.gain = down.data_ptr(), up.data_ptr(), gain.data_ptr()
+        a.num_adapters, a.max_rank = n, most
+        a.down = _dense(down, where, "down", (n, most, i), dtype, dev)
+        a.up = _dense(adapters["up"], where, "up", (n, o, most), dtype, dev)
+        a.gain = _dense(adapters["gain"], where, "gain", (n,), torch.float32, dev)
+        a.row_adapter = _dense(row_adapter, where, "row_adapter", (rows,), torch.int32, dev)
         if rank is not None:
-            _dense(rank, where, "rank", (n,), torch.int32, dev)
-            a.rank = rank.data_ptr()
-    lib = load()
-    with _on(dev, stream):
-        if out is None:
-            out = torch.empty((rows, o), dtype=dtype, device=dev)
-        else:
-            _array(out, where, "out", (rows, o), dtype, dev)
-        a.out, a.out_stride = out.data_ptr(), _row_stride(out, o) if rows else o
-        if adapters is not None:
-            workspace = _workspace(workspace, lib.jdob_edge_project_workspace(C.byref(a)), dev, where)
-            if workspace is not None:
-                a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-        jdob._check(lib.jdob_edge_project(C.byref(a), _handle(dev, stream)), where)
+            a.rank = _dense(rank, where, "rank", (n,), torch.int32, dev)
+    handle, context = _enter(dev, stream)
+    if context is not None:
+        with context:
+            return _project(a, where, dtype, dev, out, workspace, handle)
+    return _project(a, where, dtype, dev, out, workspace, handle)
+
+
+def _project(a, where, dtype, dev, out, workspace, handle):
+    shape = (a.rows, a.out_dim)
+    if out is None:
+        out = torch.empty(shape, dtype=dtype, device=dev)
+        a.out, a.out_stride = out.data_ptr(), a.out_dim
+    else:
+        a.out, a.out_stride = _array(out, where, "out", shape, dtype, dev), _row_stride(out, a.out_dim)
+    lib = _lib or load()
+    if a.num_adapters:
+        workspace = _workspace(a, workspace, lib.jdob_edge_project_workspace, dev, where)
+    code = lib.jdob_edge_project(C.byref(a), handle)
+    if code:
+        jdob._check(code, where)
     return out
 
 
-def _workspace(given, size: int, device, where: str):
-    """The caller's workspace, or one of `size` bytes; None where none is needed (or the call will refuse)."""
-    import torch
-    if given is not None:
-        _need(given.is_contiguous() and given.device == device, where, "workspace is contiguous, on the tensors' device")
-        return given
-    return torch.empty(size, dtype=torch.uint8, device=device) if size > 0 else None
+def _workspace(a, given, size, device, where: str):
+    """Sets the caller's workspace, or a new one; none where none is needed (or the call will refuse)."""
+    if given is None:
+        given = size(C.byref(a))
+        if given <= 0:
+            return None
+        given = torch.empty(given, dtype=torch.uint8, device=device)
+    elif not given.is_contiguous() or given.device != device:
+        _refuse(where, "workspace is contiguous, on the tensors' device")
+    a.workspace, a.workspace_bytes = given.data_ptr(), given.numel() * given.element_size()
+    return given
 
 
 def attend(q, k, v, query_start, key_start, key_count, scale: Optional[float] = None,
@@ -234,31 +271,38 @@ def attend(q, k, v, query_start, key_start, key_count, scale: Optional[float] = 
     Sequence u's rows query_start[u] .. query_start[u+1] stand at the end of its key_count[u] keys, which start at
     row key_start[u].  scale defaults to dim ** -0.5; max_queries and max_keys are at least the largest sequence's
     (default: all rows).  Returns out [rows, heads, dim]."""
-    import torch
     where = "jdob_edge_attend"
-    _need(q.dim() == 3 and k.dim() == 3, where, "q, k and v have rows, heads and columns")
-    (rows, h, d), (key_rows, g), dev = q.shape, k.shape[:2], q.device
-    code, n = _dtype(q.dtype, where), key_count.shape[0]
-    _array(q, where, "q", (rows, h, d), q.dtype, dev)
-    _array(k, where, "k", (key_rows, g, d), q.dtype, dev)
-    _array(v, where, "v", (key_rows, g, d), q.dtype, dev)
-    _dense(query_start, where, "query_start", (n + 1,), torch.int32, dev)
-    _dense(key_start, where, "key_start", (n,), torch.int64, dev)
-    _dense(key_count, where, "key_count", (n,), torch.int32, dev)
-    a = AttendArgs(n, h, g, d, code, rows if max_queries is None else max_queries,
+    if q.dim() != 3 or k.dim() != 3:
+        _refuse(where, "q, k and v have rows, heads and columns")
+    shape, dtype, dev = q.shape, q.dtype, q.device
+    rows, h, d = shape
+    key_rows, g = k.shape[:2]
+    n = key_count.shape[0]
+    a = AttendArgs(n, h, g, d, _dtype(dtype, where), rows if max_queries is None else max_queries,
                    key_rows if max_keys is None else max_keys, d ** -0.5 if scale is None else scale, rows, key_rows,
-                   q.data_ptr(), q.stride(0), q.stride(1), k.data_ptr(), k.stride(0), k.stride(1),
-                   v.data_ptr(), v.stride(0), v.stride(1), query_start.data_ptr(), key_start.data_ptr(),
-                   key_count.data_ptr())
-    lib = load()
-    with _on(dev, stream):
-        if out is None:
-            out = torch.empty((rows, h, d), dtype=q.dtype, device=dev)
-        else:
-            _array(out, where, "out", (rows, h, d), q.dtype, dev)
-        a.out, a.out_stride, a.out_head_stride = out.data_ptr(), out.stride(0), out.stride(1)
-        workspace = _workspace(workspace, lib.jdob_edge_attend_workspace(C.byref(a)), dev, where)
-        if workspace is not None:
-            a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-        jdob._check(lib.jdob_edge_attend(C.byref(a), _handle(dev, stream)), where)
+                   _array(q, where, "q", shape, dtype, dev), q.stride(0), q.stride(1),
+                   _array(k, where, "k", (key_rows, g, d), dtype, dev), k.stride(0), k.stride(1),
+                   _array(v, where, "v", (key_rows, g, d), dtype, dev), v.stride(0), v.stride(1),
+                   _dense(query_start, where, "query_start", (n + 1,), torch.int32, dev),
+                   _dense(key_start, where, "key_start", (n,), torch.int64, dev),
+                   _dense(key_count, where, "key_count", (n,), torch.int32, dev))
+    handle, context = _enter(dev, stream)
+    if context is not None:
+        with context:
+            return _attend(a, where, shape, dtype, dev, out, workspace, handle)
+    return _attend(a, where, shape, dtype, dev, out, workspace, handle)
+
+
+def _attend(a, where, shape, dtype, dev, out, workspace, handle):
+    if out is None:
+        out = torch.empty(shape, dtype=dtype, device=dev)
+        a.out = out.data_ptr()
+    else:
+        a.out = _array(out, where, "out", shape, dtype, dev)
+    a.out_stride, a.out_head_stride = out.stride(0), out.stride(1)
+    lib = _lib or load()
+    workspace = _workspace(a, workspace, lib.jdob_edge_attend_workspace, dev, where)
+    code = lib.jdob_edge_attend(C.byref(a), handle)
+    if code:
+        jdob._check(code, where)
     return out

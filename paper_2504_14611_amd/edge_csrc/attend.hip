@@ -69,17 +69,18 @@ __device__ inline Sequence sequence(const AttendParams &p, int u) {
 
 __device__ const u32x4 attend_zeros = {0, 0, 0, 0};
 
-// Staged keys or values: rows of DP elements, 16-byte chunks exchanged within the row so that what is
-// read at once falls on different LDS banks: of keys eight rows' equal chunks (16 bytes a lane), of
-// values eight rows' equal pairs of chunks (8 bytes a lane).  Rows of 96 elements start on other banks
-// already, and chunks stay within their group of four.
+// Staged keys or values: rows of DP elements, 16-byte chunks exchanged within the row so that what LDS
+// serves at once (256 bytes) falls on different banks.  Keys are read 16 bytes a lane, equal chunks of
+// rows 0-3, 12-15, 20-23 and 24-27 at once, then of the others; values 8 bytes a lane, four rows' equal
+// 64 bytes at once.  (With keys exchanged by r & 7 and values by twice that, every read took twice its
+// time.)
 template <int DP>
 __device__ inline int key_swap(int r) {
-  return DP == 96 ? r >> 1 & 3 : r & 7;
+  return DP == 128 ? r & 15 : DP == 96 ? r >> 2 & 3 : r >> 1 & 7;
 }
 template <int DP>
 __device__ inline int value_swap(int r) {
-  return DP == 96 ? (r >> 2 & 1) << 1 : DP == 128 ? (r & 7) << 1 : (r >> 1 & 3) << 1;
+  return DP == 128 ? (r & 3) << 2 : DP == 96 ? 0 : (r >> 1 & 1) << 2;
 }
 template <int DP>
 __device__ inline int key_spot(int r, int c) {

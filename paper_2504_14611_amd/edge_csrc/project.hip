@@ -428,6 +428,10 @@ __global__ __launch_bounds__(WAVES *WAVE) void stream_kernel(ProjectParams p) {
 
 __device__ const u32x4 edge_zeros = {0, 0, 0, 0};
 
+// The same for a tile, whose 32 rows' equal chunks are read together: LDS serves rows 0-3, 12-15, 20-23
+// and 24-27 at once, then the others, and its banks take 256 bytes, two rows.
+__device__ inline int tile_spot(int r, int c) { return r * SLICE + ((c ^ (r >> 1 & 7)) << 4); }
+
 // Stages COUNT rows' slice (bytes [at, at + 128) of rows first.., clamped to `last`) at dst.  DIRECT:
 // memory to LDS, without registers between; needs chunks that lie within the row or behind it.
 template <bool X8, bool DIRECT, int COUNT, int THREADS>
@@ -437,7 +441,7 @@ __device__ inline void stage(char *dst, const char *base, int64_t pitch, int fir
   auto each = [&](auto one) {
 #pragma unroll
     for (int i = 0; i < COUNT * 8 / THREADS; ++i) {
-      const int slot = i * THREADS + threadIdx.x, r = slot / 8, c = (slot % 8) ^ (r & 7);
+      const int slot = i * THREADS + threadIdx.x, r = slot / 8, c = (slot % 8) ^ (r >> 1 & 7);
       one(i * THREADS, first + r < last ? r : last - first, c * 16);
     }
   };
@@ -455,25 +459,72 @@ __device__ inline void stage(char *dst, const char *base, int64_t pitch, int fir
   }
 }
 
+// The low-rank part of one row's 16 columns first + 8 (e / 4) + e % 4.  The first eight ranks' B are
+// loaded before the main loop, from all adapters' corners of memory, and used behind it.
+template <typename T>
+struct RowLow {
+  typedef typename Mma<T>::frag frag;
+  int rank = 0, first, out_dim, pitch;
+  const float *v;
+  const T *b;
+  f32x4 vf[2];
+  frag bf[16];
+
+  __device__ const T *row_of(int e) const {
+    const int col = first + 8 * (e / 4) + e % 4;
+    return b + (int64_t)(col < out_dim ? col : out_dim - 1) * pitch;
+  }
+  __device__ void load(const ProjectParams &p, int row, int col) {
+    const int a = p.num_adapters > 0 && row < p.rows ? adapter_of(p, row) : -1;
+    if (a < 0) return;
+    rank = rank_of(p, a);
+    first = col;
+    out_dim = p.out_dim;
+    pitch = p.max_rank;
+    v = (const float *)p.v + (int64_t)row * p.slabs * 32;  // zeros from the rank to a multiple of 32
+    b = (const T *)p.up + (int64_t)a * p.out_dim * p.max_rank;
+    if (rank < 8) return;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) vf[i] = *(const f32x4 *)(v + 4 * i);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) bf[e] = *(const typename Raw<T, 8>::type *)row_of(e);
+  }
+  __device__ float value(int e) const {
+    float y = 0.0f;
+    if (rank >= 8)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) y += vf[k / 4][k % 4] * (float)bf[e][k];
+    for (int r = rank < 8 ? 0 : 8; r < rank; r += 8) {
+      const frag f = eight<T>(row_of(e), r, rank);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) y += v[r + k] * (float)f[k];
+    }
+    return y;
+  }
+};
+
 template <typename T, bool X8, bool DIRECT, int BM, int BN, int WM, int WN, int STAGES>
 struct Tile {
   static constexpr int THREADS = WM * WN * WAVE;
   static constexpr int FM = BM / WM / 32, FN = BN / WN / 32;  // 32x32 tiles a wave: rows, columns
   static constexpr int STAGE = (BM + BN) * SLICE;             // bytes
   static constexpr int LOADS = STAGE / 16 / THREADS;          // a thread's, each stage
+  static constexpr int ROW_LOADS = BM * 8 / THREADS;          // of them for rows
   static constexpr int OUT = BM * BN * 2;
   static constexpr int ROOM = STAGES * STAGE > OUT ? STAGES * STAGE : OUT;
 };
 
 // One workgroup: BM rows by BN columns, WM x WN waves.  W's rows are the products' first operand,
-// so a lane holds four consecutive columns of one row.  STAGES - 1 slices are under way while one
-// is multiplied.  Behind the slices of the inner dimension come those of the low-rank part: for each
+// so a lane holds four consecutive columns of one row.  A wave reads its operands a quarter of a slice
+// ahead, those of the next slice's first quarter before it multiplies the last of this one, so that the
+// barrier between them leaves the matrix units work; behind it the slice's buffer takes the slice after
+// the next.  Behind the slices of the inner dimension come those of the low-rank part: for each
 // adapter among the tile's rows, 32 ranks at a time, the rows' two-part v and the columns' B twice.
 // Their product is added to the adapter's own rows only (zeros times an infinity are not zero), so
 // other rows' v may be anything.  ROWWISE: few rows with many adapters, where each output's low-rank
 // part is computed by itself.
 template <typename T, bool X8, bool DIRECT, int BM, int BN, int WM, int WN, int STAGES, bool ROWWISE>
-__global__ __launch_bounds__(WM *WN *WAVE) void tile_kernel(ProjectParams p) {
+__global__ __launch_bounds__(WM *WN *WAVE, 2) void tile_kernel(ProjectParams p) {
   typedef Tile<T, X8, DIRECT, BM, BN, WM, WN, STAGES> K;
   typedef typename Mma<T>::frag frag;
   __shared__ __align__(16) char room[K::ROOM];
@@ -492,15 +543,17 @@ __global__ __launch_bounds__(WM *WN *WAVE) void tile_kernel(ProjectParams p) {
 
   // the dies start at different places of the inner dimension and do not all ask for the same ones
   const int turn = slices * die / 8;
+  auto buffer = [&](int t) { return room + t % STAGES * K::STAGE; };
+  auto place = [&](int t) { return (t + turn < slices ? t + turn : t + turn - slices) * SLICE; };
   auto load = [&](int t) {
-    char *const buf = room + t % STAGES * K::STAGE;
-    const int s = t + turn < slices ? t + turn : t + turn - slices;
-    stage<X8, DIRECT, BM, K::THREADS>(buf, p.x, p.x_pitch, row0, p.rows - 1, s * SLICE, len);
-    stage<X8, DIRECT, BN, K::THREADS>(buf + BM * SLICE, p.w, p.w_pitch, col0, p.out_dim - 1, s * SLICE, len);
+    char *const buf = buffer(t);
+    const int at = place(t);
+    stage<X8, DIRECT, BM, K::THREADS>(buf, p.x, p.x_pitch, row0, p.rows - 1, at, len);
+    stage<X8, DIRECT, BN, K::THREADS>(buf + BM * SLICE, p.w, p.w_pitch, col0, p.out_dim - 1, at, len);
   };
   // slice n of the low-rank part, which is slice slices + n of all
   auto load_low = [&](int n) {
-    char *const buf = room + (slices + n) % STAGES * K::STAGE;
+    char *const buf = buffer(slices + n);
     const int a = __builtin_amdgcn_readfirstlane(list[n / p.slabs]), slab = n % p.slabs;
     stage<false, true, BM, K::THREADS>(buf, (const char *)p.v + (int64_t)slab * p.rows * SLICE, SLICE, row0,
                                        p.rows - 1, 0, SLICE);
@@ -510,7 +563,7 @@ __global__ __launch_bounds__(WM *WN *WAVE) void tile_kernel(ProjectParams p) {
     const unsigned to = lds_address(buf + BM * SLICE) + wave * WAVE * 16;
 #pragma unroll
     for (int i = 0; i < BN * 8 / K::THREADS; ++i) {
-      const int e = i * K::THREADS + threadIdx.x, c = e / 8, r = ((e % 8) ^ (c & 7)) % 4 * 8;
+      const int e = i * K::THREADS + threadIdx.x, c = e / 8, r = ((e % 8) ^ (c >> 1 & 7)) % 4 * 8;
       const bool in = col0 + c < p.out_dim && r < left;
       const T *const from = up + (in ? (int64_t)c * p.max_rank + r : 0);
       if (direct) {
@@ -524,8 +577,13 @@ __global__ __launch_bounds__(WM *WN *WAVE) void tile_kernel(ProjectParams p) {
   };
   typename Main<T, X8>::acc acc[K::FM][K::FN] = {};
 #pragma unroll
-  for (int s = 0; s < STAGES - 1; ++s)
+  for (int s = 0; s < STAGES; ++s)
     if (s < slices) load(s);
+  RowLow<T> low;
+  if constexpr (ROWWISE) {
+    static_assert(K::FM == 1 && K::FN == 1, "a row a lane");
+    low.load(p, row0 + wm * 32 + l32, col0 + wn * 32 + 4 * half);
+  }
   int behind = 0;  // slices of the low-rank part
   if (!ROWWISE && p.num_adapters > 0) {
     for (int r0 = wave * WAVE; r0 < BM; r0 += K::THREADS) {
@@ -552,45 +610,77 @@ __global__ __launch_bounds__(WM *WN *WAVE) void tile_kernel(ProjectParams p) {
     __syncthreads();
     behind = __builtin_amdgcn_readfirstlane(listed) * p.slabs;
 #pragma unroll
-    for (int s = 0; s < STAGES - 1; ++s)
+    for (int s = 0; s < STAGES; ++s)
       if (s >= slices && s - slices < behind) load_low(s - slices);
   }
-  // this slice has landed and the slice before it has been read, by all waves; the next one is on its way
-  auto advance = [&](int s) {
-    if (DIRECT && s + STAGES - 2 < slices) {
-      wait_loads<(STAGES - 2) * K::LOADS>();
+  auto load_any = [&](int t) {
+    if (t < slices) {
+      load(t);
+    } else if (t - slices < behind) {
+      load_low(t - slices);
+    }
+  };
+  u32x4 xf[2][K::FM], wf[2][K::FN];
+  auto fetch = [&](int t, int k) {  // 32 bytes of the inner dimension
+    const char *const buf = buffer(t);
+#pragma unroll
+    for (int i = 0; i < K::FM; ++i)
+      xf[k & 1][i] = *(const u32x4 *)(buf + tile_spot((wm * K::FM + i) * 32 + l32, k * 2 + half));
+#pragma unroll
+    for (int j = 0; j < K::FN; ++j)
+      wf[k & 1][j] = *(const u32x4 *)(buf + BM * SLICE + tile_spot((wn * K::FN + j) * 32 + l32, k * 2 + half));
+  };
+  auto multiply = [&](int k, int i0, int i1) {
+#pragma unroll
+    for (int i = 0; i < K::FM; ++i)
+      if (i >= i0 && i < i1)
+#pragma unroll
+        for (int j = 0; j < K::FN; ++j) acc[i][j] = Main<T, X8>::mma(wf[k & 1][j], xf[k & 1][i], acc[i][j]);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  constexpr int HALF = K::FM / 2;
+  // rows of slice t, then columns
+  auto load_rows = [&](int t) {
+    if (t < slices) stage<X8, DIRECT, BM, K::THREADS>(buffer(t), p.x, p.x_pitch, row0, p.rows - 1, place(t), len);
+  };
+  auto load_columns = [&](int t) {
+    if (t < slices) {
+      stage<X8, DIRECT, BN, K::THREADS>(buffer(t) + BM * SLICE, p.w, p.w_pitch, col0, p.out_dim - 1, place(t), len);
+    } else if (t - slices < behind) {
+      load_low(t - slices);
+    }
+  };
+  // slice t has landed: of the loads after it those of STAGES - 2 slices and of `rows` are under way
+  auto landed = [&](int t) {
+    if (DIRECT && t + STAGES - 1 < slices) {
+      wait_loads<(STAGES - 2) * K::LOADS + K::ROW_LOADS>();
     } else {
       wait_loads<0>();
     }
     barrier();
-    const int next = s + STAGES - 1;
-    if (next < slices) {
-      load(next);
-    } else if (next - slices < behind) {
-      load_low(next - slices);
-    }
   };
-  for (int s = 0; s < slices; ++s) {
-    advance(s);
-    const char *const buf = room + s % STAGES * K::STAGE;
-    u32x4 xf[2][K::FM], wf[2][K::FN];
-    auto fetch = [&](int b, int k) {  // 32 bytes of the inner dimension
-#pragma unroll
-      for (int i = 0; i < K::FM; ++i)
-        xf[b][i] = *(const u32x4 *)(buf + spot((wm * K::FM + i) * 32 + l32, k * 2 + half));
-#pragma unroll
-      for (int j = 0; j < K::FN; ++j)
-        wf[b][j] = *(const u32x4 *)(buf + BM * SLICE + spot((wn * K::FN + j) * 32 + l32, k * 2 + half));
-    };
-    fetch(0, 0);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      if (k < 3) fetch((k + 1) & 1, k + 1);
-#pragma unroll
-      for (int i = 0; i < K::FM; ++i)
-#pragma unroll
-        for (int j = 0; j < K::FN; ++j) acc[i][j] = Main<T, X8>::mma(wf[k & 1][j], xf[k & 1][i], acc[i][j]);
-    }
+  wait_loads<0>();
+  barrier();
+  fetch(0, 0);
+  for (int t = 0; t < slices; ++t) {
+    fetch(t, 1);
+    __builtin_amdgcn_sched_barrier(0);
+    multiply(0, 0, K::FM);
+    fetch(t, 2);
+    __builtin_amdgcn_sched_barrier(0);
+    multiply(1, 0, K::FM);
+    fetch(t, 3);
+    __builtin_amdgcn_sched_barrier(0);
+    multiply(2, 0, HALF);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    barrier();  // the slice has been read by all waves: its buffer is free
+    load_rows(t + STAGES);
+    multiply(2, HALF, K::FM);
+    landed(t + 1);
+    load_columns(t + STAGES);
+    if (t + 1 < slices) fetch(t + 1, 0);
+    __builtin_amdgcn_sched_barrier(0);
+    multiply(3, 0, K::FM);
   }
 
   // to binary32, with the scales of 8-bit rows and columns
@@ -616,8 +706,12 @@ __global__ __launch_bounds__(WM *WN *WAVE) void tile_kernel(ProjectParams p) {
     }
   }
   for (int n = 0; n < behind; ++n) {
-    advance(slices + n);
-    const char *const buf = room + (slices + n) % STAGES * K::STAGE;
+    if (n > 0) {
+      wait_loads<0>();
+      barrier();
+      load_any(slices + n + STAGES - 1);
+    }
+    const char *const buf = buffer(slices + n);
     const int a = __builtin_amdgcn_readfirstlane(list[n / p.slabs]);
 #pragma unroll
     for (int i = 0; i < K::FM; ++i) {
@@ -626,35 +720,20 @@ __global__ __launch_bounds__(WM *WN *WAVE) void tile_kernel(ProjectParams p) {
       if (!__any(mine)) continue;
       frag v[4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) v[k] = *(const frag *)(buf + spot(r, k * 2 + half));
+      for (int k = 0; k < 4; ++k) v[k] = *(const frag *)(buf + tile_spot(r, k * 2 + half));
 #pragma unroll
       for (int j = 0; j < K::FN; ++j) {
         f32x16 more = {};
 #pragma unroll
         for (int k = 0; k < 4; ++k)
-          more = Mma<T>::m32(*(const frag *)(buf + BM * SLICE + spot((wn * K::FN + j) * 32 + l32, k * 2 + half)), v[k], more);
+          more = Mma<T>::m32(*(const frag *)(buf + BM * SLICE + tile_spot((wn * K::FN + j) * 32 + l32, k * 2 + half)), v[k], more);
         if (mine) sum[i][j] += more;
       }
     }
   }
   if constexpr (ROWWISE) {
-    if (p.num_adapters > 0) {
 #pragma unroll
-      for (int i = 0; i < K::FM; ++i) {
-        const int row = row0 + (wm * K::FM + i) * 32 + l32;
-#pragma unroll
-        for (int j = 0; j < K::FN; ++j)
-#pragma unroll
-          for (int e = 0; e < 16; e += 8) {
-            LowRank<T, 8> low[8];
-#pragma unroll
-            for (int c = 0; c < 8; ++c)
-              low[c].load(p, row, col0 + (wn * K::FN + j) * 32 + 8 * ((e + c) / 4) + 4 * half + c % 4);
-#pragma unroll
-            for (int c = 0; c < 8; ++c) sum[i][j][e + c] += low[c].value();
-          }
-      }
-    }
+    for (int e = 0; e < 16; ++e) sum[0][0][e] += low.value(e);
   }
   wait_loads<0>();
   __syncthreads();  // all slices have been read
@@ -761,13 +840,13 @@ int project(const ProjectParams &p, hipStream_t stream) {
               : launch_tile<T, X8, false, 128, 128, 2, 2, 2>(p, stream);
   if (rw) return launch_tile<T, X8, true, 64, 64, 2, 2, 4, true>(p, stream);
   // The tile that takes least time by a count of rounds: a slice of 128 bytes takes a round of 256
-  // workgroups 1.87 us with tiles of 256 x 256 (one a compute unit), a round of 512 1.10 us with
-  // 128 x 128 and 0.46 us with 64 x 64 (two a compute unit), measured at 8192 x 4096 x 4096.
+  // workgroups 1.86 us with tiles of 256 x 256 (one a compute unit), a round of 512 1.1 us (8 bits: 1.4)
+  // with 128 x 128 and 0.47 us with 64 x 64 (two a compute unit), measured at 8192 x 4096 x 4096.
   auto rounds = [&](int side, int at_once) {
     const int64_t tiles = (int64_t)((p.rows + side - 1) / side) * ((p.out_dim + side - 1) / side);
     return (double)((tiles + at_once - 1) / at_once);
   };
-  const double t256 = 1.87 * rounds(256, 256), t128 = 1.10 * rounds(128, 512), t64 = 0.46 * rounds(64, 512);
+  const double t256 = 1.86 * rounds(256, 256), t128 = (X8 ? 1.4 : 1.1) * rounds(128, 512), t64 = 0.47 * rounds(64, 512);
   if (t64 <= t128 && t64 <= t256) return launch_tile<T, X8, true, 64, 64, 2, 2, 4>(p, stream);
   if (t128 <= t256) return launch_tile<T, X8, true, 128, 128, 2, 2, 2>(p, stream);
   return launch_tile<T, X8, true, 256, 256, 2, 4, 2>(p, stream);
