@@ -46,7 +46,9 @@ extern "C" {
 
 typedef enum { JDOB_EDGE_BF16 = 0, JDOB_EDGE_F16 = 1, JDOB_EDGE_F32 = 2 } jdob_edge_dtype;
 
+#define JDOB_EDGE_MAX_ROWS 1073741824
 #define JDOB_EDGE_MAX_NORM_DIM 16384
+#define JDOB_EDGE_MAX_PROJECT_DIM 1048576 /* 8 bits: in_dim to 131072      */
 #define JDOB_EDGE_MAX_RANK 256
 #define JDOB_EDGE_MAX_HEAD_DIM 128
 #define JDOB_EDGE_MAX_SEQUENCES 65535
@@ -59,7 +61,7 @@ typedef enum { JDOB_EDGE_BF16 = 0, JDOB_EDGE_F16 = 1, JDOB_EDGE_F32 = 2 } jdob_e
  * may be x or residual itself (same stride): each row is read whole before
  * it is written.  out and q may both be asked for; sum needs a residual. */
 typedef struct {
-  int32_t rows, dim;       /* rows >= 0; 1 <= dim <= JDOB_EDGE_MAX_NORM_DIM  */
+  int32_t rows, dim;       /* rows >= 0, dim >= 1, to the limits above       */
   int32_t dtype;           /* of x, residual, weight, sum, out               */
   float eps;               /* >= 0, finite                                   */
   const void *x;           /* [rows][dim]                                    */

@@ -29,7 +29,7 @@ except ImportError:
         return torch.cuda.current_device()
 
 EDGE_BF16, EDGE_F16, EDGE_F32 = 0, 1, 2
-MAX_NORM_DIM, MAX_RANK, MAX_HEAD_DIM, MAX_SEQUENCES = 16384, 256, 128, 65535
+MAX_ROWS, MAX_NORM_DIM, MAX_RANK, MAX_HEAD_DIM, MAX_SEQUENCES = 1 << 30, 16384, 256, 128, 65535
 
 EXPORTS = ("jdob_edge_norm", "jdob_edge_project", "jdob_edge_project_workspace", "jdob_edge_attend",
            "jdob_edge_attend_workspace")
@@ -136,6 +136,8 @@ def norm(x, weight, eps: float = 1e-6, residual=None, bits8: bool = False, out16
         _refuse(where, "x has rows and columns")
     shape, dtype, dev = x.shape, x.dtype, x.device
     rows, dim = shape
+    if rows > MAX_ROWS:
+        _refuse(where, f"{rows} rows", jdob.JDOB_ERR_UNSUPPORTED)
     if out16 is None:
         out16 = not bits8
     if not (bits8 or out16):
@@ -198,6 +200,8 @@ def project(x, weight, x_scale=None, weight_scale=None, adapters: Optional[dict]
     if x.dim() != 2 or weight.dim() != 2:
         _refuse(where, "x and weight have rows and columns")
     rows, i = x.shape
+    if rows > MAX_ROWS:
+        _refuse(where, f"{rows} rows", jdob.JDOB_ERR_UNSUPPORTED)
     o, dev = weight.shape[0], x.device
     kind = x.dtype
     bits8 = kind is torch.int8
@@ -276,10 +280,12 @@ def attend(q, k, v, query_start, key_start, key_count, scale: Optional[float] = 
         _refuse(where, "q, k and v have rows, heads and columns")
     shape, dtype, dev = q.shape, q.dtype, q.device
     rows, h, d = shape
+    if rows > MAX_ROWS:
+        _refuse(where, f"{rows} rows", jdob.JDOB_ERR_UNSUPPORTED)
     key_rows, g = k.shape[:2]
     n = key_count.shape[0]
     a = AttendArgs(n, h, g, d, _dtype(dtype, where), rows if max_queries is None else max_queries,
-                   key_rows if max_keys is None else max_keys, d ** -0.5 if scale is None else scale, rows, key_rows,
+                   min(key_rows, 0x7fffffff) if max_keys is None else max_keys, d ** -0.5 if scale is None else scale, rows, key_rows,
                    _array(q, where, "q", shape, dtype, dev), q.stride(0), q.stride(1),
                    _array(k, where, "k", (key_rows, g, d), dtype, dev), k.stride(0), k.stride(1),
                    _array(v, where, "v", (key_rows, g, d), dtype, dev), v.stride(0), v.stride(1),

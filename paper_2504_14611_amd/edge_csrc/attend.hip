@@ -99,6 +99,7 @@ template <typename T, int DP, bool DIRECT, bool VALUES, int COUNT, int THREADS>
 __device__ inline void stage(char *dst, const T *base, int64_t stride, int64_t first, int count, int dim, bool careful,
                              int t, int t0) {
   constexpr int CH = DP / 8;
+  static_assert(COUNT * CH % THREADS == 0, "whole rounds");
   const T *const tile = base + first * stride;
   auto each = [&](auto one) {
 #pragma unroll
@@ -341,7 +342,9 @@ template <typename T, int DP, bool DIRECT>
 __global__ __launch_bounds__(PROMPT_WAVES *WAVE, 2) void prompt_kernel(AttendParams p) {
   typedef typename Mma<T>::frag frag;
   constexpr int THREADS = PROMPT_WAVES * WAVE, BYTES = PROMPT_KEYS * DP * 2;
-  __shared__ __align__(16) char room[4 * BYTES];  // two buffers of keys and values
+  // two buffers of keys and values; the waves' rows (32 each) come in through the second
+  __shared__ __align__(16) char room[4 * BYTES];
+  static_assert(2 * BYTES >= PROMPT_ROWS * DP * 2, "room for the rows");
   const int lane = threadIdx.x % WAVE, wave = wave_index(), l32 = lane % 32, half = lane / 32;
   // Workgroups go to the chip's eight dies in turn: heads that read one key head should share a die's cache.
   const int kv = blockIdx.x % p.heads % p.kv_heads, head = kv * p.group + blockIdx.x % p.heads / p.kv_heads;
@@ -477,7 +480,8 @@ __global__ __launch_bounds__(FEW_WAVES *WAVE) void few_kernel(AttendParams p) {
   const int columns = rows * p.group, column = tile * FEW_COLUMNS + l32;
   if (tile * FEW_COLUMNS >= columns) return;
   // this split's keys; the last split takes what the others leave (max_keys may be too small)
-  const int from = split * p.each, until = split + 1 < p.splits && from + p.each < q.keys ? from + p.each : q.keys;
+  const int from = split * p.each;
+  const int until = split + 1 < p.splits && (int64_t)from + p.each < q.keys ? from + p.each : q.keys;
   if (from >= until && split > 0) return;
   const bool have = column < columns;
   const int row = have ? column / p.group : 0, head = kv * p.group + (have ? column % p.group : 0);
@@ -587,7 +591,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void join_kernel(AttendParams p) {
   if (col >= rows * p.group) return;
   const int64_t pitch = p.dim + 4, step = 32 * pitch;
   const float *const part = p.part + (((int64_t)u * p.kv_heads + kv) * p.tiles + tile) * p.splits * step + col % FEW_COLUMNS * pitch;
-  const int used = q.keys > 0 ? (q.keys + p.each - 1) / p.each : 1, splits = used < p.splits ? used : p.splits;
+  const int used = q.keys > 0 ? (q.keys - 1) / p.each + 1 : 1, splits = used < p.splits ? used : p.splits;
   const int t = threadIdx.x, lane = t % WAVE;
   // every wave for itself: the maximum, the weights, their sum
   float tops[MAX_SPLITS / WAVE], top = LOWEST, sum = 0.0f;
@@ -633,7 +637,7 @@ int attend_check(const jdob_edge_attend_args *a, bool sizes_only) {
     return JDOB_ERR_INVALID_ARG;
   if (a->dtype != JDOB_EDGE_BF16 && a->dtype != JDOB_EDGE_F16) return JDOB_ERR_UNSUPPORTED;
   if (a->head_dim > JDOB_EDGE_MAX_HEAD_DIM || a->head_dim % 8 || a->num_heads > 1024 ||
-      a->num_sequences > JDOB_EDGE_MAX_SEQUENCES || a->query_rows > 0x7fffffff)
+      a->num_sequences > JDOB_EDGE_MAX_SEQUENCES || a->query_rows > JDOB_EDGE_MAX_ROWS)
     return JDOB_ERR_UNSUPPORTED;
   if (sizes_only || a->num_sequences == 0 || a->query_rows == 0 || a->max_queries == 0) return JDOB_OK;
   if (!a->q || !a->out || !a->query_start || !a->key_start || !a->key_count || (a->key_rows > 0 && (!a->k || !a->v)))
@@ -664,6 +668,7 @@ FewPlan few_plan(const jdob_edge_attend_args *a) {
   // about four workgroups for each place that the chip has for one (two a compute unit), whose
   // sequences may be of very different lengths, but no fewer than 512 keys each
   int64_t each = (a->max_keys * groups + 2047) / 2048;
+  each = each > a->max_keys ? a->max_keys : each;
   each = each < 512 ? 512 : (each + 63) & ~63;
   int64_t splits = (a->max_keys + each - 1) / each;
   if (splits > MAX_SPLITS) {

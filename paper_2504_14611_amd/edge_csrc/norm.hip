@@ -187,7 +187,7 @@ int norm_check(const jdob_edge_norm_args *a) {
     return JDOB_ERR_INVALID_ARG;
   if (a->dtype != JDOB_EDGE_BF16 && a->dtype != JDOB_EDGE_F16 && a->dtype != JDOB_EDGE_F32)
     return JDOB_ERR_UNSUPPORTED;
-  if (a->dim > JDOB_EDGE_MAX_NORM_DIM) return JDOB_ERR_UNSUPPORTED;
+  if (a->dim > JDOB_EDGE_MAX_NORM_DIM || a->rows > JDOB_EDGE_MAX_ROWS) return JDOB_ERR_UNSUPPORTED;
   if (a->rows == 0) return JDOB_OK;
   if (!a->x || !a->weight || (!a->out && !a->q) || (a->q && !a->scale) || (a->sum && !a->residual))
     return JDOB_ERR_INVALID_ARG;

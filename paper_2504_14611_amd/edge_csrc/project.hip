@@ -780,7 +780,8 @@ int project_check(const jdob_edge_project_args *a, bool sizes_only) {
   if (a->num_adapters > 0 && a->max_rank < 1) return JDOB_ERR_INVALID_ARG;
   if (a->dtype != JDOB_EDGE_BF16 && a->dtype != JDOB_EDGE_F16) return JDOB_ERR_UNSUPPORTED;
   if (a->num_adapters > 0 && a->max_rank > JDOB_EDGE_MAX_RANK) return JDOB_ERR_UNSUPPORTED;
-  if (a->in_dim > (1 << 20) || a->out_dim > (1 << 20) || (a->bits8 && a->in_dim > 131072))
+  if (a->rows > JDOB_EDGE_MAX_ROWS || a->in_dim > JDOB_EDGE_MAX_PROJECT_DIM ||
+      a->out_dim > JDOB_EDGE_MAX_PROJECT_DIM || (a->bits8 && a->in_dim > 131072))
     return JDOB_ERR_UNSUPPORTED;
   if (sizes_only || a->rows == 0) return JDOB_OK;
   if (!a->x || !a->weight || !a->out || a->x_stride < a->in_dim || a->weight_stride < a->in_dim ||

@@ -36,7 +36,7 @@ def test_header_binding_and_library_agree():
                     fields.append((name.strip().lstrip("* "), "pointer" if "*" in name else kind))
         kinds = {C.c_void_p: "pointer", C.c_int32: "int32_t", C.c_int64: "int64_t", C.c_float: "float"}
         assert [(n, kinds[t]) for n, t in cls._fields_] == fields
-    for name, value in (("MAX_NORM_DIM", edge.MAX_NORM_DIM), ("MAX_RANK", edge.MAX_RANK),
+    for name, value in (("MAX_ROWS", edge.MAX_ROWS), ("MAX_NORM_DIM", edge.MAX_NORM_DIM), ("MAX_RANK", edge.MAX_RANK),
                         ("MAX_HEAD_DIM", edge.MAX_HEAD_DIM), ("MAX_SEQUENCES", edge.MAX_SEQUENCES)):
         assert re.search(rf"#define JDOB_EDGE_{name} {value}\b", src), name
 
@@ -50,7 +50,7 @@ def norm_args(**kw):
 
 @pytest.mark.parametrize("fields,code", [
     ({"rows": -1}, INVALID), ({"dim": 0}, INVALID), ({"eps": -1e-6}, INVALID), ({"eps": float("nan")}, INVALID),
-    ({"eps": float("inf")}, INVALID), ({"dtype": 3}, UNSUPPORTED), ({"dtype": -1}, UNSUPPORTED),
+    ({"eps": float("inf")}, INVALID), ({"dtype": 3}, UNSUPPORTED), ({"dtype": -1}, UNSUPPORTED), ({"rows": (1 << 30) + 1}, UNSUPPORTED),
     ({"dim": 16385, **{k: 20000 for k in ("x_stride", "residual_stride", "sum_stride", "out_stride", "q_stride")}}, UNSUPPORTED),
     ({"x": None}, INVALID), ({"weight": None}, INVALID), ({"out": None, "q": None}, INVALID), ({"scale": None}, INVALID),
     ({"residual": None}, INVALID), ({"x_stride": 63}, INVALID), ({"residual_stride": 1}, INVALID),
@@ -71,7 +71,7 @@ def project_args(**kw):
 @pytest.mark.parametrize("fields,code", [
     ({"rows": -1}, INVALID), ({"in_dim": 0}, INVALID), ({"out_dim": 0}, INVALID), ({"num_adapters": -1}, INVALID),
     ({"max_rank": 0}, INVALID), ({"bits8": 2}, INVALID), ({"dtype": edge.EDGE_F32}, UNSUPPORTED),
-    ({"max_rank": 257}, UNSUPPORTED), ({"in_dim": 131073, "x_stride": 1 << 20, "weight_stride": 1 << 20}, UNSUPPORTED),
+    ({"max_rank": 257}, UNSUPPORTED), ({"rows": (1 << 30) + 1}, UNSUPPORTED), ({"out_dim": (1 << 20) + 1}, UNSUPPORTED), ({"in_dim": 131073, "x_stride": 1 << 20, "weight_stride": 1 << 20}, UNSUPPORTED),
     ({"x": None}, INVALID), ({"weight": None}, INVALID), ({"out": None}, INVALID), ({"x_scale": None}, INVALID),
     ({"weight_scale": None}, INVALID), ({"down": None}, INVALID), ({"up": None}, INVALID), ({"gain": None}, INVALID),
     ({"row_adapter": None}, INVALID), ({"workspace": None}, INVALID), ({"workspace": FAKE + 4}, INVALID),
