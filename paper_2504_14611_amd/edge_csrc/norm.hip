@@ -169,12 +169,11 @@ template <typename T>
 int norm_dispatch(const NormParams &p, hipStream_t stream) {
   constexpr int VE = 16 / (int)sizeof(T);
   const int v = (p.dim + VE - 1) / VE;  // vectors a row
+  // A wave a row saves the exchange through LDS, but keeps only as many loads under way as one wave has
+  // registers for: 4096 rows of 1024 (bf16, with a residual) take 7.3 us so and 9.0 with four waves a row,
+  // 8191 rows of 4096 take 45.6 so and 40.9 with four waves, 256 rows of 4096 7.4 and 5.1.
   if (v <= 64) return norm_launch<T, 64, 1>(p, stream);
-  if (p.rows >= 1024) {
-    if (v <= 128) return norm_launch<T, 64, 2>(p, stream);
-    if (v <= 256) return norm_launch<T, 64, 4>(p, stream);
-    if (v <= 512) return norm_launch<T, 64, 8>(p, stream);
-  }
+  if (v <= 128 && p.rows >= 1024) return norm_launch<T, 64, 2>(p, stream);
   if (v <= 256) return norm_launch<T, 256, 1>(p, stream);
   if (v <= 512) return norm_launch<T, 256, 2>(p, stream);
   if (v <= 1024) return norm_launch<T, 256, 4>(p, stream);

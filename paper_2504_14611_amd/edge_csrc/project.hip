@@ -527,6 +527,7 @@ template <typename T, bool X8, bool DIRECT, int BM, int BN, int WM, int WN, int 
 __global__ __launch_bounds__(WM *WN *WAVE, 2) void tile_kernel(ProjectParams p) {
   typedef Tile<T, X8, DIRECT, BM, BN, WM, WN, STAGES> K;
   typedef typename Mma<T>::frag frag;
+  constexpr bool SMALL = K::FM * K::FN == 1;
   __shared__ __align__(16) char room[K::ROOM];
   __shared__ int ids[BM], list[BM], listed;
   const int lane = threadIdx.x % WAVE, wave = wave_index();
@@ -659,28 +660,69 @@ __global__ __launch_bounds__(WM *WN *WAVE, 2) void tile_kernel(ProjectParams p) 
     }
     barrier();
   };
-  wait_loads<0>();
-  barrier();
-  fetch(0, 0);
-  for (int t = 0; t < slices; ++t) {
-    fetch(t, 1);
-    __builtin_amdgcn_sched_barrier(0);
-    multiply(0, 0, K::FM);
-    fetch(t, 2);
-    __builtin_amdgcn_sched_barrier(0);
-    multiply(1, 0, K::FM);
-    fetch(t, 3);
-    __builtin_amdgcn_sched_barrier(0);
-    multiply(2, 0, HALF);
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    barrier();  // the slice has been read by all waves: its buffer is free
-    load_rows(t + STAGES);
-    multiply(2, HALF, K::FM);
-    landed(t + 1);
-    load_columns(t + STAGES);
-    if (t + 1 < slices) fetch(t + 1, 0);
-    __builtin_amdgcn_sched_barrier(0);
-    multiply(3, 0, K::FM);
+  if constexpr (SMALL) {
+    // A wave's one product a quarter would not cover the reads of the next: it reads a whole slice while it
+    // multiplies the one before, and passes one barrier a slice.
+    u32x4 xs[2][4], ws[2][4];
+    auto multiply_slice = [&](auto set) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        acc[0][0] = Main<T, X8>::mma(ws[decltype(set)::value][k], xs[decltype(set)::value][k], acc[0][0]);
+    };
+    auto step = [&](int t, auto set, auto other) {
+      // slice t has landed and the one before it has been read, by all waves
+      if (DIRECT && t + STAGES - 2 < slices) {
+        wait_loads<(STAGES - 2) * K::LOADS>();
+      } else {
+        wait_loads<0>();
+      }
+      barrier();
+      if (t > 0) load_any(t + STAGES - 1);
+      const char *const buf = buffer(t);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        xs[decltype(set)::value][k] = *(const u32x4 *)(buf + tile_spot(wm * 32 + l32, k * 2 + half));
+        ws[decltype(set)::value][k] = *(const u32x4 *)(buf + BM * SLICE + tile_spot(wn * 32 + l32, k * 2 + half));
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      if (t > 0) multiply_slice(other);
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    int t = 0;
+    for (; t + 1 < slices; t += 2) {
+      step(t, Count<0>(), Count<1>());
+      step(t + 1, Count<1>(), Count<0>());
+    }
+    if (t < slices) {
+      step(t, Count<0>(), Count<1>());
+      multiply_slice(Count<0>());
+    } else {
+      multiply_slice(Count<1>());
+    }
+  } else {
+    wait_loads<0>();
+    barrier();
+    fetch(0, 0);
+    for (int t = 0; t < slices; ++t) {
+      fetch(t, 1);
+      __builtin_amdgcn_sched_barrier(0);
+      multiply(0, 0, K::FM);
+      fetch(t, 2);
+      __builtin_amdgcn_sched_barrier(0);
+      multiply(1, 0, K::FM);
+      fetch(t, 3);
+      __builtin_amdgcn_sched_barrier(0);
+      multiply(2, 0, HALF);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      barrier();  // the slice has been read by all waves: its buffer is free
+      load_rows(t + STAGES);
+      multiply(2, HALF, K::FM);
+      landed(t + 1);
+      load_columns(t + STAGES);
+      if (t + 1 < slices) fetch(t + 1, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      multiply(3, 0, K::FM);
+    }
   }
 
   // to binary32, with the scales of 8-bit rows and columns
@@ -706,7 +748,7 @@ __global__ __launch_bounds__(WM *WN *WAVE, 2) void tile_kernel(ProjectParams p) 
     }
   }
   for (int n = 0; n < behind; ++n) {
-    if (n > 0) {
+    if (SMALL || n > 0) {
       wait_loads<0>();
       barrier();
       load_any(slices + n + STAGES - 1);
@@ -821,7 +863,7 @@ int launch_tile(const ProjectParams &p, hipStream_t stream) {
 }
 
 // Few rows with many adapters: the low-rank part output by output.
-bool rowwise(int rows, int num_adapters) { return rows <= 512 && num_adapters * 16 >= rows; }
+bool rowwise(int rows, int num_adapters) { return rows <= 512 && num_adapters * 8 >= rows; }
 
 template <typename T, bool X8>
 int project(const ProjectParams &p, hipStream_t stream) {
