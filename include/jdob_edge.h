@@ -55,8 +55,9 @@ typedef enum { JDOB_EDGE_BF16 = 0, JDOB_EDGE_F16 = 1, JDOB_EDGE_F32 = 2 } jdob_e
 
 /* h = x + residual;  y_i = h_i * weight_i / sqrt(mean(h^2) + eps).
  * Sums are binary32 and start from the unrounded h.  8-bit output:
- * scale = max|y| / 127, q_i = y_i / scale rounded to the nearest integer (to
- * even) in [-127, 127], so that q_i * scale stands for y_i; a row of zeros
+ * scale = max|y| / 127, q_i = y_i / scale (y before it is rounded to dtype,
+ * a binary32 division) rounded to the nearest integer (to even) in
+ * [-127, 127], so that q_i * scale stands for y_i; a row of zeros
  * has scale 0; a row with a NaN or an infinity in h has scale NaN.  `sum`
  * may be x or residual itself (same stride): each row is read whole before
  * it is written.  out and q may both be asked for; sum needs a residual. */

@@ -137,10 +137,9 @@ __global__ __launch_bounds__(norm_threads(TPR)) void norm_kernel(NormParams p) {
       }
     const unsigned top = row_max<TPR>(m, part_max);
     const bool finite = top < 0x7f800000u;
-    // below 2^-100 the reciprocal could overflow: such a row counts as zeros
+    // below 2^-100 a row counts as zeros
     const bool zero = top < 0x0d800000u;
     const float scale = zero ? 0.0f : __uint_as_float(top) / 127.0f;
-    const float inv = zero || !finite ? 0.0f : 1.0f / scale;
     if (t == 0) p.scale[row] = finite ? scale : __uint_as_float(0x7fc00000u);
     int8_t *const q = p.q + row * p.q_stride;
 #pragma unroll
@@ -148,7 +147,7 @@ __global__ __launch_bounds__(norm_threads(TPR)) void norm_kernel(NormParams p) {
       const int at = (j * TPR + t) * VE;
       typename Raw<int8_t, VE>::type c;
 #pragma unroll
-      for (int i = 0; i < VE; ++i) c[i] = finite ? (int8_t)(int)rintf(h[j][i] * inv) : (int8_t)0;
+      for (int i = 0; i < VE; ++i) c[i] = finite && !zero ? (int8_t)(int)rintf(h[j][i] / scale) : (int8_t)0;
       if (at + VE <= dim) {
         *(typename Raw<int8_t, VE>::type *)(q + at) = c;
       } else {

@@ -91,3 +91,12 @@ def test_norm_one_row_between_others_and_on_another_stream():
     for key in ("sum", "q", "scale"):
         assert torch.equal(got[key], all_rows[key])
     assert edge.norm(x[:0], w, residual=r[:0], bits8=True)["q"].shape == (0, 4096)
+
+
+@pytest.mark.parametrize("rows,dim", [(2000, 4096), (3000, 1000), (600, 16384)])
+def test_codes_are_the_division_of_the_rows_by_their_scale(rows, dim):
+    """binary32 rows come out as they are divided: every code is the nearest integer to out / scale, ties to even."""
+    x, r, w = inputs(rows, dim, F32, True, seed=dim)
+    got = edge.norm(x, w, residual=r, bits8=True, out16=True)
+    want = torch.round(got["out"].cpu() / got["scale"].cpu()[:, None])
+    assert torch.equal(got["q"].cpu().float(), want), (got["q"].cpu().float() != want).sum()
