@@ -57,8 +57,10 @@ typedef enum { JDOB_EDGE_BF16 = 0, JDOB_EDGE_F16 = 1, JDOB_EDGE_F32 = 2 } jdob_e
  * Sums are binary32 and start from the unrounded h.  8-bit output:
  * scale = max|y| / 127, q_i = y_i / scale (y before it is rounded to dtype,
  * a binary32 division) rounded to the nearest integer (to even) in
- * [-127, 127], so that q_i * scale stands for y_i; a row of zeros
- * has scale 0; a row with a NaN or an infinity in h has scale NaN.  `sum`
+ * [-127, 127], so that q_i * scale stands for y_i (coarser below
+ * max|y| = 2^-119, whose scales are subnormal); a row whose y are zeros, or
+ * whose scale binary32 has no number for, has scale 0; a row with a NaN or an
+ * infinity in y has scale NaN, and so has a row of zeros with eps = 0.  `sum`
  * may be x or residual itself (same stride): each row is read whole before
  * it is written.  out and q may both be asked for; sum needs a residual. */
 typedef struct {

@@ -137,9 +137,9 @@ __global__ __launch_bounds__(norm_threads(TPR)) void norm_kernel(NormParams p) {
       }
     const unsigned top = row_max<TPR>(m, part_max);
     const bool finite = top < 0x7f800000u;
-    // below 2^-100 a row counts as zeros
-    const bool zero = top < 0x0d800000u;
-    const float scale = zero ? 0.0f : __uint_as_float(top) / 127.0f;
+    // 0 for a row of zeros and where binary32 holds no such number; a subnormal scale is rounded so coarsely
+    // that a row's largest values may pass 127 times it
+    const float scale = __uint_as_float(top) / 127.0f;
     if (t == 0) p.scale[row] = finite ? scale : __uint_as_float(0x7fc00000u);
     int8_t *const q = p.q + row * p.q_stride;
 #pragma unroll
@@ -147,7 +147,10 @@ __global__ __launch_bounds__(norm_threads(TPR)) void norm_kernel(NormParams p) {
       const int at = (j * TPR + t) * VE;
       typename Raw<int8_t, VE>::type c;
 #pragma unroll
-      for (int i = 0; i < VE; ++i) c[i] = finite && !zero ? (int8_t)(int)rintf(h[j][i] / scale) : (int8_t)0;
+      for (int i = 0; i < VE; ++i) {
+        const float v = fminf(fmaxf(rintf(h[j][i] / scale), -127.0f), 127.0f);
+        c[i] = finite && scale > 0.0f ? (int8_t)(int)v : (int8_t)0;
+      }
       if (at + VE <= dim) {
         *(typename Raw<int8_t, VE>::type *)(q + at) = c;
       } else {

@@ -100,3 +100,21 @@ def test_codes_are_the_division_of_the_rows_by_their_scale(rows, dim):
     got = edge.norm(x, w, residual=r, bits8=True, out16=True)
     want = torch.round(got["out"].cpu() / got["scale"].cpu()[:, None])
     assert torch.equal(got["q"].cpu().float(), want), (got["q"].cpu().float() != want).sum()
+
+
+@pytest.mark.parametrize("exponent", [-95, -105, -118, -126, -133, -140])
+@pytest.mark.parametrize("rows,dim", [(5, 300), (4, 3000), (3, 16384)])
+def test_rows_of_the_smallest_values_are_no_rows_of_zeros(rows, dim, exponent):
+    """The scale is max / 127 as far as binary32 has it (a subnormal one in the end), codes stay within 127."""
+    x, _, w = inputs(rows, dim, F32, False, seed=dim)
+    w = torch.full_like(w, 2.0 ** exponent)
+    got = {k: v.cpu() for k, v in edge.norm(x, w, bits8=True, out16=True).items() if v is not None}
+    top = got["out"].abs().amax(dim=1)
+    assert (got["scale"] > 0).all() and torch.equal(got["scale"], top / 127)
+    want = torch.round(got["out"] / got["scale"][:, None]).clamp(-127, 127)
+    assert torch.equal(got["q"].float(), want) and (got["q"].abs() > 0).any(dim=1).all()
+
+
+def test_a_scale_that_binary32_does_not_have_is_a_row_of_zeros():
+    got = edge.norm(torch.ones(2, 100, device="cuda"), torch.full((100,), 2.0 ** -147, device="cuda"), bits8=True)
+    assert (got["scale"] == 0).all() and (got["q"] == 0).all()
