@@ -54,7 +54,8 @@ typedef enum { JDOB_EDGE_BF16 = 0, JDOB_EDGE_F16 = 1, JDOB_EDGE_F32 = 2 } jdob_e
 #define JDOB_EDGE_MAX_SEQUENCES 65535
 
 /* h = x + residual;  y_i = h_i * weight_i / sqrt(mean(h^2) + eps).
- * Sums are binary32 and start from the unrounded h.  8-bit output:
+ * Sums are binary32 and start from the unrounded h; where the squares leave
+ * binary32 the row is scaled by a power of two first.  8-bit output:
  * scale = max|y| / 127, q_i = y_i / scale (y before it is rounded to dtype,
  * a binary32 division) rounded to the nearest integer (to even) in
  * [-127, 127], so that q_i * scale stands for y_i (coarser below

@@ -57,7 +57,7 @@ __global__ __launch_bounds__(norm_threads(TPR)) void norm_kernel(NormParams p) {
   constexpr int VE = 16 / (int)sizeof(T);
   constexpr int RPB = norm_threads(TPR) / TPR;
   __shared__ float part_sum[norm_threads(TPR) / WAVE];
-  __shared__ unsigned part_max[norm_threads(TPR) / WAVE];
+  __shared__ unsigned part_max[norm_threads(TPR) / WAVE], part_peak[norm_threads(TPR) / WAVE];
   const int row = blockIdx.x * RPB + threadIdx.x / TPR, t = threadIdx.x % TPR;
   if (row >= p.rows) return;  // whole waves, and with TPR > 64 whole workgroups
   const int dim = p.dim;
@@ -105,7 +105,34 @@ __global__ __launch_bounds__(norm_threads(TPR)) void norm_kernel(NormParams p) {
   for (int j = 0; j < NV; ++j)
 #pragma unroll
     for (int i = 0; i < VE; ++i) ss += h[j][i] * h[j][i];
-  const float rms = 1.0f / sqrtf(row_sum<TPR>(ss, part_sum) / (float)dim + p.eps);
+  const float mean = row_sum<TPR>(ss, part_sum) / (float)dim + p.eps;
+  float rms = 1.0f / sqrtf(mean);
+  if (!(mean > 0x1p-90f && mean < INFINITY)) {
+    // Squares that left binary32 (or none: zeros, a NaN, an infinity): once more with the row scaled by a
+    // power of two that brings its largest value to [1, 2).  All threads of the row are here.
+    unsigned m = 0;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int i = 0; i < VE; ++i) {
+        const unsigned a = __float_as_uint(h[j][i]) & 0x7fffffffu;
+        m = a > m ? a : m;
+      }
+    m = row_max<TPR>(m, part_peak);
+    if (m > 0 && m < 0x7f800000u) {
+      const int e = -ilogbf(__uint_as_float(m));
+      ss = 0.0f;
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int i = 0; i < VE; ++i) {
+          h[j][i] = ldexpf(h[j][i], e);
+          ss += h[j][i] * h[j][i];
+        }
+      // (eps scaled alike may be no binary32 number)
+      rms = (float)(1.0 / sqrt((double)row_sum<TPR>(ss, part_sum) / dim + ldexp((double)p.eps, 2 * e)));
+    }
+  }
 #pragma unroll
   for (int j = 0; j < NV; ++j)
 #pragma unroll

@@ -118,3 +118,16 @@ def test_rows_of_the_smallest_values_are_no_rows_of_zeros(rows, dim, exponent):
 def test_a_scale_that_binary32_does_not_have_is_a_row_of_zeros():
     got = edge.norm(torch.ones(2, 100, device="cuda"), torch.full((100,), 2.0 ** -147, device="cuda"), bits8=True)
     assert (got["scale"] == 0).all() and (got["q"] == 0).all()
+
+
+@pytest.mark.parametrize("dtype,size,eps", [(BF16, 1e25, 1e-5), (F32, 1e37, 1e-5), (F32, 2e19, 1.0), (BF16, 1e-25, 0.0),
+                                            (F32, 1e-36, 0.0), (F32, 3e-20, 1e-38), (F32, 1e-30, 1e-38)])
+@pytest.mark.parametrize("rows,dim", [(5, 100), (1500, 1000), (6, 4096), (3, 16384)])
+def test_rows_whose_squares_leave_binary32(rows, dim, dtype, size, eps):
+    """Rows so large or small that the sum of their squares is no binary32 number, between ordinary ones."""
+    x, r, w = inputs(rows, dim, dtype, True, seed=rows + dim)
+    x[::2] *= size
+    r[::2] *= size
+    for residual in (None, r):
+        got = edge.norm(x, w, eps=eps, residual=residual, bits8=True, out16=True)
+        check(got, x, w, eps, residual, (rows, dim, dtype, size, eps, residual is not None))
