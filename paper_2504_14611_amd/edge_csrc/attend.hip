@@ -138,7 +138,7 @@ __device__ inline void stage(char *dst, const T *base, int64_t stride, int64_t f
 // The running state of 32 rows in a wave: lane l and l + 32 hold row l % 32.
 template <int DP>
 struct State {
-  float top, sum;           // the maximum so far (log2 units), this half's sum
+  float top, sum;           // the maximum so far (of q.k; -inf: nothing seen yet), this half's sum
   f32x16 out[DP / 32];      // out[d][e]: column 32 d + 8 (e / 4) + 4 half + e % 4
 
   __device__ void clear();
@@ -157,19 +157,22 @@ __device__ inline float other_half(float x) {
   return __uint_as_float(threadIdx.x % WAVE < 32 ? both[1] : both[0]);
 }
 
-// The maximum starts below every score that binary32 arithmetic gives real rows, and above -inf, so
-// that masked scores (-inf) give exp2(-inf) = 0 also where nothing has been seen yet.
-constexpr float LOWEST = -1e30f;
+// What a row's scores are taken relative to: its maximum, or 0 where it has seen nothing (masked scores
+// are -inf, and -inf - -inf would be NaN).
+__device__ inline float base_of(float top) { return top == -INFINITY ? 0.0f : top; }
 
 template <int DP>
 __device__ void State<DP>::clear() {
-  top = LOWEST;
+  top = -INFINITY;
   sum = 0.0f;
 #pragma unroll
   for (int d = 0; d < DP / 32; ++d) out[d] = (f32x16){};
 }
 
 constexpr float GROWTH = 8.0f;  // the maximum may lag behind by this much (p up to 2^8) before out is rescaled
+// Up to here (log2 units) sc * scale - top * scale may be formed with one rounding of top * scale: it puts p
+// off by at most a factor of two, the same for all of a row, which its sum takes back.
+constexpr float NEAR = 0x1p24f;
 
 // Scores of 32 rows with KT * 32 staged keys, softmax, and the values' sums.  The lane's row sees the
 // tile's keys 0 .. sees; MASKED: some key of the tile lies behind that for some row.
@@ -226,28 +229,41 @@ __device__ inline void attend_tile(State<DP> &s, const typename Mma<T>::frag (&q
       for (int e = 0; e < 16; ++e)
         sc[t][e] = t * 32 + 8 * (e / 4) + 4 * half + e % 4 <= sees ? sc[t][e] : -INFINITY;
   }
-  float top = LOWEST;
+  float top = -INFINITY;
 #pragma unroll
   for (int t = 0; t < KT; ++t)
 #pragma unroll
     for (int e = 0; e < 16; ++e) top = fmaxf(top, sc[t][e]);
-  top = fmaxf(top, other_half(top)) * scale;
-  if (__any(top > s.top + GROWTH)) {
+  top = fmaxf(top, other_half(top));
+  // (false where neither has seen anything: -inf - -inf is NaN)
+  const bool grows = (top - s.top) * scale > GROWTH;
+  if (__any(grows)) {
     // a row's own scores decide for it: what other rows of the wave see does not change its roundings
-    const float next = top > s.top + GROWTH ? top : s.top;
+    const float next = grows ? top : s.top;
     // (nothing has been seen yet: out is zero, or holds infinities that are to stay)
-    const float f = s.top == LOWEST ? 1.0f : __builtin_amdgcn_exp2f(s.top - next);
+    const float f = s.top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((s.top - next) * scale);
     s.top = next;
     s.sum *= f;
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d) s.out[d] *= f;
+  }
+  float times = scale, base = base_of(s.top) * scale;
+  const bool far = !(fabsf(base) < NEAR);
+  if (__any(far)) {
+    // the difference first, again row by row
+#pragma unroll
+    for (int t = 0; t < KT; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) sc[t][e] = far ? (sc[t][e] - s.top) * scale : sc[t][e];
+    times = far ? 1.0f : times;
+    base = far ? 0.0f : base;
   }
   frag p[KT * 2];
 #pragma unroll
   for (int t = 0; t < KT; ++t)
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      const float x = __builtin_amdgcn_exp2f(sc[t][e] * scale - s.top);
+      const float x = __builtin_amdgcn_exp2f(sc[t][e] * times - base);
       s.sum += x;
       p[t * 2 + e / 8][e % 8] = (T)x;
     }
@@ -471,9 +487,9 @@ constexpr int FEW_WAVES = 2, FEW_COLUMNS = 32, FEW_KEYS = 32;
 
 // A workgroup takes 32 columns (rows times the heads of one key head) and `each` keys of them; its
 // waves take 32 keys in turn, each staged in the wave's own two buffers, so that no wave waits for
-// another before the end.
+// another before the end.  (Heads to 64 leave registers for two waves a SIMD, if the compiler is told to.)
 template <typename T, int DP, bool DIRECT>
-__global__ __launch_bounds__(FEW_WAVES *WAVE) void few_kernel(AttendParams p) {
+__global__ __launch_bounds__(FEW_WAVES *WAVE, DP == 64 ? 2 : 1) void few_kernel(AttendParams p) {
   typedef typename Mma<T>::frag frag;
   constexpr int THREADS = FEW_WAVES * WAVE, BYTES = FEW_KEYS * DP * 2, CORNER = 4 * BYTES;
   constexpr int LOADS = 2 * BYTES / (WAVE * 16), MIX = FEW_WAVES * 32 * (DP + 4) * 4;
@@ -547,12 +563,13 @@ __global__ __launch_bounds__(FEW_WAVES *WAVE) void few_kernel(AttendParams p) {
     sums[wave][l32] = s.sum;
   }
   __syncthreads();  // also: the staged keys have been read
-  float top = LOWEST, sum = 0.0f;
+  float top = -INFINITY, sum = 0.0f;
 #pragma unroll
   for (int w = 0; w < FEW_WAVES; ++w) top = fmaxf(top, tops[w][l32]);
+  const float base = base_of(top);
 #pragma unroll
-  for (int w = 0; w < FEW_WAVES; ++w) sum += sums[w][l32] * __builtin_amdgcn_exp2f(tops[w][l32] - top);
-  const float f = __builtin_amdgcn_exp2f(s.top - top);
+  for (int w = 0; w < FEW_WAVES; ++w) sum += sums[w][l32] * __builtin_amdgcn_exp2f((tops[w][l32] - base) * p.scale);
+  const float f = __builtin_amdgcn_exp2f((s.top - base) * p.scale);
   float *const mix = (float *)room;  // [wave][column][DP + 4]
 #pragma unroll
   for (int d = 0; d < DP / 32; ++d)
@@ -601,18 +618,19 @@ __global__ __launch_bounds__(JOIN_THREADS) void join_kernel(AttendParams p) {
   const int used = q.keys > 0 ? (q.keys - 1) / p.each + 1 : 1, splits = used < p.splits ? used : p.splits;
   const int t = threadIdx.x, lane = t % WAVE;
   // every wave for itself: the maximum, the weights, their sum
-  float tops[MAX_SPLITS / WAVE], top = LOWEST, sum = 0.0f;
+  float tops[MAX_SPLITS / WAVE], top = -INFINITY, sum = 0.0f;
 #pragma unroll
   for (int i = 0; i < MAX_SPLITS / WAVE; ++i) {
-    tops[i] = i * WAVE + lane < splits ? part[(i * WAVE + lane) * step + p.dim] : LOWEST;
+    tops[i] = i * WAVE + lane < splits ? part[(i * WAVE + lane) * step + p.dim] : -INFINITY;
     top = fmaxf(top, tops[i]);
   }
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+  const float base = base_of(top);
 #pragma unroll
   for (int i = 0; i < MAX_SPLITS / WAVE; ++i)
     if (i * WAVE + lane < splits) {
-      const float w = __builtin_amdgcn_exp2f(tops[i] - top);
+      const float w = __builtin_amdgcn_exp2f((tops[i] - base) * p.scale);
       sum += w * part[(i * WAVE + lane) * step + p.dim + 1];
       if (t < WAVE) weight[i * WAVE + lane] = w;
     }

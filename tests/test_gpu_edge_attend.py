@@ -185,3 +185,50 @@ def test_nothing_to_do():
     assert edge.attend(**s).shape == (0, 2, 64)
     s = inputs([0, 0], [4, 0], 2, 1, 64, BF16)
     assert edge.attend(**s).shape == (0, 2, 64)
+
+
+def far_scores(kind, keys, dim, dtype):
+    """Keys whose scores with the query of `far_query` are far from zero and equal, or so far apart that one wins:
+    the weights are 0 or 1 / n exactly, in 64 bits as in any other."""
+    j = torch.arange(keys, device="cuda", dtype=torch.float64)[:, None].expand(keys, dim)
+    low = torch.finfo(dtype).min
+    return {"lowest": j * 0 + low, "highest": j * 0 - low, "first": -(j + 1) * 2.0 ** 100, "last": (j + 1) * 2.0 ** 100,
+            "lowest, then zeros": torch.where(j < keys // 2, low, 0.0), "zeros, then lowest": torch.where(j < keys // 2, 0.0, low),
+            "large": j * 0 + 60000.0, "large, then larger": torch.where(j < keys // 2, 50000.0, 60000.0),
+            "large and negative": j * 0 - 60000.0}[kind].to(dtype)
+
+
+@pytest.mark.parametrize("new,keys", [([1], [300]), ([5, 2], [70, 2]), ([1], [3000]), ([100], [130]), ([200, 140], [200, 100]),
+                                      ([300], [700])])
+@pytest.mark.parametrize("kind,dtype", [("lowest", BF16), ("highest", BF16), ("first", BF16), ("last", BF16),
+                                        ("lowest, then zeros", BF16), ("zeros, then lowest", BF16), ("lowest", F16),
+                                        ("large", F16), ("large, then larger", F16), ("large and negative", F16)])
+def test_scores_far_from_zero(new, keys, kind, dtype):
+    """Scores that binary32 holds are scores, however far from zero: a row's weights are their softmax."""
+    s = inputs(new, keys, 4, 2, 64, dtype, seed=sum(keys))
+    other = edge.attend(**s)
+    for first, m in zip(s["key_start"].tolist(), keys):
+        s["k"][first:first + m, 0] = far_scores(kind, m, 64, dtype)
+    s["q"][:, :2] = 60000.0 if dtype == F16 else 2.0 ** -10
+    for scale in (None, 0.01, 7.3):
+        got = edge.attend(**s, scale=scale)
+        ref = {k: s[k] for k in ("q", "k", "v", "query_start", "key_start", "key_count")}
+        out, size, _ = model.attend(**ref, scale=64 ** -0.5 if scale is None else scale)
+        off = (got.double() - out).abs() - model.attend_bound(out, size, torch.zeros_like(out[:, :, 0]), 64, max(keys), dtype)
+        assert not got.isnan().any() and off[:, :2].max() <= 0, (scale, off[:, :2].max())
+        if scale is None:  # the other key head's heads are what they were
+            assert torch.equal(got[:, 2:], other[:, 2:])
+
+
+@pytest.mark.parametrize("new,keys", [(1, 300), (100, 130), (300, 700)])
+def test_rows_far_from_zero_beside_ordinary_ones(new, keys):
+    """A row's roundings do not depend on the rows beside it, large scores among them."""
+    s = inputs([new], [keys], 4, 2, 64, F16, seed=5)
+    s["k"][s["key_start"][0]:][:keys, :, :8] = 30000.0
+    s["q"][:, :, :8] = 0
+    plain = check(s, "ordinary")
+    s["q"][::3, ::2, :8] = 60000.0
+    got = edge.attend(**s)
+    keep = torch.ones(got.shape[:2], dtype=torch.bool, device="cuda")
+    keep[::3, ::2] = False
+    assert torch.equal(got[keep], plain[keep]) and not got.isnan().any()
