@@ -5,9 +5,9 @@ addition, in the rows' type or in 8 bits with scales), `project` (the projection
 row's low-rank adapter) and `attend` (causal attention of packed sequences of different lengths).
 
 Argument marshalling only, like paper_2504_14611_amd.jdob: the work runs in the HIP kernels of the library, and
-there is no fallback.  Tensors are device tensors; outputs and workspaces that the caller does not pass are
-allocated by torch on the stream that the call runs on.  `stream` is a raw HIP stream handle (default: torch's
-current stream of the tensors' device).  Refused arguments raise jdob.JdobError with the library's status code.
+there is no fallback.  Tensors are device tensors (others are refused); outputs and workspaces that the caller does
+not pass are allocated by torch on the stream that the call runs on.  `stream` is a raw HIP stream handle (default:
+torch's current stream of the tensors' device).  Refused arguments raise jdob.JdobError with the library's status code.
 """
 
 from __future__ import annotations
@@ -78,15 +78,16 @@ def load():
     return _lib
 
 
-_CODES = {torch.bfloat16: EDGE_BF16, torch.float16: EDGE_F16, torch.float32: EDGE_F32}
+_CODES16 = {torch.bfloat16: EDGE_BF16, torch.float16: EDGE_F16}
+_CODES = {**_CODES16, torch.float32: EDGE_F32}
 
 
 def _refuse(where: str, why: str, code: int = jdob.JDOB_ERR_INVALID_ARG):
     raise jdob.JdobError(code, f"{where}: {why}")
 
 
-def _dtype(t, where: str) -> int:
-    code = _CODES.get(t)
+def _dtype(t, where: str, codes=_CODES16) -> int:
+    code = codes.get(t)
     if code is None:
         _refuse(where, f"type {t}", jdob.JDOB_ERR_UNSUPPORTED)
     return code
@@ -115,11 +116,12 @@ def _row_stride(t, width: int) -> int:
     return stride if stride > width or t.shape[0] > 1 else width
 
 
-def _enter(device, stream):
+def _enter(device, stream, where: str):
     """The raw stream of a call on `device`, and the context (or None) in which its outputs are allocated and its
-    kernels launched: `stream`'s, or the device's where it is not torch's current one."""
+    kernels launched: `stream`'s, or the device's where it is not torch's current one.  Kernels that are given
+    memory of the host would fault."""
     if device.type != "cuda":
-        return stream, None
+        _refuse(where, f"tensors on {device}, expected a GPU's")
     if stream is not None:
         return stream, torch.cuda.stream(torch.cuda.ExternalStream(stream, device=device))
     index = device.index
@@ -142,12 +144,13 @@ def norm(x, weight, eps: float = 1e-6, residual=None, bits8: bool = False, out16
         out16 = not bits8
     if not (bits8 or out16):
         _refuse(where, "neither output is asked for")
-    a = NormArgs(rows, dim, _dtype(dtype, where), eps, _array(x, where, "x", shape, dtype, dev), _row_stride(x, dim))
+    a = NormArgs(rows, dim, _dtype(dtype, where, _CODES), eps, _array(x, where, "x", shape, dtype, dev),
+                 _row_stride(x, dim))
     a.weight = _dense(weight, where, "weight", (dim,), dtype, dev)
     if residual is not None:
         a.residual = _array(residual, where, "residual", shape, dtype, dev)
         a.residual_stride = _row_stride(residual, dim)
-    handle, context = _enter(dev, stream)
+    handle, context = _enter(dev, stream, where)
     if context is not None:
         with context:
             return _norm(a, where, x, bits8, out16, into, handle)
@@ -232,7 +235,7 @@ def project(x, weight, x_scale=None, weight_scale=None, adapters: Optional[dict]
         a.row_adapter = _dense(row_adapter, where, "row_adapter", (rows,), torch.int32, dev)
         if rank is not None:
             a.rank = _dense(rank, where, "rank", (n,), torch.int32, dev)
-    handle, context = _enter(dev, stream)
+    handle, context = _enter(dev, stream, where)
     if context is not None:
         with context:
             return _project(a, where, dtype, dev, out, workspace, handle)
@@ -282,6 +285,8 @@ def attend(q, k, v, query_start, key_start, key_count, scale: Optional[float] = 
     rows, h, d = shape
     if rows > MAX_ROWS:
         _refuse(where, f"{rows} rows", jdob.JDOB_ERR_UNSUPPORTED)
+    if d % 8 or d > MAX_HEAD_DIM:
+        _refuse(where, f"heads of {d}", jdob.JDOB_ERR_UNSUPPORTED)
     key_rows, g = k.shape[:2]
     n = key_count.shape[0]
     a = AttendArgs(n, h, g, d, _dtype(dtype, where), rows if max_queries is None else max_queries,
@@ -292,7 +297,7 @@ def attend(q, k, v, query_start, key_start, key_count, scale: Optional[float] = 
                    _dense(query_start, where, "query_start", (n + 1,), torch.int32, dev),
                    _dense(key_start, where, "key_start", (n,), torch.int64, dev),
                    _dense(key_count, where, "key_count", (n,), torch.int32, dev))
-    handle, context = _enter(dev, stream)
+    handle, context = _enter(dev, stream, where)
     if context is not None:
         with context:
             return _attend(a, where, shape, dtype, dev, out, workspace, handle)

@@ -186,3 +186,19 @@ def test_binding_refuses_tensors_that_do_not_fit():
     refused(INVALID, edge.attend, q, k, k, at, first, count, scale=-1.0)
     refused(UNSUPPORTED, edge.attend, q.float(), k.float(), k.float(), at, first, count)
     refused(UNSUPPORTED, edge.attend, q[:, :, :12], k[:, :, :12], k[:, :, :12], at, first, count)
+
+
+def test_binding_refuses_tensors_on_the_host():
+    """Tensors that fit but for where they are: a kernel would be given the host's memory."""
+    x, w, m = (torch.zeros(s, dtype=torch.bfloat16) for s in ((3, 8), (8,), (5, 8)))
+    assert "cpu" in refused(INVALID, edge.norm, x, w)
+    refused(INVALID, edge.norm, x, w, residual=x, bits8=True, into={"sum": x}, stream=0)
+    refused(INVALID, edge.norm, x[:0], w)
+    a = {"down": torch.zeros(2, 4, 8, dtype=torch.bfloat16), "up": torch.zeros(2, 5, 4, dtype=torch.bfloat16),
+         "gain": torch.ones(2)}
+    assert "cpu" in refused(INVALID, edge.project, x, m)
+    refused(INVALID, edge.project, x, m, adapters=a, row_adapter=torch.zeros(3, dtype=torch.int32), stream=0)
+    q, k = torch.zeros(3, 4, 16, dtype=torch.float16), torch.zeros(9, 2, 16, dtype=torch.float16)
+    at, first, count = (torch.tensor(v, dtype=t) for v, t in (([0, 3], torch.int32), ([0], torch.int64), ([9], torch.int32)))
+    assert "cpu" in refused(INVALID, edge.attend, q, k, k, at, first, count)
+    refused(INVALID, edge.attend, *(t.to("meta") for t in (q, k, k, at, first, count)))
