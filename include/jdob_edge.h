@@ -87,7 +87,7 @@ int jdob_edge_norm(const jdob_edge_norm_args *a, void *hip_stream);
 /* out = x W^T + gain_a ((x A_a^T) B_a^T), a = row_adapter[row].
  * x and W are of dtype (16 bits), or both 8-bit integers that stand for
  * x * x_scale[row] and W * weight_scale[column]; the adapters are of dtype
- * always.  Sums are binary32 (8-bit products: 32-bit integers, exact for
+ * always.  Sums are binary32 (8-bit products: integers, exact for any codes,
  * in_dim <= 131072); the low-rank rows x A_a^T are kept in binary32 in the
  * workspace and multiplied as two 16-bit parts (bfloat16: 16 bits of
  * mantissa, binary16: 22); with JDOB_EDGE_F16 they must stay below 65504.

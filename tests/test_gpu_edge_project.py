@@ -151,3 +151,16 @@ def test_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("rows,out", [(1, 1), (20, 40), (64, 17), (70, 70), (300, 300)])
+@pytest.mark.parametrize("shift", [0, 1])
+def test_the_largest_eight_bit_sum(rows, out, shift):
+    """131072 products of -128 and -128 are 2^31, one more than 32-bit integers hold; the others are exact beside it."""
+    x, w = (torch.full((n, 131072 + 16), -128, dtype=torch.int8, device="cuda")[:, shift:shift + 131072] for n in (rows, out))
+    x[1::2] = 127
+    x[2::3, 5] = 127
+    one = torch.ones(max(rows, out), device="cuda")
+    got = edge.project(x, w, x_scale=one[:rows] * 2.0 ** -16, weight_scale=one[:out], dtype=BF16)
+    want = x.double() @ w.double().T * 2.0 ** -16
+    assert torch.equal(got, want.float().to(BF16))
