@@ -89,8 +89,9 @@ int jdob_edge_norm(const jdob_edge_norm_args *a, void *hip_stream);
  * x * x_scale[row] and W * weight_scale[column]; the adapters are of dtype
  * always.  Sums are binary32 (8-bit products: integers, exact for any codes,
  * in_dim <= 131072); the low-rank rows x A_a^T are kept in binary32 in the
- * workspace and multiplied as two 16-bit parts (bfloat16: 16 bits of
- * mantissa, binary16: 22); with JDOB_EDGE_F16 they must stay below 65504.
+ * workspace or, from 65 rows on, as two 16-bit parts (16 bits of mantissa with
+ * bfloat16; 22 with binary16, whatever their size, for ranks that are not more
+ * than 2^17 times smaller than the largest of 16).
  * An adapter with a rank below max_rank uses the first `rank` rows of A and
  * columns of B; what lies behind them is not used.                          */
 typedef struct {

@@ -29,8 +29,12 @@ struct ProjectParams {
   const int *rank, *row_adapter;
   // The low-rank rows, gain and scales applied, zeros behind the adapter's rank; slabs = ranks / 32.
   // stream_kernel: binary32 [rows][32 slabs].  tile_kernel: [slab][rows][64] of dtype, the rows' 32
-  // values rounded, then what the rounding left of each.
+  // values rounded, then what the rounding left of each.  binary16 holds neither large values nor what is
+  // left of small ones: there 16 ranks' values of a row are divided by a power of two that brings the
+  // largest of them to [2^14, 2^15), v_scale [slab][rows][2] (so 22 bits are left of any that is not more
+  // than 2^17 times smaller than the largest).
   void *v;
+  float *v_scale;
   int slabs, split;                // split: v is in two parts
   void *out;
   int64_t out_stride;
@@ -285,11 +289,23 @@ __global__ __launch_bounds__(DOWN_WAVES *WAVE) void down_kernel(ProjectParams p)
         for (int i = 0; i < 4; ++i) s[i] = r + i < rank ? s[i] : 0.0f;
         if (p.split) {
           T *const dst = (T *)p.v + ((int64_t)(r / 32) * p.rows + row) * 64 + r % 32;
+          if constexpr (__is_same(T, _Float16)) {
+            // the lanes that hold the row's other ranks of these 16 are here, too
+            float top = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) top = fmaxf(top, fabsf(s[i]) < INFINITY ? fabsf(s[i]) : 0.0f);
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const int e = __builtin_amdgcn_frexp_expf(top) - 15, down_by = e < -126 ? -126 : e;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[i] = ldexpf(s[i], -down_by);
+            if (q == 0) p.v_scale[((int64_t)(r / 32) * p.rows + row) * 2 + r / 16 % 2] = ldexpf(1.0f, down_by);
+          }
           float high[4], low[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             high[i] = (float)(T)s[i];
-            low[i] = s[i] - high[i];
+            low[i] = fabsf(high[i]) < INFINITY ? s[i] - high[i] : 0.0f;
           }
           store_f32<T, 4>(dst, high);
           store_f32<T, 4>(dst + 32, low);
@@ -540,7 +556,8 @@ template <typename T, bool X8, bool DIRECT, int BM, int BN, int WM, int WN, int 
 __global__ __launch_bounds__(WM *WN *WAVE, 2) void tile_kernel(ProjectParams p) {
   typedef Tile<T, X8, DIRECT, BM, BN, WM, WN, STAGES> K;
   typedef typename Mma<T>::frag frag;
-  constexpr bool SMALL = K::FM * K::FN == 1;
+  constexpr bool SMALL = K::FM * K::FN == 1, SCALED = __is_same(T, _Float16);
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
   __shared__ __align__(16) char room[K::ROOM];
   __shared__ int ids[BM], list[BM], listed;
   const int lane = threadIdx.x % WAVE, wave = wave_index();
@@ -761,6 +778,16 @@ __global__ __launch_bounds__(WM *WN *WAVE, 2) void tile_kernel(ProjectParams p) 
     }
   }
   for (int n = 0; n < behind; ++n) {
+    f32x2 times[K::FM];  // the powers of two that ranks 0-15 and 16-31 of the slab were divided by
+    if constexpr (SCALED) {
+#pragma unroll
+      for (int i = 0; i < K::FM; ++i) {
+        const int row = row0 + (wm * K::FM + i) * 32 + l32;
+        times[i] = ((const f32x2 *)p.v_scale)[(int64_t)(n % p.slabs) * p.rows + (row < p.rows ? row : p.rows - 1)];
+      }
+#pragma unroll
+      for (int i = 0; i < K::FM; ++i) asm volatile("" : "+v"(times[i]));  // here, before further loads are under way
+    }
     if (SMALL || n > 0) {
       wait_loads<0>();
       barrier();
@@ -778,11 +805,21 @@ __global__ __launch_bounds__(WM *WN *WAVE, 2) void tile_kernel(ProjectParams p) 
       for (int k = 0; k < 4; ++k) v[k] = *(const frag *)(buf + tile_spot(r, k * 2 + half));
 #pragma unroll
       for (int j = 0; j < K::FN; ++j) {
-        f32x16 more = {};
+        auto up = [&](int k) { return *(const frag *)(buf + BM * SLICE + tile_spot((wn * K::FN + j) * 32 + l32, k * 2 + half)); };
+        if constexpr (SCALED) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-          more = Mma<T>::m32(*(const frag *)(buf + BM * SLICE + tile_spot((wn * K::FN + j) * 32 + l32, k * 2 + half)), v[k], more);
-        if (mine) sum[i][j] += more;
+          for (int k = 0; k < 2; ++k) {  // 16 ranks: the rounded values, and what the rounding left
+            f32x16 more = {};
+            more = Mma<T>::m32(up(k), v[k], more);
+            more = Mma<T>::m32(up(k + 2), v[k + 2], more);
+            if (mine) sum[i][j] += more * times[i][k];
+          }
+        } else {
+          f32x16 more = {};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) more = Mma<T>::m32(up(k), v[k], more);
+          if (mine) sum[i][j] += more;
+        }
       }
     }
   }
@@ -919,19 +956,21 @@ extern "C" int64_t jdob_edge_project_workspace(const jdob_edge_project_args *a) 
   using namespace edge;
   if (project_check(a, true) != JDOB_OK) return -1;
   if (a->num_adapters == 0 || a->rows == 0) return 0;
-  // 32 ranks of a row: binary32, or two 16-bit parts
-  return (int64_t)a->rows * ((a->max_rank + 31) / 32) * 128;
+  // 32 ranks of a row: binary32, or two 16-bit parts; two scales
+  return (int64_t)a->rows * ((a->max_rank + 31) / 32) * (a->dtype == JDOB_EDGE_F16 ? 136 : 128);
 }
 
 extern "C" int jdob_edge_project(const jdob_edge_project_args *a, void *hip_stream) {
   using namespace edge;
   const int code = project_check(a, false);
   if (code != JDOB_OK || a->rows == 0) return code;
-  const int size = a->bits8 ? 1 : 2;
+  const int size = a->bits8 ? 1 : 2, slabs = (a->max_rank + 31) / 32;
+  const bool split = a->rows > STREAM_ROWS && !rowwise(a->rows, a->num_adapters);
   const ProjectParams p = {a->rows, a->in_dim, a->out_dim, (const char *)a->x, (const char *)a->weight,
                      a->x_stride * size, a->weight_stride * size, a->x_scale, a->weight_scale,
                      a->num_adapters, a->max_rank, a->down, a->up, a->gain, a->rank,
-                     a->row_adapter, a->workspace, (a->max_rank + 31) / 32, a->rows > STREAM_ROWS && !rowwise(a->rows, a->num_adapters), a->out, a->out_stride};
+                     a->row_adapter, a->workspace, (float *)((char *)a->workspace + (int64_t)a->rows * slabs * 128),
+                     slabs, split, a->out, a->out_stride};
   hipStream_t stream = (hipStream_t)hip_stream;
   if (a->dtype == JDOB_EDGE_BF16)
     return a->bits8 ? project<__bf16, true>(p, stream) : project<__bf16, false>(p, stream);

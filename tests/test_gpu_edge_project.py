@@ -164,3 +164,20 @@ def test_the_largest_eight_bit_sum(rows, out, shift):
     got = edge.project(x, w, x_scale=one[:rows] * 2.0 ** -16, weight_scale=one[:out], dtype=BF16)
     want = x.double() @ w.double().T * 2.0 ** -16
     assert torch.equal(got, want.float().to(BF16))
+
+
+@pytest.mark.parametrize("x,down,up", [(100.0, 100.0, 2.0 ** -14), (1e4, 3e3, 2.0 ** -24), (2.0 ** -9, 2.0 ** -10, 2.0 ** 13),
+                                       (2.0 ** -6, 2.0 ** -8, 2.0 ** 10), (2.0 ** -12, 2.0 ** -13, 2.0 ** 13)])
+@pytest.mark.parametrize("rows,i,o,n", [(40, 128, 96, 3), (200, 128, 96, 3), (300, 1000, 1111, 5), (100, 128, 96, 40),
+                                        (2055, 328, 4100, 6)])
+def test_low_rank_rows_of_any_size(rows, i, o, n, x, down, up):
+    """binary16 low-rank rows x A^T above 65504 and far below 1, of many rows as of few."""
+    s = inputs(rows, i, o, F16, False, n, 40, seed=rows)
+    s["adapters"]["rank"] = torch.tensor([40, 17, 33][:n] + [40] * (n - 3), dtype=torch.int32, device="cuda")
+    s["x"].mul_(x)
+    s["weight"].mul_(min(1.0, 1 / x))
+    s["adapters"]["down"].mul_(down)
+    s["adapters"]["up"].normal_().mul_(up)
+    s["adapters"]["down"][:, 3] *= 2.0 ** -6   # ranks of different sizes beside each other
+    got = check(s)
+    assert got.isfinite().all()
