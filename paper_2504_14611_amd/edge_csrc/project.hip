@@ -82,10 +82,9 @@ struct Main<T, true> {
   }
 };
 
-// A sum of products as binary32.  131072 products of two codes are at most 2^31 (all of them -128), which
-// wraps around to -2^31; no sum is as low as that itself.
-__device__ inline float as_f32(float sum) { return sum; }
-__device__ inline float as_f32(int sum) { return sum == INT32_MIN ? 0x1p31f : (float)sum; }
+// 131072 products of two codes are at most 2^31 (all of them -128), which wraps around to -2^31; no sum is as
+// low as that itself, and with fewer products none is as high.
+__device__ inline bool may_wrap(const ProjectParams &p) { return p.in_dim == 131072; }
 
 template <int N>
 struct Count {
@@ -446,8 +445,11 @@ __global__ __launch_bounds__(WAVES *WAVE) void stream_kernel(ProjectParams p) {
     auto sum = part(0);
 #pragma unroll
     for (int w = 1; w < WAVES; ++w) sum += part(w);
-    float y = as_f32(sum);
-    if constexpr (X8) y *= p.x_scale[row] * p.w_scale[col0 + c];
+    float y = (float)sum;
+    if constexpr (X8) {
+      if (may_wrap(p) && sum == INT32_MIN) y = -y;
+      y *= p.x_scale[row] * p.w_scale[col0 + c];
+    }
     if (p.num_adapters > 0) y += low[e].value();
     ((T *)p.out)[row * p.out_stride + col0 + c] = (T)y;
   }
@@ -770,7 +772,11 @@ __global__ __launch_bounds__(WM *WN *WAVE, 2) void tile_kernel(ProjectParams p) 
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           const int col = col0 + (wn * K::FN + j) * 32 + 8 * (e / 4) + 4 * half + e % 4;
-          sum[i][j][e] = as_f32(acc[i][j][e]) * (xs * p.w_scale[col < p.out_dim ? col : p.out_dim - 1]);
+          sum[i][j][e] = (float)acc[i][j][e] * (xs * p.w_scale[col < p.out_dim ? col : p.out_dim - 1]);
+        }
+        if (may_wrap(p)) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) sum[i][j][e] = acc[i][j][e] == INT32_MIN ? -sum[i][j][e] : sum[i][j][e];
         }
       } else {
         sum[i][j] = acc[i][j];
