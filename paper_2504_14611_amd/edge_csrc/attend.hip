@@ -370,8 +370,8 @@ __global__ __launch_bounds__(PROMPT_WAVES *WAVE, 2) void prompt_kernel(AttendPar
   static_assert(2 * BYTES >= PROMPT_ROWS * DP * 2, "room for the rows");
   const int lane = threadIdx.x % WAVE, wave = wave_index(), l32 = lane % 32, half = lane / 32;
   // Workgroups go to the chip's eight dies in turn: heads that read one key head should share a die's cache.
-  const int kv = blockIdx.x % p.heads % p.kv_heads, head = kv * p.group + blockIdx.x % p.heads / p.kv_heads;
-  const int tile = blockIdx.x / p.heads;
+  const int kv = block_index() % p.heads % p.kv_heads, head = kv * p.group + block_index() % p.heads / p.kv_heads;
+  const int tile = block_index() / p.heads;
   int t;
   Sequence q;
   if (!find_tile(p, tile, &t, &q)) return;
@@ -496,8 +496,9 @@ __global__ __launch_bounds__(FEW_WAVES *WAVE, DP == 64 ? 2 : 1) void few_kernel(
   __shared__ __align__(16) char room[FEW_WAVES * CORNER > MIX ? FEW_WAVES * CORNER : MIX];
   __shared__ float tops[FEW_WAVES][32], sums[FEW_WAVES][32];
   const int lane = threadIdx.x % WAVE, wave = wave_index(), l32 = lane % 32, half = lane / 32;
-  const int kv = blockIdx.x % p.kv_heads, split = blockIdx.x / p.kv_heads % p.splits;
-  const int tile = blockIdx.x / p.kv_heads / p.splits % p.tiles, u = blockIdx.x / p.kv_heads / p.splits / p.tiles;
+  const int kv = block_index() % p.kv_heads, split = block_index() / p.kv_heads % p.splits;
+  const int tile = block_index() / p.kv_heads / p.splits % p.tiles, u = block_index() / p.kv_heads / p.splits / p.tiles;
+  if (u >= p.sequences) return;
   const Sequence q = sequence(p, u);
   const int rows = q.rows < p.max_queries ? q.rows : p.max_queries;
   const int columns = rows * p.group, column = tile * FEW_COLUMNS + l32;
@@ -608,8 +609,9 @@ template <typename T>
 __global__ __launch_bounds__(JOIN_THREADS) void join_kernel(AttendParams p) {
   __shared__ float weight[MAX_SPLITS], mix[8][128];
   const int columns_each = p.max_queries * p.group;
-  const int kv = blockIdx.x % p.kv_heads, col = blockIdx.x / p.kv_heads % columns_each;
-  const int u = blockIdx.x / p.kv_heads / columns_each, tile = col / FEW_COLUMNS;
+  const int kv = block_index() % p.kv_heads, col = block_index() / p.kv_heads % columns_each;
+  const int u = block_index() / p.kv_heads / columns_each, tile = col / FEW_COLUMNS;
+  if (u >= p.sequences) return;
   const Sequence q = sequence(p, u);
   const int rows = q.rows < p.max_queries ? q.rows : p.max_queries;
   if (col >= rows * p.group) return;
@@ -709,17 +711,16 @@ int attend(AttendParams p, bool few, bool direct, hipStream_t stream) {
   if (few) {
     const int64_t groups = (int64_t)p.sequences * p.kv_heads * p.tiles;
     const int64_t columns = (int64_t)p.sequences * p.kv_heads * p.max_queries * p.group;
-    if (groups * p.splits > 0x7fffffff || columns > 0x7fffffff) return JDOB_ERR_UNSUPPORTED;
-    const dim3 grid((unsigned)(groups * p.splits));
-    const int code = direct ? launch(few_kernel<T, DP, true>, grid, FEW_WAVES * WAVE, stream, p)
-                          : launch(few_kernel<T, DP, false>, grid, FEW_WAVES * WAVE, stream, p);
+    if (groups * p.splits > MAX_BLOCKS || columns > MAX_BLOCKS) return JDOB_ERR_UNSUPPORTED;
+    const int code = direct ? launch(few_kernel<T, DP, true>, groups * p.splits, FEW_WAVES * WAVE, stream, p)
+                            : launch(few_kernel<T, DP, false>, groups * p.splits, FEW_WAVES * WAVE, stream, p);
     if (code != JDOB_OK || p.splits == 1) return code;
-    return launch(join_kernel<T>, dim3((unsigned)columns), JOIN_THREADS, stream, p);
+    return launch(join_kernel<T>, columns, JOIN_THREADS, stream, p);
   }
   const int64_t blocks = (int64_t)p.tiles * p.heads;
-  if (blocks > 0x7fffffff) return JDOB_ERR_UNSUPPORTED;
-  return direct ? launch(prompt_kernel<T, DP, true>, dim3((unsigned)blocks), PROMPT_WAVES * WAVE, stream, p)
-              : launch(prompt_kernel<T, DP, false>, dim3((unsigned)blocks), PROMPT_WAVES * WAVE, stream, p);
+  if (blocks > MAX_BLOCKS) return JDOB_ERR_UNSUPPORTED;
+  return direct ? launch(prompt_kernel<T, DP, true>, blocks, PROMPT_WAVES * WAVE, stream, p)
+                : launch(prompt_kernel<T, DP, false>, blocks, PROMPT_WAVES * WAVE, stream, p);
 }
 
 template <typename T>

@@ -98,10 +98,19 @@ __device__ inline void barrier() {
   asm volatile("" ::: "memory");
 }
 
-// Launches a kernel of one parameter struct and returns the status of this launch alone.
+// A dimension of a grid takes fewer than 2^32 threads: more than FOLD workgroups stand in rows of FOLD, and
+// those behind the last one, in the last row, have nothing to do.
+constexpr int FOLD = 1 << 21, MAX_BLOCKS = 0x7fffffff - FOLD;
+
+__device__ inline unsigned block_index() { return blockIdx.y * FOLD + blockIdx.x; }
+
+// Launches a kernel of one parameter struct with `blocks` workgroups, to MAX_BLOCKS, in each of `layers`, and
+// returns the status of this launch alone.
 template <typename P>
-inline int launch(void (*kernel)(P), dim3 grid, int threads, hipStream_t stream, P params) {
+inline int launch(void (*kernel)(P), int64_t blocks, int threads, hipStream_t stream, P params, int layers = 1) {
   void *args[] = {&params};
+  const int64_t rows = (blocks + FOLD - 1) / FOLD;
+  const dim3 grid((unsigned)(rows > 1 ? FOLD : blocks), (unsigned)rows, (unsigned)layers);
   return hipLaunchKernel((const void *)kernel, grid, dim3(threads), args, 0, stream) == hipSuccess
              ? JDOB_OK
              : JDOB_ERR_HIP;

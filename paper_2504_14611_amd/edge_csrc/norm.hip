@@ -58,7 +58,7 @@ __global__ __launch_bounds__(norm_threads(TPR)) void norm_kernel(NormParams p) {
   constexpr int RPB = norm_threads(TPR) / TPR;
   __shared__ float part_sum[norm_threads(TPR) / WAVE];
   __shared__ unsigned part_max[norm_threads(TPR) / WAVE], part_peak[norm_threads(TPR) / WAVE];
-  const int row = blockIdx.x * RPB + threadIdx.x / TPR, t = threadIdx.x % TPR;
+  const int row = (int)block_index() * RPB + threadIdx.x / TPR, t = threadIdx.x % TPR;
   if (row >= p.rows) return;  // whole waves, and with TPR > 64 whole workgroups
   const int dim = p.dim;
   const T *const x = (const T *)p.x + row * p.x_stride;
@@ -192,8 +192,7 @@ __global__ __launch_bounds__(norm_threads(TPR)) void norm_kernel(NormParams p) {
 template <typename T, int TPR, int NV>
 int norm_launch(const NormParams &p, hipStream_t stream) {
   constexpr int RPB = norm_threads(TPR) / TPR;
-  return launch(norm_kernel<T, TPR, NV>, dim3((unsigned)((p.rows + RPB - 1) / RPB)),
-                norm_threads(TPR), stream, p);
+  return launch(norm_kernel<T, TPR, NV>, (p.rows + RPB - 1) / RPB, norm_threads(TPR), stream, p);
 }
 
 template <typename T>

@@ -172,7 +172,7 @@ __device__ inline typename Mma<T>::frag eight(const T *row, int k, int len) {
 constexpr int DOWN_ROWS = 32, DOWN_WAVES = 8;
 
 // A workgroup takes 32 rows, each of its waves one contiguous part of the inner dimension, RC * 16
-// ranks at a time.  Of the adapters among its rows it takes every gridDim.y-th.  8-bit rows become
+// ranks at a time.  Of the adapters among its rows it takes every gridDim.z-th.  8-bit rows become
 // 16-bit ones on their way into LDS (both 16-bit types hold them exactly): a slice of them is 64
 // elements too.
 template <typename T, bool X8, int RC>
@@ -180,7 +180,8 @@ __global__ __launch_bounds__(DOWN_WAVES *WAVE) void down_kernel(ProjectParams p)
   constexpr int DEPTH = RC == 4 ? 2 : RC == 2 && X8 ? 3 : 4, RANKS = RC * 16, CORNER = (RANKS + DOWN_ROWS) * SLICE, SUMS = RC * 2 * WAVE * 16;
   __shared__ __align__(16) char room[DOWN_WAVES * (CORNER > SUMS ? CORNER : SUMS)];
   const int lane = threadIdx.x % WAVE, wave = wave_index();
-  const int row0 = blockIdx.x * DOWN_ROWS, m = lane % 16, q = lane / 16;
+  const int row0 = (int)block_index() * DOWN_ROWS, m = lane % 16, q = lane / 16;
+  if (row0 >= p.rows) return;
   char *const corner = room + wave * CORNER;
   // x: eight lanes a row and eight elements a lane
   const char *xr[DOWN_ROWS / 8];
@@ -198,7 +199,7 @@ __global__ __launch_bounds__(DOWN_WAVES *WAVE) void down_kernel(ProjectParams p)
     const int a = __builtin_amdgcn_readlane(mine, __builtin_ctzll(left));
     const unsigned long long these = __ballot(mine == a);
     left &= ~these;
-    if (n % (int)gridDim.y != (int)blockIdx.y) continue;
+    if (n % (int)gridDim.z != (int)blockIdx.z) continue;
     const int rank = rank_of(p, a);
     const float gain = p.gain[a];
     const char *const down = (const char *)p.down + (int64_t)a * p.max_rank * p.in_dim * 2;
@@ -567,7 +568,8 @@ __global__ __launch_bounds__(WM *WN *WAVE, 2) void tile_kernel(ProjectParams p) 
   const int tiles_m = (p.rows + BM - 1) / BM, tiles_n = (p.out_dim + BN - 1) / BN;
   // Workgroups go to the chip's eight dies in turn: each die takes a contiguous run of tiles, in
   // groups of eight tiles of rows, so that what its cache holds serves several tiles.
-  const int total = tiles_m * tiles_n, die = blockIdx.x % 8, slot = blockIdx.x / 8;
+  const int total = tiles_m * tiles_n, die = block_index() % 8, slot = block_index() / 8;
+  if (block_index() >= (unsigned)total) return;
   const int tile = die * (total / 8) + (die < total % 8 ? die : total % 8) + slot;
   const int group = tile / (8 * tiles_n), high = tiles_m - group * 8 < 8 ? tiles_m - group * 8 : 8;
   const int in_group = tile - group * 8 * tiles_n;
@@ -883,6 +885,8 @@ int project_check(const jdob_edge_project_args *a, bool sizes_only) {
   if (a->rows > JDOB_EDGE_MAX_ROWS || a->in_dim > JDOB_EDGE_MAX_PROJECT_DIM ||
       a->out_dim > JDOB_EDGE_MAX_PROJECT_DIM || (a->bits8 && a->in_dim > 131072))
     return JDOB_ERR_UNSUPPORTED;
+  // the smallest tiles have to fit a grid
+  if ((int64_t)((a->rows + 63) / 64) * ((a->out_dim + 63) / 64) > MAX_BLOCKS) return JDOB_ERR_UNSUPPORTED;
   if (sizes_only || a->rows == 0) return JDOB_OK;
   if (!a->x || !a->weight || !a->out || a->x_stride < a->in_dim || a->weight_stride < a->in_dim ||
       a->out_stride < a->out_dim || (a->bits8 && (!a->x_scale || !a->weight_scale)))
@@ -899,25 +903,22 @@ template <typename T, bool X8>
 int launch_down(const ProjectParams &p, hipStream_t stream) {
   const int groups = (p.rows + DOWN_ROWS - 1) / DOWN_ROWS;
   // few rows may all have adapters of their own: those are dealt to several workgroups
-  const dim3 grid((unsigned)groups, groups <= 4 ? (p.num_adapters < 32 ? p.num_adapters : 32) : 1);
+  const int layers = groups <= 4 ? (p.num_adapters < 32 ? p.num_adapters : 32) : 1;
   constexpr int threads = DOWN_WAVES * WAVE;
-  if (p.max_rank <= 16) return launch(down_kernel<T, X8, 1>, grid, threads, stream, p);
-  if (p.max_rank <= 32) return launch(down_kernel<T, X8, 2>, grid, threads, stream, p);
-  return launch(down_kernel<T, X8, 4>, grid, threads, stream, p);
+  if (p.max_rank <= 16) return launch(down_kernel<T, X8, 1>, groups, threads, stream, p, layers);
+  if (p.max_rank <= 32) return launch(down_kernel<T, X8, 2>, groups, threads, stream, p, layers);
+  return launch(down_kernel<T, X8, 4>, groups, threads, stream, p, layers);
 }
 
 template <typename T, bool X8, int NT, int WAVES, int DW, int DX>
 int launch_stream(const ProjectParams &p, hipStream_t stream) {
-  return launch(stream_kernel<T, X8, NT, WAVES, DW, DX>, dim3((unsigned)((p.out_dim + 15) / 16)), WAVES * WAVE,
-                stream, p);
+  return launch(stream_kernel<T, X8, NT, WAVES, DW, DX>, (p.out_dim + 15) / 16, WAVES * WAVE, stream, p);
 }
 
 template <typename T, bool X8, bool DIRECT, int BM, int BN, int WM, int WN, int STAGES, bool ROWWISE = false>
 int launch_tile(const ProjectParams &p, hipStream_t stream) {
   const int64_t tiles = (int64_t)((p.rows + BM - 1) / BM) * ((p.out_dim + BN - 1) / BN);
-  if (tiles > 0x7fffffff) return JDOB_ERR_UNSUPPORTED;
-  return launch(tile_kernel<T, X8, DIRECT, BM, BN, WM, WN, STAGES, ROWWISE>, dim3((unsigned)tiles), WM * WN * WAVE,
-                stream, p);
+  return launch(tile_kernel<T, X8, DIRECT, BM, BN, WM, WN, STAGES, ROWWISE>, tiles, WM * WN * WAVE, stream, p);
 }
 
 // Few rows with many adapters: the low-rank part output by output.  Through 4096 x 4096 with rank 16, in

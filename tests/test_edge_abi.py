@@ -202,3 +202,11 @@ def test_binding_refuses_tensors_on_the_host():
     at, first, count = (torch.tensor(v, dtype=t) for v, t in (([0, 3], torch.int32), ([0], torch.int64), ([9], torch.int32)))
     assert "cpu" in refused(INVALID, edge.attend, q, k, k, at, first, count)
     refused(INVALID, edge.attend, *(t.to("meta") for t in (q, k, k, at, first, count)))
+
+
+def test_grids_that_no_launch_takes_are_refused_before_anything_is_launched():
+    lib = edge.load()
+    a = project_args(rows=1 << 30, out_dim=1 << 20, out_stride=1 << 20, workspace_bytes=1 << 40)
+    assert lib.jdob_edge_project(C.byref(a), None) == UNSUPPORTED and lib.jdob_edge_project_workspace(C.byref(a)) == -1
+    a = attend_args(num_heads=1024, num_kv_heads=1024, query_rows=1 << 30, max_queries=1 << 30)
+    assert lib.jdob_edge_attend(C.byref(a), None) == UNSUPPORTED

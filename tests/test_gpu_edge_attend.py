@@ -232,3 +232,16 @@ def test_rows_far_from_zero_beside_ordinary_ones(new, keys):
     keep = torch.ones(got.shape[:2], dtype=torch.bool, device="cuda")
     keep[::3, ::2] = False
     assert torch.equal(got[keep], plain[keep]) and not got.isnan().any()
+
+
+def test_more_rows_than_one_dimension_of_a_grid():
+    """2^28 rows of eight heads, of which the last four see keys."""
+    rows, dim = (1 << 28) + 3, 8
+    s = inputs([4], [4], 8, 8, dim, BF16)
+    want = check(s, "four rows")
+    s["q"] = s["q"][:1].expand(rows, 8, dim)
+    s["query_start"], s["max_queries"] = torch.tensor([0, rows], dtype=torch.int32, device="cuda"), rows
+    got = edge.attend(**s)
+    assert torch.equal(got[rows - 4], want[0])
+    for at in range(0, rows - 4, 1 << 24):
+        assert not got[at:min(at + (1 << 24), rows - 4)].any(), at

@@ -131,3 +131,14 @@ def test_rows_whose_squares_leave_binary32(rows, dim, dtype, size, eps):
     for residual in (None, r):
         got = edge.norm(x, w, eps=eps, residual=residual, bits8=True, out16=True)
         check(got, x, w, eps, residual, (rows, dim, dtype, size, eps, residual is not None))
+
+
+@pytest.mark.parametrize("rows,dim,dtype", [((1 << 26) + 5, 8, BF16), ((1 << 24) + 3, 1100, BF16)])
+def test_more_rows_than_one_dimension_of_a_grid(rows, dim, dtype):
+    w = torch.ones(dim, dtype=dtype, device="cuda")
+    x = torch.empty(rows, dim, dtype=dtype, device="cuda").normal_(generator=torch.Generator(device="cuda").manual_seed(0))
+    got = edge.norm(x, w, bits8=True, out16=True)
+    for part in (slice(0, 1000), slice(rows // 2, rows // 2 + 1000), slice(rows - 1000, rows)):
+        check({k: v[part] if v is not None else None for k, v in got.items()}, x[part], w, 1e-6, None, part)
+    del x
+    assert (got["scale"] > 0).all() and got["q"].view(-1)[::dim].numel() == rows

@@ -181,3 +181,18 @@ def test_low_rank_rows_of_any_size(rows, i, o, n, x, down, up):
     s["adapters"]["down"][:, 3] *= 2.0 ** -6   # ranks of different sizes beside each other
     got = check(s)
     assert got.isfinite().all()
+
+
+@pytest.mark.parametrize("rows,n", [((1 << 28) + 37, 1), (1 << 30, 0)])
+def test_more_rows_than_one_dimension_of_a_grid(rows, n):
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    s = inputs(1, 8, 8, BF16, False, n, 4)
+    s["x"] = torch.empty(rows, 8, dtype=BF16, device="cuda").normal_(generator=gen)
+    if n:
+        s["row_adapter"] = torch.zeros(rows, dtype=torch.int32, device="cuda")
+    got = edge.project(**s)
+    for at in (0, rows // 2, rows - 500):
+        part = {**s, "x": s["x"][at:at + 500]}
+        if n:
+            part["row_adapter"] = s["row_adapter"][at:at + 500]
+        check(part, got[at:at + 500], at)
