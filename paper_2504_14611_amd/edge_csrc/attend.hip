@@ -700,10 +700,10 @@ FewPlan few_plan(const jdob_edge_attend_args *a) {
   each = each < 512 ? 512 : (each + 63) & ~63;
   int64_t splits = (a->max_keys + each - 1) / each;
   if (splits > MAX_SPLITS) {
-    each = ((a->max_keys + MAX_SPLITS - 1) / MAX_SPLITS + 63) & ~63;
+    each = (((int64_t)a->max_keys + MAX_SPLITS - 1) / MAX_SPLITS + 63) & ~63;
     splits = (a->max_keys + each - 1) / each;
   }
-  return {true, (int)tiles, (int)(splits < 1 ? 1 : splits), (int)each};
+  return {true, (int)tiles, (int)(splits < 1 ? 1 : splits), (int)(each < INT32_MAX ? each : INT32_MAX)};
 }
 
 template <typename T, int DP>

@@ -204,6 +204,14 @@ def test_binding_refuses_tensors_on_the_host():
     refused(INVALID, edge.attend, *(t.to("meta") for t in (q, k, k, at, first, count)))
 
 
+def test_the_longest_key_hints_split_the_keys():
+    """Hints up to the largest a call can give: the workspace grows with the splits, to as many as there are at most."""
+    lib = edge.load()
+    sizes = [lib.jdob_edge_attend_workspace(C.byref(attend_args(num_sequences=1, max_keys=n)))
+             for n in (100000, 1 << 28, (1 << 31) - 257, (1 << 31) - 255, (1 << 31) - 1)]
+    assert 0 < sizes[0] <= sizes[1] and len(set(sizes[1:])) == 1
+
+
 def test_grids_that_no_launch_takes_are_refused_before_anything_is_launched():
     lib = edge.load()
     a = project_args(rows=1 << 30, out_dim=1 << 20, out_stride=1 << 20, workspace_bytes=1 << 40)
