@@ -293,7 +293,7 @@ __device__ inline bool any_non_finite(const char *values) {
 // Replaces the staged values' infinities and NaN by zeros after adding them to the rows that see them
 // (their products with p = 0 of rows that do not would be NaN).  Rare, and slow.
 template <typename T, int DP, int KEYS>
-__device__ inline void take_non_finite(State<DP> &s, char *values, int first, int limit) {
+__device__ inline void take_non_finite(State<DP> &s, char *values, int sees) {
   constexpr unsigned EXP = __is_same(T, __bf16) ? 0x7f80u : 0x7c00u;
   const int half = threadIdx.x % WAVE / 32;
   for (int r = 0; r < KEYS; ++r)
@@ -304,7 +304,7 @@ __device__ inline void take_non_finite(State<DP> &s, char *values, int first, in
         const int at = 32 * d + 8 * (e / 4) + 4 * half + e % 4;
         const T x = *(const T *)(values + value_spot<DP>(r, at / 8) + at % 8 * 2);
         const unsigned bits = __builtin_bit_cast(unsigned short, x);
-        if ((bits & EXP) == EXP && first + r <= limit) s.out[d][e] += (float)x;
+        if ((bits & EXP) == EXP && r <= sees) s.out[d][e] += (float)x;
       }
 }
 
@@ -381,13 +381,13 @@ __global__ __launch_bounds__(PROMPT_WAVES *WAVE, 2) void prompt_kernel(AttendPar
   const T *const v = (const T *)p.v + q.key * p.v_stride + kv * p.v_head;
   const int last_row = (row0 + PROMPT_ROWS < q.rows ? row0 + PROMPT_ROWS : q.rows) - 1;
   const int seen = shift + last_row + 1;  // keys that some row of the workgroup sees
-  const int tiles = seen > 0 ? (seen + PROMPT_KEYS - 1) / PROMPT_KEYS : 0;
+  const int tiles = seen > 0 ? (seen - 1) / PROMPT_KEYS + 1 : 0;  // (counts of keys go up to 2^31 - 1)
   // tiles that all rows of the workgroup see
   const int whole = shift + row0 < 0 ? 0 : (shift + row0 + 1) / PROMPT_KEYS;
   // the last key that the wave's last row sees (-1: it has no rows, or they see nothing)
   const int wave_last = wave_row + 31 < last_row ? wave_row + 31 : last_row;
   const int wave_any = wave_row <= last_row ? shift + wave_last : -1;
-  const int limit = shift + mine;
+  const int limit = shift + (mine < last_row ? mine : last_row);
   bool careful = false;
   auto keys = [&](int kt) { return room + (kt & 1) * 2 * BYTES; };
   auto values = [&](int kt) { return room + ((kt & 1) * 2 + 1) * BYTES; };
@@ -454,7 +454,7 @@ __global__ __launch_bounds__(PROMPT_WAVES *WAVE, 2) void prompt_kernel(AttendPar
       const int first = kt * PROMPT_KEYS;
       char *const v_now = values(kt);
       if (any_non_finite<T, DP, PROMPT_KEYS>(v_now)) {  // the same for all waves
-        take_non_finite<T, DP, PROMPT_KEYS>(s, v_now, first, limit);
+        take_non_finite<T, DP, PROMPT_KEYS>(s, v_now, limit - first);
         __syncthreads();
         clear_non_finite<T, DP, PROMPT_KEYS, THREADS>(v_now, threadIdx.x);
         __syncthreads();
@@ -504,8 +504,8 @@ __global__ __launch_bounds__(FEW_WAVES *WAVE, DP == 64 ? 2 : 1) void few_kernel(
   const int columns = rows * p.group, column = tile * FEW_COLUMNS + l32;
   if (tile * FEW_COLUMNS >= columns) return;
   // this split's keys; the last split takes what the others leave (max_keys may be too small)
-  const int from = split * p.each;
-  const int until = split + 1 < p.splits && (int64_t)from + p.each < q.keys ? from + p.each : q.keys;
+  const int64_t from = (int64_t)split * p.each;
+  const int64_t until = split + 1 < p.splits && from + p.each < q.keys ? from + p.each : q.keys;
   if (from >= until && split > 0) return;
   const bool have = column < columns;
   const int row = have ? column / p.group : 0, head = kv * p.group + (have ? column % p.group : 0);
@@ -521,12 +521,13 @@ __global__ __launch_bounds__(FEW_WAVES *WAVE, DP == 64 ? 2 : 1) void few_kernel(
   char *const corner = room + wave * CORNER;
   auto keys_of = [&](bool careful) {
     s.clear();
-    auto load = [&](int b, int first) {
+    auto load = [&](int b, int64_t first) {
       stage<T, DP, DIRECT, false, FEW_KEYS, WAVE>(corner + b * 2 * BYTES, k, p.k_stride, first, q.keys, p.dim, careful, lane, 0);
       stage<T, DP, DIRECT, true, FEW_KEYS, WAVE>(corner + (b * 2 + 1) * BYTES, v, p.v_stride, first, q.keys, p.dim, careful,
                                                  lane, 0);
     };
-    int first = from + wave * FEW_KEYS, b = 0;
+    int64_t first = from + wave * FEW_KEYS;  // passes 2^31 behind the longest sequence's end
+    int b = 0;
     if (first < until) load(0, first);
     for (; first < until; first += FEW_WAVES * FEW_KEYS, b ^= 1) {
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the other buffer has been read
@@ -539,19 +540,19 @@ __global__ __launch_bounds__(FEW_WAVES *WAVE, DP == 64 ? 2 : 1) void few_kernel(
       const char *const keys = corner + b * 2 * BYTES;
       char *const values = corner + (b * 2 + 1) * BYTES;
       // keys behind `until` are the next split's (or none)
-      const int last = limit < until - 1 ? limit : until - 1;
+      const int64_t last = limit < until - 1 ? limit : until - 1;
       if (first + FEW_KEYS - 1 <= first_limit && first + FEW_KEYS <= until && !careful) {
         attend_tile<T, DP, 1, false>(s, qf, keys, values, 0, p.scale);
         continue;
       }
       if (careful && any_non_finite<T, DP, FEW_KEYS>(values)) {
-        take_non_finite<T, DP, FEW_KEYS>(s, values, first, last);
+        take_non_finite<T, DP, FEW_KEYS>(s, values, (int)(last - first));
         // the wave's own values: its lanes run together, their LDS accesses in order
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         clear_non_finite<T, DP, FEW_KEYS, WAVE>(values, lane);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       }
-      attend_tile<T, DP, 1, true>(s, qf, keys, values, last - first, p.scale);
+      attend_tile<T, DP, 1, true>(s, qf, keys, values, (int)(last - first), p.scale);
     }
   };
   keys_of(false);

@@ -245,3 +245,15 @@ def test_more_rows_than_one_dimension_of_a_grid():
     assert torch.equal(got[rows - 4], want[0])
     for at in range(0, rows - 4, 1 << 24):
         assert not got[at:min(at + (1 << 24), rows - 4)].any(), at
+
+
+def test_the_longest_sequence():
+    """2^31 - 1 keys: positions behind the last one pass 32 bits."""
+    m = (1 << 31) - 1
+    kv = torch.zeros(m, 1, 8, dtype=BF16, device="cuda")
+    kv[m - 1], kv[m - 3] = 16.0, 12.0
+    q = torch.full((3, 1, 8), 16.0, dtype=BF16, device="cuda")
+    at = torch.tensor([0, 3], dtype=torch.int32, device="cuda")
+    first, count = torch.zeros(1, dtype=torch.int64, device="cuda"), torch.full((1,), m, dtype=torch.int32, device="cuda")
+    got = edge.attend(q, kv, kv, at, first, count)
+    assert got[:, 0, 0].tolist() == [12.0, 12.0, 16.0] and torch.equal(got, got[:, :, :1].expand(3, 1, 8))
