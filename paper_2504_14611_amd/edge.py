@@ -161,14 +161,14 @@ def _norm(a, where, x, bits8, out16, into, handle):
     shape, dtype, dev, dim = x.shape, x.dtype, x.device, a.dim
     total = out = q = scale = None
     if a.residual_stride:
-        total = into and into.get("sum")
+        total = into.get("sum") if into else None
         if total is None:
             total = torch.empty_like(x, memory_format=torch.contiguous_format)
             a.sum, a.sum_stride = total.data_ptr(), dim
         else:
             a.sum, a.sum_stride = _array(total, where, "sum", shape, dtype, dev), _row_stride(total, dim)
     if out16:
-        out = into and into.get("out")
+        out = into.get("out") if into else None
         if out is None:
             out = torch.empty_like(x, memory_format=torch.contiguous_format)
             a.out, a.out_stride = out.data_ptr(), dim

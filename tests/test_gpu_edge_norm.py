@@ -142,3 +142,13 @@ def test_more_rows_than_one_dimension_of_a_grid(rows, dim, dtype):
         check({k: v[part] if v is not None else None for k, v in got.items()}, x[part], w, 1e-6, None, part)
     del x
     assert (got["scale"] > 0).all() and got["q"].view(-1)[::dim].numel() == rows
+
+
+def test_buffers_for_some_outputs_or_none():
+    x, r, w = inputs(30, 500, BF16, True)
+    want = edge.norm(x, w, residual=r, bits8=True, out16=True)
+    for names in ((), ("sum",), ("q", "out"), ("scale",), ("sum", "out", "q", "scale")):
+        into = {k: torch.empty_like(want[k]) for k in names}
+        got = edge.norm(x, w, residual=r, bits8=True, out16=True, into=into)
+        for key in want:
+            assert torch.equal(got[key], want[key]) and (key not in into or got[key] is into[key]), (names, key)
