@@ -30,6 +30,7 @@ except ImportError:
 
 EDGE_BF16, EDGE_F16, EDGE_F32 = 0, 1, 2
 MAX_ROWS, MAX_NORM_DIM, MAX_RANK, MAX_HEAD_DIM, MAX_SEQUENCES = 1 << 30, 16384, 256, 128, 65535
+_MAX_I32 = 0x7fffffff
 
 EXPORTS = ("jdob_edge_norm", "jdob_edge_project", "jdob_edge_project_workspace", "jdob_edge_attend",
            "jdob_edge_attend_workspace")
@@ -138,8 +139,8 @@ def norm(x, weight, eps: float = 1e-6, residual=None, bits8: bool = False, out16
         _refuse(where, "x has rows and columns")
     shape, dtype, dev = x.shape, x.dtype, x.device
     rows, dim = shape
-    if rows > MAX_ROWS:
-        _refuse(where, f"{rows} rows", jdob.JDOB_ERR_UNSUPPORTED)
+    if rows > MAX_ROWS or dim > MAX_NORM_DIM:
+        _refuse(where, f"{rows} rows of {dim}", jdob.JDOB_ERR_UNSUPPORTED)
     if out16 is None:
         out16 = not bits8
     if not (bits8 or out16):
@@ -203,9 +204,9 @@ def project(x, weight, x_scale=None, weight_scale=None, adapters: Optional[dict]
     if x.dim() != 2 or weight.dim() != 2:
         _refuse(where, "x and weight have rows and columns")
     rows, i = x.shape
-    if rows > MAX_ROWS:
-        _refuse(where, f"{rows} rows", jdob.JDOB_ERR_UNSUPPORTED)
     o, dev = weight.shape[0], x.device
+    if rows > MAX_ROWS or i > _MAX_I32 or o > _MAX_I32:  # (the library knows the smaller limits)
+        _refuse(where, f"{rows} rows of {i} and {o}", jdob.JDOB_ERR_UNSUPPORTED)
     kind = x.dtype
     bits8 = kind is torch.int8
     if dtype is None:
@@ -228,6 +229,8 @@ def project(x, weight, x_scale=None, weight_scale=None, adapters: Optional[dict]
         if down.dim() != 3:
             _refuse(where, "down is [adapters, rank, in]")
         n, most = down.shape[:2]
+        if n > _MAX_I32 or most > MAX_RANK:
+            _refuse(where, f"{n} adapters of rank {most}", jdob.JDOB_ERR_UNSUPPORTED)
         a.num_adapters, a.max_rank = n, most
         a.down = _dense(down, where, "down", (n, most, i), dtype, dev)
         a.up = _dense(adapters["up"], where, "up", (n, o, most), dtype, dev)
@@ -289,8 +292,14 @@ def attend(q, k, v, query_start, key_start, key_count, scale: Optional[float] = 
         _refuse(where, f"heads of {d}", jdob.JDOB_ERR_UNSUPPORTED)
     key_rows, g = k.shape[:2]
     n = key_count.shape[0]
-    a = AttendArgs(n, h, g, d, _dtype(dtype, where), rows if max_queries is None else max_queries,
-                   min(key_rows, 0x7fffffff) if max_keys is None else max_keys, d ** -0.5 if scale is None else scale, rows, key_rows,
+    if n > MAX_SEQUENCES:
+        _refuse(where, f"{n} sequences", jdob.JDOB_ERR_UNSUPPORTED)
+    most = rows if max_queries is None else max_queries
+    longest = key_rows if max_keys is None else max_keys
+    if most < 0 or longest < 0:
+        _refuse(where, f"max_queries {most}, max_keys {longest}")
+    a = AttendArgs(n, h, g, d, _dtype(dtype, where), min(most, _MAX_I32), min(longest, _MAX_I32),
+                   d ** -0.5 if scale is None else scale, rows, key_rows,
                    _array(q, where, "q", shape, dtype, dev), q.stride(0), q.stride(1),
                    _array(k, where, "k", (key_rows, g, d), dtype, dev), k.stride(0), k.stride(1),
                    _array(v, where, "v", (key_rows, g, d), dtype, dev), v.stride(0), v.stride(1),

@@ -204,6 +204,26 @@ def test_binding_refuses_tensors_on_the_host():
     refused(INVALID, edge.attend, *(t.to("meta") for t in (q, k, k, at, first, count)))
 
 
+def test_binding_refuses_sizes_that_32_bits_would_cut():
+    """Shapes and hints whose low 32 bits are small numbers are not taken for those."""
+    def t(*shape, dtype=torch.bfloat16):
+        return torch.empty(*shape, dtype=dtype, device="meta")
+    big = 1 << 32
+    refused(UNSUPPORTED, edge.norm, t(1, big + 8), t(8))
+    refused(UNSUPPORTED, edge.norm, t(big + 1, 8), t(8))
+    refused(UNSUPPORTED, edge.project, t(1, big + 8), t(5, big + 8))
+    refused(UNSUPPORTED, edge.project, t(1, 8), t(big + 5, 8))
+    for down, up, gain in ((t(2, big + 4, 8), t(2, 5, big + 4), t(2, dtype=torch.float32)),
+                           (t(big + 2, 4, 8), t(big + 2, 5, 4), t(big + 2, dtype=torch.float32))):
+        refused(UNSUPPORTED, edge.project, t(1, 8), t(5, 8), adapters={"down": down, "up": up, "gain": gain},
+                row_adapter=t(1, dtype=torch.int32))
+    q, k, at = t(3, 4, 16), t(9, 2, 16), t(2, dtype=torch.int32)
+    first, count = t(1, dtype=torch.int64), t(1, dtype=torch.int32)
+    refused(UNSUPPORTED, edge.attend, q, k, k, t(big + 2, dtype=torch.int32), t(big + 1, dtype=torch.int64), t(big + 1, dtype=torch.int32))
+    assert "max_" in refused(INVALID, edge.attend, q, k, k, at, first, count, max_queries=1 - big)
+    assert "max_" in refused(INVALID, edge.attend, q, k, k, at, first, count, max_keys=1 - big)
+
+
 def test_the_longest_key_hints_split_the_keys():
     """Hints up to the largest a call can give: the workspace grows with the splits, to as many as there are at most."""
     lib = edge.load()

@@ -257,3 +257,12 @@ def test_the_longest_sequence():
     first, count = torch.zeros(1, dtype=torch.int64, device="cuda"), torch.full((1,), m, dtype=torch.int32, device="cuda")
     got = edge.attend(q, kv, kv, at, first, count)
     assert got[:, 0, 0].tolist() == [12.0, 12.0, 16.0] and torch.equal(got, got[:, :, :1].expand(3, 1, 8))
+
+
+def test_hints_beyond_32_bits():
+    s = inputs([5, 3], [9, 700], 4, 2, 64, BF16)
+    want = check(s, "exact hints")
+    for most in (1 << 31, (1 << 32) + 1):
+        check({**s, "max_queries": most}, most)
+        assert torch.equal(edge.attend(**{**s, "max_queries": 5, "max_keys": 700}), want)
+        check({**s, "max_keys": most}, most)
