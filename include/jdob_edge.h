@@ -135,7 +135,7 @@ int jdob_edge_project(const jdob_edge_project_args *a, void *hip_stream);
  * the launch); rows beyond max_queries may be left unwritten.              */
 typedef struct {
   int32_t num_sequences;          /* 0 .. JDOB_EDGE_MAX_SEQUENCES            */
-  int32_t num_heads, num_kv_heads;/* num_heads a multiple of num_kv_heads    */
+  int32_t num_heads, num_kv_heads;/* num_heads a multiple of num_kv_heads, to 1024 */
   int32_t head_dim;               /* a multiple of 8, to JDOB_EDGE_MAX_HEAD_DIM */
   int32_t dtype;                  /* BF16 or F16                             */
   int32_t max_queries, max_keys;  /* >= 0                                    */
@@ -151,7 +151,7 @@ typedef struct {
   const int64_t *key_start;       /* [num_sequences]                         */
   const int32_t *key_count;       /* [num_sequences]                         */
   void *out;                      /* [query_rows][num_heads][head_dim]       */
-  int64_t out_stride, out_head_stride;
+  int64_t out_stride, out_head_stride; /* >= head_dim, where there is more than one */
   void *workspace;                /* jdob_edge_attend_workspace bytes        */
   int64_t workspace_bytes;
 } jdob_edge_attend_args;

@@ -673,6 +673,9 @@ int attend_check(const jdob_edge_attend_args *a, bool sizes_only) {
   if (a->q_stride < 0 || a->q_head_stride < 0 || a->k_stride < 0 || a->k_head_stride < 0 || a->v_stride < 0 ||
       a->v_head_stride < 0 || a->out_stride < 0 || a->out_head_stride < 0)
     return JDOB_ERR_INVALID_ARG;
+  // rows and heads of out that are written at once must not share elements
+  if ((a->query_rows > 1 && a->out_stride < a->head_dim) || (a->num_heads > 1 && a->out_head_stride < a->head_dim))
+    return JDOB_ERR_INVALID_ARG;
   const int64_t need = jdob_edge_attend_workspace(a);
   if (need > 0 && (!a->workspace || (uintptr_t)a->workspace % 16 || a->workspace_bytes < need))
     return JDOB_ERR_INVALID_ARG;

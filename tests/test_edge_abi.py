@@ -224,6 +224,14 @@ def test_binding_refuses_sizes_that_32_bits_would_cut():
     assert "max_" in refused(INVALID, edge.attend, q, k, k, at, first, count, max_keys=1 - big)
 
 
+@pytest.mark.parametrize("fields,code", [
+    ({"out_stride": 0}, INVALID), ({"out_stride": 63}, INVALID), ({"out_head_stride": 0}, INVALID),
+    ({"out_head_stride": 56}, INVALID),
+])
+def test_attend_refuses_outputs_whose_rows_or_heads_overlap(fields, code):
+    assert edge.load().jdob_edge_attend(C.byref(attend_args(**fields)), None) == code
+
+
 def test_the_longest_key_hints_split_the_keys():
     """Hints up to the largest a call can give: the workspace grows with the splits, to as many as there are at most."""
     lib = edge.load()
