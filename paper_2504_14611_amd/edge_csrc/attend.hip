@@ -471,7 +471,7 @@ __global__ __launch_bounds__(PROMPT_WAVES *WAVE, 2) void prompt_kernel(AttendPar
       const float y[4] = {s.out[d][4 * e] * f, s.out[d][4 * e + 1] * f, s.out[d][4 * e + 2] * f, s.out[d][4 * e + 3] * f};
       store_f32<T, 4>((T *)(corner + key_spot<DP>(l32, d * 4 + e) + half * 8), y);
     }
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  lanes_meet();
   T *const out = (T *)p.out + (q.row + wave_row) * p.out_stride + head * p.out_head;
 #pragma unroll
   for (int i = 0; i < 32 * DP / 8 / WAVE; ++i) {
@@ -548,9 +548,9 @@ __global__ __launch_bounds__(FEW_WAVES *WAVE, DP == 64 ? 2 : 1) void few_kernel(
       if (careful && any_non_finite<T, DP, FEW_KEYS>(values)) {
         take_non_finite<T, DP, FEW_KEYS>(s, values, (int)(last - first));
         // the wave's own values: its lanes run together, their LDS accesses in order
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        lanes_meet();
         clear_non_finite<T, DP, FEW_KEYS, WAVE>(values, lane);
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        lanes_meet();
       }
       attend_tile<T, DP, 1, true>(s, qf, keys, values, (int)(last - first), p.scale);
     }

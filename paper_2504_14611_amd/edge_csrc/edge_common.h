@@ -91,6 +91,10 @@ __device__ inline void wait_loads() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "i"(N) : "memory");
 }
 
+// Between a wave's stores to LDS and other lanes' reads of them, and between those reads and the next
+// stores: the hardware takes a wave's LDS accesses in order, and so must the compiler, which knows a lane's only.
+__device__ inline void lanes_meet() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
+
 // A barrier that waits for nothing but the waves.
 __device__ inline void barrier() {
   asm volatile("" ::: "memory");

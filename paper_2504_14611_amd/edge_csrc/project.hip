@@ -218,6 +218,7 @@ __global__ __launch_bounds__(DOWN_WAVES *WAVE) void down_kernel(ProjectParams p)
           for (int i = 0; i < DOWN_ROWS / 8; ++i) xv[d][i] = *(const xword *)(xr[i] + s * (X8 ? 64 : 128));
         };
         auto multiply = [&](int d) {
+          lanes_meet();
           Rows<RANKS>::put(corner, av[d]);
 #pragma unroll
           for (int i = 0; i < DOWN_ROWS / 8; ++i) {
@@ -234,6 +235,7 @@ __global__ __launch_bounds__(DOWN_WAVES *WAVE) void down_kernel(ProjectParams p)
               *(u32x4 *)to = xv[d][i];
             }
           }
+          lanes_meet();
           typedef typename Mma<T>::frag frag;
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
@@ -410,8 +412,10 @@ __global__ __launch_bounds__(WAVES *WAVE) void stream_kernel(ProjectParams p) {
   acc_t acc[NT] = {};
   char *const corner = room + wave * CORNER;
   auto multiply = [&](const u32x4 (&wv)[2], const u32x4 (&xv)[NT * 2]) {
+    lanes_meet();
     Rows<16>::put(corner, wv);
     Rows<NT * 16>::put(corner + 16 * SLICE, xv);
+    lanes_meet();
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const u32x4 wf = *(const u32x4 *)(corner + spot(m, h * 4 + q));
@@ -638,7 +642,7 @@ __global__ __launch_bounds__(WM *WN *WAVE, 2) void tile_kernel(ProjectParams p) 
           if (lane == 0) list[n] = b;
           ++n;
         }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        lanes_meet();
       }
       if (lane == 0) listed = n;
     }
