@@ -181,19 +181,22 @@ def instance(shape: Shape, users: int, tokens: int, alpha: float, beta: float, s
 def carry_out(shape: Shape, chain: Sequence[dict], cut: int, offloaders: Sequence[int], rows: dict, more: int = 0,
               device="cuda"):
     """The offloaders' prompts (`rows`: user -> [tokens, width]) through the chain: blocks 1..cut each on their own
-    device, the others in one batch on the edge, then `more` further single rows a user on the edge, each the row
+    device, the others in one batch on the edge, then `more` further single rows a user the same way, each the row
     that left the last block before it.  Returns user -> the rows that left the last block."""
     import torch
     lengths = [rows[u].shape[0] for u in offloaders]
-    sent = [Edge(shape, chain[:cut], [u], 0, rows[u].shape[0], device).run(rows[u], [rows[u].shape[0]])
-            for u in offloaders]
+    devices = [Edge(shape, chain[:cut], [u], 0, n + more, device) for u, n in zip(offloaders, lengths)]
     e = Edge(shape, chain, offloaders, cut, max(lengths) + more, device)
-    out = list(e.run(torch.cat(sent), lengths).split(lengths))
-    last = torch.stack([o[-1] for o in out])
+
+    def through(entering):
+        sent = [d.run(x, [x.shape[0]]) for d, x in zip(devices, entering)]
+        new = [x.shape[0] for x in sent]
+        return e.run(torch.cat(sent), new).split(new)
+
+    out = [through([rows[u] for u in offloaders])]
     for _ in range(more):
-        last = e.run(last, [1] * len(offloaders))
-        out = [torch.cat([o, last[i:i + 1]]) for i, o in enumerate(out)]
-    return dict(zip(offloaders, out))
+        out.append(through([x[-1:] for x in out[-1]]))
+    return {u: torch.cat(parts) for u, parts in zip(offloaders, zip(*out))}
 
 
 def main(argv=None) -> Dict[str, object]:

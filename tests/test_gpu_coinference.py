@@ -85,3 +85,21 @@ def test_the_command(capsys):
     assert r["alpha"] >= 0 and r["beta"] >= 0 and "policy" in capsys.readouterr().out
     for o in r.get("out", {}).values():
         assert torch.isfinite(o).all()
+
+
+@pytest.mark.parametrize("cut", [0, 1, 3])
+def test_further_rows_pass_every_block(chain, rows, cut):
+    """Where the chain is cut does not change what comes out of it.  (A further row is the output before it: what two
+    ways of computing differ by enters the next pass, so each pass may add its own 0.04.)"""
+    users = [2, 0, 4]
+    out = co.carry_out(SHAPE, chain, cut, users, rows, 3)
+    for u in users:
+        e = co.Edge(SHAPE, chain, [u], 0, 80)
+        n = rows[u].shape[0]
+        want = [e.run(rows[u], [n])]
+        for _ in range(3):
+            want.append(e.run(want[-1][-1:], [1]))
+        assert out[u].shape == (n + 3, SHAPE.width)
+        assert off(out[u][:n], want[0]) < 0.04, u
+        for k in range(3):
+            assert off(out[u][n + k], want[k + 1][0]) < 0.04 * (k + 2), (u, k)
