@@ -4,7 +4,7 @@ The chain's sub-tasks are decoder blocks that all users share, each user with a 
 The planner (jdob.solve_batch) takes the latency of a batch of b users on the edge GPU as alpha_l + beta_l * b per
 sub-task; here the edge operators (edge.norm, edge.project, edge.attend) are that latency and the carrying out:
 
-1. `profile` times a block on this GPU for batches of users and fits alpha and beta,
+1. `profile` times the blocks on this GPU for batches of users and fits alpha and beta of one,
 2. `instance` puts them with the devices, uplinks and deadlines into a problem, which jdob.solve_batch decides:
    the partition point s, the GPU level, and which users offload,
 3. `Edge` computes blocks s+1..L for the offloaded users' rows in one batch, all users' rows packed one after the
@@ -138,7 +138,8 @@ def fit(batches: Sequence[int], seconds: Sequence[float]) -> tuple:
 
 
 def profile(shape: Shape, chain: Sequence[dict], users: int, tokens: int, repeats: int = 5, device="cuda") -> tuple:
-    """alpha, beta in seconds of one block for b users' prompts of `tokens` rows, timed on this GPU."""
+    """alpha, beta in seconds of one block for b users' prompts of `tokens` rows, timed on this GPU: the whole chain's
+    time over its blocks, as a batch brings its index arrays to the GPU once and not for every block."""
     import torch
     batches = sorted({1, *[max(1, users * k // 4) for k in (1, 2, 3, 4)]})
     seconds = []
@@ -146,13 +147,13 @@ def profile(shape: Shape, chain: Sequence[dict], users: int, tokens: int, repeat
         rows = torch.randn(b * tokens, shape.width, device=device).bfloat16()
         times = []
         for _ in range(repeats + 2):
-            e = Edge(shape, chain[:1], list(range(b)), 0, tokens, device)
+            e = Edge(shape, chain, list(range(b)), 0, tokens, device)
             torch.cuda.synchronize()
             t = time.perf_counter()
             e.run(rows, [tokens] * b)
             torch.cuda.synchronize()
             times.append(time.perf_counter() - t)
-        seconds.append(sorted(times[2:])[repeats // 2])
+        seconds.append(sorted(times[2:])[repeats // 2] / len(chain))
     return fit(batches, seconds)
 
 

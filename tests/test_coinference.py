@@ -43,3 +43,22 @@ def test_edge_refuses_rows_that_do_not_fit():
         e.run(torch.zeros(3, 64).bfloat16(), [1, 1])
     with pytest.raises(ValueError):
         e.run(torch.zeros(6, 64).bfloat16(), [1, 5])
+
+
+def test_profile_charges_a_batch_once_for_what_it_does_once(monkeypatch):
+    """A batch that takes 5 ms once and (2 + 0.1 b) ms a block: over 10 blocks that is 2.5 ms + 0.1 ms a user a block."""
+    torch = pytest.importorskip("torch")
+    now = [0.0]
+
+    class Timed:
+        def __init__(self, shape, chain, users, first, room, device="cuda"):
+            self.blocks, self.users = len(chain[first:]), len(users)
+
+        def run(self, rows, lengths):
+            now[0] += 5e-3 + self.blocks * (2e-3 + 1e-4 * self.users)
+
+    monkeypatch.setattr(co, "Edge", Timed)
+    monkeypatch.setattr(co.time, "perf_counter", lambda: now[0])
+    monkeypatch.setattr(torch.cuda, "synchronize", lambda *a: None)
+    alpha, beta = co.profile(co.Shape(width=64), [{}] * 10, 8, 4, device="cpu")
+    assert abs(alpha - 2.5e-3) < 1e-9 and abs(beta - 1e-4) < 1e-10
