@@ -102,6 +102,8 @@ class Edge:
             raise ValueError("a length for every user, and a row for each")
         if any(c + m > self.room for c, m in zip(self.count, lengths)):
             raise ValueError(f"the cache has room for {self.room} rows a user")
+        if not self.chain:
+            return rows
         starts = [sum(lengths[:u]) for u in range(n + 1)]
         query_start = torch.tensor(starts, dtype=torch.int32, device=dev)
         key_start = torch.arange(n, device=dev) * self.room
