@@ -13,6 +13,11 @@
 // one key head stand together as 32 columns, each wave takes other keys, and the keys are split
 // over workgroups, whose partial results `join_kernel` puts together.
 //
+// p is rounded to dtype for its product with v, its sum is not.  Against 64 bits that makes the output's error
+// 2.0e-3 with prompts and 2.3e-3 with tokens where its own rounding to bfloat16 alone makes 1.6e-3 and 1.7e-3.
+// With p in two parts, the rounded one and what it left, the errors are those; a prompt of 16,384 rows then takes
+// 1.49 ms for 1.02, ragged prompts 214 us for 184, tokens 136 us for 131.
+//
 // Measured (kernel alone): 16,384 rows with 16 heads of 128 1.02-1.09 ms (1.0-1.08 PFLOP/s); 32 prompts of
 // 40 to 1000 rows 180-210 us (their rows, keys and values move in 69 us, their products take 60 at a
 // library's rate); one row of 32 heads after 131,071 keys 107 us (5.0 TB/s) and 9 us for the join.
