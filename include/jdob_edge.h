@@ -34,6 +34,7 @@
  * checked by the host: entries out of range never lead to an access out of
  * bounds (they are clamped, or the row counts as one without an adapter).
  * Outputs must not overlap inputs unless an argument says that they may.
+ * The operators are forward passes.
  */
 #ifndef JDOB_EDGE_H
 #define JDOB_EDGE_H
@@ -132,7 +133,8 @@ int jdob_edge_project(const jdob_edge_project_args *a, void *hip_stream);
  * output are binary32; p is rounded to dtype before it is multiplied with v
  * (relative error 2^-8 or 2^-11 of each term, the size of out's own rounding).
  * max_queries and max_keys are at least the largest n and m (both only size
- * the launch); rows beyond max_queries may be left unwritten.              */
+ * the launch and choose the kernel for all of the call's sequences); rows
+ * beyond max_queries may be left unwritten.                                */
 typedef struct {
   int32_t num_sequences;          /* 0 .. JDOB_EDGE_MAX_SEQUENCES            */
   int32_t num_heads, num_kv_heads;/* num_heads a multiple of num_kv_heads, to 1024 */

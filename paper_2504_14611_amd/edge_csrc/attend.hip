@@ -19,9 +19,9 @@
 // 1.49 ms for 1.02, ragged prompts 214 us for 184, tokens 136 us for 131.
 //
 // Measured (kernel alone): 16,384 rows with 16 heads of 128 1.02-1.09 ms (1.0-1.08 PFLOP/s); 32 prompts of
-// 40 to 1000 rows 180-210 us (their rows, keys and values move in 69 us, their products take 60 at a
-// library's rate); one row of 32 heads after 131,071 keys 107 us (5.0 TB/s) and 9 us for the join.
-// Many rows are bound by instructions: the matrix units are busy 59 % of the time (27 % with the short
+// 40 to 1000 rows 180-220 us (their rows, keys and values move in 69 us, their products take 60 at a
+// library's rate); one row of 32 heads after 131,071 keys 109 us (4.9 TB/s) and 10 us for the join.
+// Many rows are bound by instructions: the matrix units are busy 58 % of the time (27 % with the short
 // prompts, whose tiles' beginnings cost as much as their products), the vector units for p nearly as
 // long, in turn within a wave and only by chance at once in two.  Few rows are bound by HBM.
 #include "edge_common.h"
@@ -698,7 +698,7 @@ FewPlan few_plan(const jdob_edge_attend_args *a) {
   const int64_t groups = tiles * a->num_kv_heads * a->num_sequences;
   // Many rows take prompt_kernel, whose workgroups stage each key once for 128 rows of one head, unless
   // that gives the chip too few workgroups for the keys there are: 64 rows of 32 heads after 20,000 keys
-  // (32 workgroups) take 475 us there and 98 us here.
+  // (32 workgroups) take 369 us there and 100 us here.
   const int64_t prompts = (a->query_rows / PROMPT_ROWS + a->num_sequences) * a->num_heads;
   const bool long_keys = prompts < 256 && a->max_keys >= 1024 && columns <= 4096;
   if ((columns > 128 && !long_keys) || groups > (1 << 24)) return {false, 0, 0, 0};

@@ -5,8 +5,8 @@
 // Bound: HBM.  A row is read once, kept in registers as binary32 through both reductions (the sum
 // of squares, then the largest |y|) and written once, so the bytes moved are the operator's own.
 // A row belongs to TPR threads with NV vectors of 16 bytes each.  8191 bfloat16 rows of 4096 with a
-// residual, in 8 bits: 41 us back to back, 5.7 TB/s (a large copy moves 4.8 TB/s; part of these rows stays
-// in the last cache from pass to pass); 32 rows: 4.6 us, a launch.
+// residual, in 8 bits: 42 us back to back, 5.5 TB/s (a large copy moves 4.8 TB/s; part of these rows stays
+// in the last cache from pass to pass); 32 rows: 4.8 us, a launch.
 #include "edge_common.h"
 
 namespace edge {
@@ -200,8 +200,8 @@ int norm_dispatch(const NormParams &p, hipStream_t stream) {
   constexpr int VE = 16 / (int)sizeof(T);
   const int v = (p.dim + VE - 1) / VE;  // vectors a row
   // A wave a row saves the exchange through LDS, but keeps only as many loads under way as one wave has
-  // registers for: 4096 rows of 1024 (bf16, with a residual) take 7.3 us so and 9.0 with four waves a row,
-  // 8191 rows of 4096 take 45.6 so and 40.9 with four waves, 256 rows of 4096 7.4 and 5.1.
+  // registers for: 4096 rows of 1024 (bf16, with a residual, in 8 bits; calls in a graph) take 11.1 us so and
+  // 14.2 with four waves a row, 8191 rows of 4096 take 60 so and 46 with four waves, 256 rows of 4096 10.4 and 6.6.
   if (v <= 64) return norm_launch<T, 64, 1>(p, stream);
   if (v <= 128 && p.rows >= 1024) return norm_launch<T, 64, 2>(p, stream);
   if (v <= 256) return norm_launch<T, 256, 1>(p, stream);

@@ -6,10 +6,11 @@
 // x W^T and adds the low-rank rows times B_a^T before it stores: `stream_kernel` for few rows, where
 // reading W is all that counts, `tile_kernel` for many, where the products are.
 //
-// Measured (kernel alone): x A^T of 8192 x 4096 with rank 16 22-24 us (3 TB/s of x), of 32 rows with
-// 32 adapters 10 us; W streamed past 32 rows, 4096 x 4096, 9.6 us (3.5 TB/s); tiles at 8192 x 4096 x 4096
-// 225-240 us (1.15-1.2 PFLOP/s; a library's product without adapters 178 us), 6007 x 4096 x 14336 in 8
-// bits 365-390 us (1.8-1.9 POP/s; a library's 1.87).  The matrix units are busy 61 % (53 %) of the large
+// Measured (kernel alone): x A^T of 8192 x 4096 with rank 16 22-25 us (3 TB/s of x), of 32 rows with
+// 32 adapters 11 us; W streamed past 32 rows, 4096 x 4096, 9.8 us (3.4 TB/s); tiles at 8192 x 4096 x 4096
+// 235 us in a graph (1.17 PFLOP/s; a library's product 178 us), with 32 adapters 242 at least and 278 in the
+// middle of single launches; 6007 x 4096 x 14336 in 8 bits 357 us in a graph (1.97 POP/s; a library's 1.87),
+// with 16 adapters 396 and 439.  The matrix units are busy 61 % (54 %) of the large
 // tiles' time, at clocks that the load lowers to about 2.1 GHz; LDS is busy a quarter of it, without
 // conflicts.  What is left is the slices' two barriers, the loads' issue behind them, and the tiles'
 // beginnings and ends (one workgroup a compute unit).
@@ -875,8 +876,10 @@ __global__ __launch_bounds__(WM *WN *WAVE, 2) void tile_kernel(ProjectParams p) 
 
 // ------------------------------------------------------------------ host side
 
-// Up to here W streams through: 64 rows through 4096 x 4096 take 13.3 us so and 28.5 by tiles of 64 x 64,
-// through 14336 columns 42 and 29 (x then passes 896 workgroups); 128 rows would take 34 and 19 (8 bits).
+// Up to here W streams through.  64 rows of 4096 (calls in a graph, without adapters) through 1024 columns take
+// 12.1 us so and 23.9 by tiles of 64 x 64 (8 bits: 8.1 and 14.2), through 4096 columns 14.5 and 24.3 (11.1 and
+// 14.7).  The rule looks at rows alone: through 14336 columns, where x passes 896 workgroups, tiles would be
+// the faster ones from 33 rows on (64 rows: 53 and 30, 8 bits 31 and 16).
 constexpr int STREAM_ROWS = 64;
 
 int project_check(const jdob_edge_project_args *a, bool sizes_only) {
@@ -906,7 +909,9 @@ int project_check(const jdob_edge_project_args *a, bool sizes_only) {
 template <typename T, bool X8>
 int launch_down(const ProjectParams &p, hipStream_t stream) {
   const int groups = (p.rows + DOWN_ROWS - 1) / DOWN_ROWS;
-  // few rows may all have adapters of their own: those are dealt to several workgroups
+  // Few rows may all have adapters of their own: up to 128 rows those are dealt to several workgroups.  Beyond,
+  // a workgroup takes all of its 32 rows' adapters one after the other: through 4096 x 4096 with 64 adapters of
+  // rank 16, 128 rows take 40 us, 129 rows 127 and 512 rows 82.
   const int layers = groups <= 4 ? (p.num_adapters < 32 ? p.num_adapters : 32) : 1;
   constexpr int threads = DOWN_WAVES * WAVE;
   if (p.max_rank <= 16) return launch(down_kernel<T, X8, 1>, groups, threads, stream, p, layers);
@@ -926,8 +931,9 @@ int launch_tile(const ProjectParams &p, hipStream_t stream) {
 }
 
 // Few rows with many adapters: the low-rank part output by output.  Through 4096 x 4096 with rank 16, in
-// slices and so: 128 rows with 8 adapters 39.3 and 42.8 us, with 16 42.0 and 43.1, with 64 58.2 and 45.0;
-// 512 rows with 64 86.0 and 85.3.
+// slices and so (calls in a graph): 128 rows with 8 adapters 36.1 and 38.1 us, with 16 38.5 and 38.3, with 64
+// 54.7 and 40.4; 512 rows with 64 84.3 and 81.9.  (It counts the adapters that there are, not those that the
+// rows have, which the host does not know.)
 bool rowwise(int rows, int num_adapters) { return rows <= 512 && num_adapters * 8 >= rows; }
 
 template <typename T, bool X8>
@@ -947,9 +953,10 @@ int project(const ProjectParams &p, hipStream_t stream) {
     return rw ? launch_tile<T, X8, false, 64, 64, 2, 2, 2, true>(p, stream)
               : launch_tile<T, X8, false, 128, 128, 2, 2, 2>(p, stream);
   if (rw) return launch_tile<T, X8, true, 64, 64, 2, 2, 4, true>(p, stream);
-  // The tile that takes least time by a count of rounds: a slice of 128 bytes takes a round of 256
-  // workgroups 1.86 us with tiles of 256 x 256 (one a compute unit), a round of 512 1.1 us (8 bits: 1.4)
-  // with 128 x 128 and 0.47 us with 64 x 64 (two a compute unit), measured at 8192 x 4096 x 4096.
+  // The tile that takes least time by a count of rounds, of 256 workgroups with tiles of 256 x 256 (one a compute
+  // unit) and of 512 with the others (two).  Measured at 8192 x 4096 x 4096, a slice of 128 bytes takes a round
+  // 1.84 us with 256 x 256 (8 bits: 2.10), 1.08 with 128 x 128 (1.23) and 0.43 with 64 x 64 (0.45); the rule
+  // takes 256 x 256 as equal in both types.
   auto rounds = [&](int side, int at_once) {
     const int64_t tiles = (int64_t)((p.rows + side - 1) / side) * ((p.out_dim + side - 1) / side);
     return (double)((tiles + at_once - 1) / at_once);
