@@ -18,6 +18,12 @@
  *                      heads; the new rows stand at the end of the
  *                      sequence's keys (a whole prompt, a chunk after a
  *                      history, a single token)
+ *   jdob_edge_cache_write, jdob_edge_cache_read
+ *                      new rows' keys and values into the pages of a
+ *                      cache, 16-bit or quantised to 8 bits, and back
+ *   jdob_edge_attend_paged
+ *                      causal attention of sequences' newest rows (a
+ *                      single token, a few at once) over such pages
  *
  * The conventions are those of jdob.h: array pointers are DEVICE pointers
  * owned by the caller; calls enqueue work on `hip_stream` and return without
@@ -163,6 +169,93 @@ typedef struct {
  * the sizes are read.                                                       */
 int64_t jdob_edge_attend_workspace(const jdob_edge_attend_args *a);
 int jdob_edge_attend(const jdob_edge_attend_args *a, void *hip_stream);
+
+/* A paged cache of keys and values.  Key j of a sequence stands on page
+ * table[j / page_size] of the sequence's row of a table, in slot
+ * j % page_size.  A key is absent where j / page_size is not below the table's
+ * width or the entry is outside [0, num_pages): pages that have been given
+ * back (keys behind a window) or not been taken yet.  Sequences may share
+ * pages that none of them writes.
+ * With bits8 = 0 k and v hold rows of dtype.  With bits8 = 1 they hold 8-bit
+ * codes that stand for code * scale of their slot and head:
+ *   scale = max|x| / 127,  code = x / scale (binary32 divisions) rounded to
+ * the nearest integer (to even) in [-127, 127]; zeros have scale 0, a row
+ * with a NaN or an infinity has codes 0 and scale NaN (below max|x| = 2^-119
+ * scales are subnormal and codes coarser).  dtype is then that of the rows
+ * outside the cache.  Slots that no row was written to may hold anything.   */
+#define JDOB_EDGE_MAX_PAGE_SIZE 65536
+
+typedef struct {
+  int32_t num_pages, page_size;   /* >= 0; 1 .. JDOB_EDGE_MAX_PAGE_SIZE      */
+  int32_t num_kv_heads, head_dim; /* 1 .. 1024; as in jdob_edge_attend       */
+  int32_t dtype;                  /* BF16 or F16                             */
+  int32_t bits8;                  /* 1: k and v are int8_t, with scales      */
+  void *k;                        /* [num_pages][num_kv_heads][page_size][head_dim] */
+  int64_t k_page_stride, k_head_stride, k_slot_stride; /* any order of the three */
+  void *v;
+  int64_t v_page_stride, v_head_stride, v_slot_stride;
+  float *k_scale;                 /* [num_pages][num_kv_heads][page_size], 8 bits only */
+  int64_t k_scale_page_stride, k_scale_head_stride, k_scale_slot_stride;
+  float *v_scale;
+  int64_t v_scale_page_stride, v_scale_head_stride, v_scale_slot_stride;
+} jdob_edge_cache;
+
+/* Sequence u has rows row_start[u] .. row_start[u+1]-1 of k and v (n of
+ * them), which are the last of its m = key_count[u] keys: its row i is key
+ * m - n + i.  jdob_edge_cache_write puts the rows into the cache; a row whose
+ * key is absent or negative, or that belongs to no sequence, is left out, and
+ * nothing else of the cache changes.  At most one row may be written to a
+ * slot.  jdob_edge_cache_read does the reverse with the same arguments:
+ * 8-bit rows become code * scale rounded to dtype, a row whose key is absent
+ * or negative becomes zeros, a row of no sequence is left as it was.        */
+typedef struct {
+  jdob_edge_cache cache;
+  int32_t num_sequences;          /* 0 .. JDOB_EDGE_MAX_SEQUENCES            */
+  int32_t table_width;            /* >= 0                                    */
+  const int32_t *table;           /* [num_sequences][table_width]            */
+  int64_t table_stride;           /* >= table_width                          */
+  const int32_t *row_start;       /* [num_sequences + 1], ascending          */
+  const int32_t *key_count;       /* [num_sequences]                         */
+  int32_t rows;                   /* of k and v                              */
+  void *k;                        /* [rows][num_kv_heads][head_dim]          */
+  int64_t k_stride, k_head_stride;
+  void *v;
+  int64_t v_stride, v_head_stride;
+} jdob_edge_cache_rows_args;
+
+int jdob_edge_cache_write(const jdob_edge_cache_rows_args *a, void *hip_stream);
+int jdob_edge_cache_read(const jdob_edge_cache_rows_args *a, void *hip_stream);
+
+/* jdob_edge_attend with keys and values on pages: sequence u's rows
+ * query_start[u] .. query_start[u+1]-1 stand at the end of its key_count[u]
+ * keys and see those of them that are there.  Made for few rows a sequence:
+ * the keys are read once for every 32 rows times heads of a key head.  All
+ * else is as in jdob_edge_attend; with an 8-bit cache p * scale of the value
+ * keeps 16 bits in its product with the codes.                              */
+typedef struct {
+  jdob_edge_cache cache;
+  int32_t num_sequences, table_width;
+  const int32_t *table;
+  int64_t table_stride;
+  const int32_t *query_start;     /* [num_sequences + 1], ascending          */
+  const int32_t *key_count;       /* [num_sequences]                         */
+  int32_t num_heads;              /* a multiple of num_kv_heads, to 1024     */
+  int32_t max_queries, max_keys;  /* >= 0, as in jdob_edge_attend            */
+  float scale;                    /* > 0, finite                             */
+  int64_t query_rows;             /* rows of q and out                       */
+  const void *q;                  /* [query_rows][num_heads][head_dim]       */
+  int64_t q_stride, q_head_stride;
+  void *out;                      /* [query_rows][num_heads][head_dim]       */
+  int64_t out_stride, out_head_stride; /* >= head_dim, where there is more than one */
+  void *workspace;                /* jdob_edge_attend_paged_workspace bytes  */
+  int64_t workspace_bytes;
+} jdob_edge_attend_paged_args;
+
+/* Bytes that jdob_edge_attend_paged needs (16-byte aligned; 0 where the keys
+ * are not split over workgroups); -1 where the arguments are not valid.  Only
+ * the sizes are read.                                                       */
+int64_t jdob_edge_attend_paged_workspace(const jdob_edge_attend_paged_args *a);
+int jdob_edge_attend_paged(const jdob_edge_attend_paged_args *a, void *hip_stream);
 
 #ifdef __cplusplus
 }

@@ -23,7 +23,8 @@ ROOT = os.path.dirname(HERE)
 # kernels and entry points of users sharing their parameters; heterogeneous users
 SOURCES = [os.path.join(HERE, "csrc", f) for f in ("jdob.hip", "jdob_hetero.hip")]
 # the edge operators (include/jdob_edge.h)
-EDGE_SOURCES = [os.path.join(HERE, "edge_csrc", f) for f in ("norm.hip", "project.hip", "attend.hip")]
+EDGE_SOURCES = [os.path.join(HERE, "edge_csrc", f) for f in ("norm.hip", "project.hip", "attend.hip", "cache.hip",
+                                                              "paged.hip")]
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libjdob.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

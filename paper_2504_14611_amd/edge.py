@@ -2,7 +2,9 @@
 
 What the edge GPU computes for the users that a policy offloads: `norm` (RMS norm of rows with the residual's
 addition, in the rows' type or in 8 bits with scales), `project` (the projection that all users share beside each
-row's low-rank adapter) and `attend` (causal attention of packed sequences of different lengths).
+row's low-rank adapter), `attend` (causal attention of packed sequences of different lengths), and what works on a paged
+cache of keys and values (`make_cache`): `cache_write` and `cache_read` (rows into it, quantised to 8 bits where it is of
+8 bits, and back) and `attend_paged` (attention of sequences' newest rows over it).
 
 Argument marshalling only, like paper_2504_14611_amd.jdob: the work runs in the HIP kernels of the library, and
 there is no fallback.  Tensors are device tensors (others are refused); outputs and workspaces that the caller does
@@ -13,6 +15,7 @@ also where an input requires gradients.  Refused arguments raise jdob.JdobError 
 
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 from typing import Dict, Optional
 
@@ -31,10 +34,12 @@ except ImportError:
 
 EDGE_BF16, EDGE_F16, EDGE_F32 = 0, 1, 2
 MAX_ROWS, MAX_NORM_DIM, MAX_RANK, MAX_HEAD_DIM, MAX_SEQUENCES = 1 << 30, 16384, 256, 128, 65535
+MAX_PAGE_SIZE = 65536
 _MAX_I32 = 0x7fffffff
 
 EXPORTS = ("jdob_edge_norm", "jdob_edge_project", "jdob_edge_project_workspace", "jdob_edge_attend",
-           "jdob_edge_attend_workspace")
+           "jdob_edge_attend_workspace", "jdob_edge_cache_write", "jdob_edge_cache_read", "jdob_edge_attend_paged",
+           "jdob_edge_attend_paged_workspace")
 
 _P, _I32, _I64, _F32 = C.c_void_p, C.c_int32, C.c_int64, C.c_float
 
@@ -62,6 +67,29 @@ class AttendArgs(C.Structure):
                 ("out_stride", _I64), ("out_head_stride", _I64), ("workspace", _P), ("workspace_bytes", _I64)]
 
 
+class Cache(C.Structure):
+    _fields_ = [("num_pages", _I32), ("page_size", _I32), ("num_kv_heads", _I32), ("head_dim", _I32), ("dtype", _I32),
+                ("bits8", _I32), ("k", _P), ("k_page_stride", _I64), ("k_head_stride", _I64), ("k_slot_stride", _I64),
+                ("v", _P), ("v_page_stride", _I64), ("v_head_stride", _I64), ("v_slot_stride", _I64), ("k_scale", _P),
+                ("k_scale_page_stride", _I64), ("k_scale_head_stride", _I64), ("k_scale_slot_stride", _I64),
+                ("v_scale", _P), ("v_scale_page_stride", _I64), ("v_scale_head_stride", _I64),
+                ("v_scale_slot_stride", _I64)]
+
+
+class CacheRowsArgs(C.Structure):
+    _fields_ = [("cache", Cache), ("num_sequences", _I32), ("table_width", _I32), ("table", _P), ("table_stride", _I64),
+                ("row_start", _P), ("key_count", _P), ("rows", _I32), ("k", _P), ("k_stride", _I64),
+                ("k_head_stride", _I64), ("v", _P), ("v_stride", _I64), ("v_head_stride", _I64)]
+
+
+class AttendPagedArgs(C.Structure):
+    _fields_ = [("cache", Cache), ("num_sequences", _I32), ("table_width", _I32), ("table", _P), ("table_stride", _I64),
+                ("query_start", _P), ("key_count", _P), ("num_heads", _I32), ("max_queries", _I32), ("max_keys", _I32),
+                ("scale", _F32), ("query_rows", _I64), ("q", _P), ("q_stride", _I64), ("q_head_stride", _I64),
+                ("out", _P), ("out_stride", _I64), ("out_head_stride", _I64), ("workspace", _P),
+                ("workspace_bytes", _I64)]
+
+
 _lib = None
 
 
@@ -70,10 +98,12 @@ def load():
     global _lib
     if _lib is None:
         lib = jdob.load()
-        for name, args in (("norm", NormArgs), ("project", ProjectArgs), ("attend", AttendArgs)):
+        for name, args in (("norm", NormArgs), ("project", ProjectArgs), ("attend", AttendArgs),
+                           ("cache_write", CacheRowsArgs), ("cache_read", CacheRowsArgs),
+                           ("attend_paged", AttendPagedArgs)):
             call = getattr(lib, "jdob_edge_" + name)
             call.argtypes, call.restype = [C.POINTER(args), C.c_void_p], C.c_int
-            if args is not NormArgs:
+            if args not in (NormArgs, CacheRowsArgs):
                 size = getattr(lib, f"jdob_edge_{name}_workspace")
                 size.argtypes, size.restype = [C.POINTER(args)], C.c_int64
         _lib = lib
@@ -326,6 +356,184 @@ def _attend(a, where, shape, dtype, dev, out, workspace, handle):
     lib = _lib or load()
     workspace = _workspace(a, workspace, lib.jdob_edge_attend_workspace, dev, where)
     code = lib.jdob_edge_attend(C.byref(a), handle)
+    if code:
+        jdob._check(code, where)
+    return out
+
+
+def make_cache(pages: int, page_size: int, kv_heads: int, dim: int, dtype=torch.bfloat16, bits8: bool = False,
+               device="cuda") -> Dict[str, object]:
+    """A paged cache as the calls below take it: `k` and `v` [pages, kv_heads, page_size, dim] of `dtype`, or with bits8
+    of int8 beside `k_scale` and `v_scale` [pages, kv_heads, page_size] (float32).  Nothing is set: keys that were not
+    written are never seen.  Any tensors of these shapes will do, views of others among them (only the last dimension of
+    k and v has to be contiguous); this order of dimensions reads fastest, and page sizes that are multiples of 16."""
+    where = "make_cache"
+    if min(pages, page_size, kv_heads, dim) < 0 or not (page_size and kv_heads and dim):
+        _refuse(where, f"{pages} pages of {page_size} keys, {kv_heads} heads of {dim}")
+    _dtype(dtype, where)
+    if page_size > MAX_PAGE_SIZE or pages > _MAX_I32 or kv_heads > 1024 or dim > MAX_HEAD_DIM or dim % 8:
+        _refuse(where, f"{pages} pages of {page_size} keys, {kv_heads} heads of {dim}", jdob.JDOB_ERR_UNSUPPORTED)
+    shape = (pages, kv_heads, page_size, dim)
+    kind = torch.int8 if bits8 else dtype
+    cache = {name: torch.empty(shape, dtype=kind, device=device) for name in ("k", "v")}
+    for name in ("k_scale", "v_scale"):
+        cache[name] = torch.empty(shape[:3], dtype=torch.float32, device=device) if bits8 else None
+    return cache
+
+
+def _strides4(t, where: str, name: str, shape, dtype, device):
+    """Pointer and strides of pages, heads and slots; of a dimension with one entry the stride is never used."""
+    if t is None:
+        _refuse(where, f"the cache has no {name}")
+    if t.dtype is not dtype or t.shape != shape or t.device != device:
+        _refuse(where, f"the cache's {name} is {tuple(t.shape)} {t.dtype} on {t.device}, "
+                       f"expected {tuple(shape)} {dtype} on {device}")
+    return (t.data_ptr(), *t.stride()[:3])
+
+
+def _cache(cache: dict, where: str, dtype, table, row_start, key_count):
+    """The cache as the library takes it, and the sequences' part of the arguments."""
+    k, v = cache["k"], cache["v"]
+    if k.dim() != 4:
+        _refuse(where, "the cache's k and v are [pages, heads, page size, columns]")
+    shape, kind, dev = k.shape, k.dtype, k.device
+    bits8 = kind is torch.int8
+    if not bits8 and kind is not dtype:
+        _refuse(where, f"the cache is {kind}, expected {dtype} or int8")
+    pages, g, size, d = shape
+    if pages > _MAX_I32 or g > 1024 or size > MAX_PAGE_SIZE or d > MAX_HEAD_DIM or d % 8:
+        _refuse(where, f"{pages} pages of {size} keys, {g} heads of {d}", jdob.JDOB_ERR_UNSUPPORTED)
+    if (k.stride(3) != 1 or v.stride(-1) != 1) and d > 1:
+        _refuse(where, "the cache's last dimension is not contiguous")
+    c = Cache(pages, size, g, d, _dtype(dtype, where), bits8, *_strides4(k, where, "k", shape, kind, dev),
+              *_strides4(v, where, "v", shape, kind, dev))
+    if bits8:
+        c.k_scale, c.k_scale_page_stride, c.k_scale_head_stride, c.k_scale_slot_stride = \
+            _strides4(cache.get("k_scale"), where, "k_scale", shape[:3], torch.float32, dev)
+        c.v_scale, c.v_scale_page_stride, c.v_scale_head_stride, c.v_scale_slot_stride = \
+            _strides4(cache.get("v_scale"), where, "v_scale", shape[:3], torch.float32, dev)
+    elif cache.get("k_scale") is not None or cache.get("v_scale") is not None:
+        _refuse(where, "scales belong to an 8-bit cache")
+    if table.dim() != 2:
+        _refuse(where, "table is [sequences, pages]")
+    n, width = table.shape
+    if n > MAX_SEQUENCES or width > _MAX_I32:
+        _refuse(where, f"{n} sequences of {width} pages", jdob.JDOB_ERR_UNSUPPORTED)
+    return (c, n, width, _array(table, where, "table", (n, width), torch.int32, dev), _row_stride(table, width),
+            _dense(row_start, where, "row_start", (n + 1,), torch.int32, dev),
+            _dense(key_count, where, "key_count", (n,), torch.int32, dev))
+
+
+def cache_write(k, v, cache: dict, table, row_start, key_count, stream=None) -> None:
+    """jdob_edge_cache_write: rows k and v [rows, kv_heads, dim] (any row and head strides) into the cache's pages.
+    Sequence u's rows row_start[u] .. row_start[u+1] are the last of its key_count[u] keys; key j stands on page
+    table[u][j // page_size], and rows whose entry is no page are left out.  table [n, width] int32, row_start [n + 1]
+    int32, key_count [n] int32.  No two rows may go to one slot."""
+    where = "jdob_edge_cache_write"
+    if k.dim() != 3:
+        _refuse(where, "k and v have rows, heads and columns")
+    _rows(cache, where, k.dtype, k, v, table, row_start, key_count, stream)
+
+
+def cache_read(cache: dict, table, row_start, key_count, rows: Optional[int] = None, dtype=None,
+               into: Optional[dict] = None, stream=None):
+    """jdob_edge_cache_read: the reverse of cache_write with the same arguments.  Returns k and v [rows, kv_heads, dim]:
+    8-bit rows as the values that they stand for, rounded to `dtype` (default: a 16-bit cache's own, else bfloat16);
+    rows whose key is absent are zeros.  `into` holds the caller's own `k` and `v` (rows of no sequence stay as they
+    were); else `rows` is how many to allocate, which row_start on the GPU says, too, but not without waiting for it:
+    row_start's last entry (further ones stay unset)."""
+    where = "jdob_edge_cache_read"
+    k, v = (into.get("k"), into.get("v")) if into else (None, None)
+    kind, dev = cache["k"].dtype, cache["k"].device
+    if dtype is None:
+        dtype = k.dtype if k is not None else torch.bfloat16 if kind is torch.int8 else kind
+    if k is None or v is None:
+        given = v if k is None else k
+        if cache["k"].dim() != 4:
+            _refuse(where, "the cache's k and v are [pages, heads, page size, columns]")
+        if given is None and (rows is None or rows < 0):
+            _refuse(where, f"rows is {rows}, and no buffer is given")
+        shape = (rows if given is None else given.shape[0], cache["k"].shape[1], cache["k"].shape[3])
+        _dtype(dtype, where)
+        with _allocating(dev, stream, where):
+            k = torch.empty(shape, dtype=dtype, device=dev) if k is None else k
+            v = torch.empty(shape, dtype=dtype, device=dev) if v is None else v
+    if k.dim() != 3 or (rows is not None and k.shape[0] != rows):
+        _refuse(where, f"k is {tuple(k.shape)}, expected {rows} rows, heads and columns")
+    _rows(cache, where, dtype, k, v, table, row_start, key_count, stream)
+    return k, v
+
+
+def _allocating(device, stream, where: str):
+    """The context in which a call's outputs are allocated."""
+    return _enter(device, stream, where)[1] or contextlib.nullcontext()
+
+
+def _rows(cache, where, dtype, k, v, table, row_start, key_count, stream):
+    dev = k.device
+    rows = k.shape[0]
+    if rows > MAX_ROWS:
+        _refuse(where, f"{rows} rows", jdob.JDOB_ERR_UNSUPPORTED)
+    part = _cache(cache, where, dtype, table, row_start, key_count)
+    shape = (rows, part[0].num_kv_heads, part[0].head_dim)
+    if cache["k"].device != dev:
+        _refuse(where, f"the cache is on {cache['k'].device}, expected {dev}")
+    a = CacheRowsArgs(*part, rows, _array(k, where, "k", shape, dtype, dev), k.stride(0), k.stride(1),
+                      _array(v, where, "v", shape, dtype, dev), v.stride(0), v.stride(1))
+    handle, context = _enter(dev, stream, where)
+    lib = _lib or load()
+    call = lib.jdob_edge_cache_write if where == "jdob_edge_cache_write" else lib.jdob_edge_cache_read
+    if context is not None:
+        with context:
+            code = call(C.byref(a), handle)
+    else:
+        code = call(C.byref(a), handle)
+    if code:
+        jdob._check(code, where)
+
+
+def attend_paged(q, cache: dict, table, query_start, key_count, scale: Optional[float] = None,
+                 max_queries: Optional[int] = None, max_keys: Optional[int] = None, out=None, workspace=None, stream=None):
+    """jdob_edge_attend_paged: causal attention of sequences' newest rows, q [rows, heads, dim] (any row and head
+    strides), over a paged cache.  Sequence u's rows query_start[u] .. query_start[u+1] stand at the end of its
+    key_count[u] keys; key j stands on page table[u][j // page_size] and is not seen where that is no page.  The rows'
+    own keys have been written before (cache_write).  Made for few rows a sequence; many go through cache_read and
+    attend.  scale defaults to dim ** -0.5; max_queries and max_keys are at least the largest sequence's (default: all
+    rows, all that the table has room for) and worth giving.  Returns out [rows, heads, dim]."""
+    where = "jdob_edge_attend_paged"
+    if q.dim() != 3:
+        _refuse(where, "q has rows, heads and columns")
+    shape, dtype, dev = q.shape, q.dtype, q.device
+    rows, h, d = shape
+    if rows > MAX_ROWS:
+        _refuse(where, f"{rows} rows", jdob.JDOB_ERR_UNSUPPORTED)
+    part = _cache(cache, where, dtype, table, query_start, key_count)
+    c, n, width = part[:3]
+    if cache["k"].device != dev or c.head_dim != d:
+        _refuse(where, f"the cache has heads of {c.head_dim} on {cache['k'].device}, expected {d} on {dev}")
+    most = rows if max_queries is None else max_queries
+    longest = width * c.page_size if max_keys is None else max_keys
+    if most < 0 or longest < 0:
+        _refuse(where, f"max_queries {most}, max_keys {longest}")
+    a = AttendPagedArgs(*part, h, min(most, _MAX_I32), min(longest, _MAX_I32), d ** -0.5 if scale is None else scale,
+                        rows, _array(q, where, "q", shape, dtype, dev), q.stride(0), q.stride(1))
+    handle, context = _enter(dev, stream, where)
+    if context is not None:
+        with context:
+            return _attend_paged(a, where, shape, dtype, dev, out, workspace, handle)
+    return _attend_paged(a, where, shape, dtype, dev, out, workspace, handle)
+
+
+def _attend_paged(a, where, shape, dtype, dev, out, workspace, handle):
+    if out is None:
+        out = torch.empty(shape, dtype=dtype, device=dev)
+        a.out = out.data_ptr()
+    else:
+        a.out = _array(out, where, "out", shape, dtype, dev)
+    a.out_stride, a.out_head_stride = out.stride(0), out.stride(1)
+    lib = _lib or load()
+    workspace = _workspace(a, workspace, lib.jdob_edge_attend_paged_workspace, dev, where)
+    code = lib.jdob_edge_attend_paged(C.byref(a), handle)
     if code:
         jdob._check(code, where)
     return out
