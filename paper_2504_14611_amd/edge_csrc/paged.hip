@@ -109,6 +109,7 @@ struct Anywhere {
     }
   }
 
+  __device__ void find(int64_t) {}
   __device__ void load(Tile<DP, BITS8> &t, int64_t first) const {
     typedef typename std::conditional<BITS8, int8_t, unsigned short>::type E;
     constexpr int N = BITS8 ? 4 : 2;  // elements a word
@@ -152,6 +153,121 @@ struct Anywhere {
   }
 };
 
+// A stretch of memory from `at` on: what is read from behind its end is zero and does not touch memory.  Both are the
+// same for all lanes of the wave.
+__device__ inline __amdgpu_buffer_rsrc_t window(const void *at, int bytes) {
+  const uint64_t a = (uint64_t)at;
+  const uint64_t same = (uint64_t)__builtin_amdgcn_readfirstlane((unsigned)(a >> 32)) << 32 |
+                        (unsigned)__builtin_amdgcn_readfirstlane((unsigned)a);
+  return __builtin_amdgcn_make_buffer_rsrc((void *)same, 0, __builtin_amdgcn_readfirstlane(bytes), 0x00020000);
+}
+template <int BYTES>
+__device__ inline void window_load(unsigned *to, __amdgpu_buffer_rsrc_t w, unsigned offset) {
+  if constexpr (BYTES == 16) {
+    const u32x4 x = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(w, offset, 0, 0));
+    to[0] = x[0], to[1] = x[1], to[2] = x[2], to[3] = x[3];
+  } else if constexpr (BYTES == 8) {
+    const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(w, offset, 0, 0));
+    to[0] = x[0], to[1] = x[1];
+  } else if constexpr (BYTES == 4) {
+    *to = __builtin_amdgcn_raw_buffer_load_b32(w, offset, 0, 0);
+  } else {
+    *to = (unsigned short)__builtin_amdgcn_raw_buffer_load_b16(w, offset, 0, 0);
+  }
+}
+
+// The same where 16 keys that start at a multiple of 16 stand side by side on one page, and their rows at multiples of
+// 16 bytes: the page is looked up once for all lanes, a lane's offsets within the 16 rows stay the same from tile to
+// tile, and rows behind the last key, or of a page that is not there, are kept out by the end of a window.
+template <typename T, int DP, bool BITS8>
+struct InPages {
+  typedef typename std::conditional<BITS8, int8_t, unsigned short>::type E;
+  static constexpr int SZ = sizeof(E), NK = BITS8 ? (DP + 32) / 64 : DP / 32, NV = DP == 96 ? 2 : 1;
+  static constexpr unsigned BEHIND = 0x80000000u;  // behind any window's end
+  const PagedParams &p;
+  int u, head, until;
+  unsigned k_at[NK], v_at[4][NV];
+  struct Spot {
+    int page[2], slot[2];
+  } spot;  // of the next tile
+
+  __device__ InPages(const PagedParams &p, int u, int head, int until) : p(p), u(u), head(head), until(until) {
+    const int l16 = threadIdx.x % 16, g = threadIdx.x % WAVE / 16, dim = p.c.dim;
+#pragma unroll
+    for (int i = 0; i < NK; ++i) {
+      const int e = key_element<DP, BITS8>(BITS8 ? 2 * i : i, g);
+      k_at[i] = e < dim ? (unsigned)(l16 * p.c.k.slot + e) * SZ : BEHIND;
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const unsigned row = (unsigned)((g * 4 + r) * p.c.v.slot);
+      if constexpr (DP == 96) {
+        v_at[r][0] = l16 * 4 < dim ? (row + l16 * 4) * SZ : BEHIND;
+        v_at[r][1] = 64 + l16 * 2 < dim ? (row + 64 + l16 * 2) * SZ : BEHIND;
+      } else {
+        v_at[r][0] = l16 * (DP / 16) < dim ? (row + l16 * (DP / 16)) * SZ : BEHIND;
+      }
+    }
+  }
+
+  __device__ void find(int64_t first) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      spot.page[h] = -1;
+      spot.slot[h] = 0;
+      if (first + h * 16 < until)
+        spot.page[h] = __builtin_amdgcn_readfirstlane(page_of(p.c, u, (int)first + h * 16, &spot.slot[h]));
+    }
+  }
+
+  __device__ void load(Tile<DP, BITS8> &t, int64_t first) const {
+    t.gone = 0;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int page = spot.page[h], slot = spot.slot[h];
+      const int64_t behind = until - (first + h * 16);
+      const int rows = page < 0 ? 0 : behind < 16 ? (int)behind : 16;  // (a page only where there are keys)
+      const E *const k = (const E *)p.c.k.at + page * p.c.k.page + head * p.c.k.head + slot * p.c.k.slot;
+      const E *const v = (const E *)p.c.v.at + page * p.c.v.page + head * p.c.v.head + slot * p.c.v.slot;
+      const auto kw = window(k, rows ? (int)((rows - 1) * p.c.k.slot + p.c.dim) * SZ : 0);
+      const auto vw = window(v, rows ? (int)((rows - 1) * p.c.v.slot + p.c.dim) * SZ : 0);
+#pragma unroll
+      for (int i = 0; i < NK; ++i) {
+        if constexpr (BITS8) {
+          if (i * 64 + 64 <= DP) {
+            window_load<16>(t.k[h] + i * 4, kw, k_at[i]);
+          } else {
+            window_load<8>(t.k[h] + i * 4, kw, k_at[i]);
+          }
+        } else {
+          window_load<16>(t.k[h] + i * 4, kw, k_at[i]);
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        unsigned *const to = t.v[h * 4 + r];
+        if constexpr (DP == 96) {
+          window_load<4 * SZ>(to, vw, v_at[r][0]);
+          window_load<2 * SZ>(to + SZ, vw, v_at[r][1]);
+        } else {
+          window_load<DP / 16 * SZ>(to, vw, v_at[r][0]);
+        }
+      }
+      if constexpr (BITS8) {
+        // (all 16 are on the page, those behind the last key among them)
+        const float *const ks = p.c.k.scale + page * p.c.k.scale_page + head * p.c.k.scale_head + slot;
+        const float *const vs = p.c.v.scale + page * p.c.v.scale_page + head * p.c.v.scale_head + slot;
+        unsigned w[2][4];
+        window_load<16>(w[0], window(ks, rows ? 64 : 0), threadIdx.x % WAVE / 16 * 16);
+        window_load<16>(w[1], window(vs, rows ? 64 : 0), threadIdx.x % WAVE / 16 * 16);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) t.k_scale[h][r] = __uint_as_float(w[0][r]), t.v_scale[h][r] = __uint_as_float(w[1][r]);
+      }
+      t.gone |= page < 0 ? 0xfu << (h * 4) : 0;
+    }
+  }
+};
+
 // The running state of 16 columns in a wave: lanes l % 16 + 16 g hold column l % 16.
 template <int DP>
 struct State16 {
@@ -163,8 +279,11 @@ __device__ inline float base_of(float top) { return top == -INFINITY ? 0.0f : to
 
 // What the four lanes of a column hold, put together.
 __device__ inline float column_max(float x) {
-  x = fmaxf(x, __shfl_xor(x, 16));
-  return fmaxf(x, __shfl_xor(x, 32));
+  const unsigned a = __float_as_uint(x);
+  const auto b = __builtin_amdgcn_permlane16_swap(a, a, false, false);
+  const unsigned c = __float_as_uint(fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1])));
+  const auto d = __builtin_amdgcn_permlane32_swap(c, c, false, false);
+  return fmaxf(__uint_as_float(d[0]), __uint_as_float(d[1]));
 }
 __device__ inline float column_sum(float x) {
   x += __shfl_xor(x, 16);
@@ -338,8 +457,8 @@ __device__ inline void add_non_finite(const PagedParams &p, State16<DP> (&s)[CT]
 
 constexpr int PAGED_WAVES = 4, TILE_KEYS = 32;
 
-template <typename T, int DP, bool BITS8, int CT>
-__global__ __launch_bounds__(PAGED_WAVES *WAVE, 2) void paged_kernel(PagedParams p) {
+template <typename T, int DP, bool BITS8, int CT, bool IN_PAGES>
+__global__ __launch_bounds__(PAGED_WAVES *WAVE, CT == 1 ? 2 : 1) void paged_kernel(PagedParams p) {
   typedef typename Mma16<T>::frag frag;
   constexpr int THREADS = PAGED_WAVES * WAVE, COLUMNS = 16 * CT, PITCH = DP + 4;
   __shared__ __align__(16) float mix[PAGED_WAVES * COLUMNS * PITCH];
@@ -383,12 +502,16 @@ __global__ __launch_bounds__(PAGED_WAVES *WAVE, 2) void paged_kernel(PagedParams
     for (int i = 0; i < DP / 16; ++i) s[c].out[i] = (f32x4){};
   }
   const int first_limit = shift + first_row;
-  const Anywhere<T, DP, BITS8> cache(p, u, kv, (int)until);
+  typedef typename std::conditional<IN_PAGES, InPages<T, DP, BITS8>, Anywhere<T, DP, BITS8>>::type Cache;
+  constexpr int STEP = PAGED_WAVES * TILE_KEYS;
+  Cache cache(p, u, kv, (int)until);
   int64_t first = from + wave * TILE_KEYS;  // passes 2^31 behind the longest sequence's end
-  Tile<DP, BITS8> now, next;
-  cache.load(now, first);
-  for (; first < until; first += PAGED_WAVES * TILE_KEYS) {
-    cache.load(next, first + PAGED_WAVES * TILE_KEYS);
+  Tile<DP, BITS8> even, odd;
+  // Takes the tile at `first`, while the next one is loaded and the page of the one behind that is looked up.
+  auto take = [&](Tile<DP, BITS8> &now, Tile<DP, BITS8> &next) {
+    cache.load(next, first + STEP);
+    cache.find(first + 2 * STEP);
+    __builtin_amdgcn_sched_barrier(0);
     int sees[CT];
 #pragma unroll
     for (int c = 0; c < CT; ++c) sees[c] = (int)((limit[c] < until ? limit[c] : until - 1) - first);
@@ -401,7 +524,15 @@ __global__ __launch_bounds__(PAGED_WAVES *WAVE, 2) void paged_kernel(PagedParams
       }
       attend_tile<T, DP, BITS8, CT, true>(s, qf, now, sees, p.scale);
     }
-    now = next;
+    first += STEP;
+  };
+  cache.find(first);
+  cache.load(even, first);
+  cache.find(first + STEP);
+  while (first < until) {
+    take(even, odd);
+    if (first >= until) break;
+    take(odd, even);
   }
   // the waves' results: each column's maximum, then sums and outputs relative to it
 #pragma unroll
@@ -549,22 +680,36 @@ PagedPlan paged_plan(const jdob_edge_attend_paged_args *a) {
 }
 
 template <typename T, int DP, bool BITS8>
-int paged(const PagedParams &p, int columns, int64_t blocks, hipStream_t stream) {
-  return columns == 16 ? launch(paged_kernel<T, DP, BITS8, 1>, blocks, PAGED_WAVES * WAVE, stream, p)
-                       : launch(paged_kernel<T, DP, BITS8, 2>, blocks, PAGED_WAVES * WAVE, stream, p);
+int paged(const PagedParams &p, int columns, bool in_pages, int64_t blocks, hipStream_t stream) {
+  if (columns == 16)
+    return launch(in_pages ? paged_kernel<T, DP, BITS8, 1, true> : paged_kernel<T, DP, BITS8, 1, false>, blocks,
+                  PAGED_WAVES * WAVE, stream, p);
+  return launch(in_pages ? paged_kernel<T, DP, BITS8, 2, true> : paged_kernel<T, DP, BITS8, 2, false>, blocks,
+                PAGED_WAVES * WAVE, stream, p);
+}
+
+// Whether a pool's rows can be read as InPages reads them; 16 rows have to stay within a window, whose offsets pass
+// 2^31 nowhere.
+bool in_pages(const Pool &x, bool bits8) {
+  const int64_t unit = bits8 ? 16 : 8;
+  return (uintptr_t)x.at % 16 == 0 && x.page % unit == 0 && x.head % unit == 0 && x.slot % unit == 0 && x.slot < (1 << 24) &&
+         (!bits8 || x.scale_slot == 1);
 }
 
 template <typename T, bool BITS8>
 int paged(const PagedParams &p, const PagedPlan &f, hipStream_t stream) {
+  // (8-bit keys are read 16 elements at once up to 64, and beyond 96 to 128)
+  const bool in = p.c.page_size % 16 == 0 && in_pages(p.c.k, BITS8) && in_pages(p.c.v, BITS8) &&
+                  (!BITS8 || p.c.dim % 16 == 0 || (p.c.dim > 64 && p.c.dim <= 96));
   const int64_t groups = (int64_t)p.c.sequences * p.c.kv_heads * f.tiles;
   const int64_t all = (int64_t)p.c.sequences * p.c.kv_heads * f.queries * p.group;
   // (each factor is below 2^31, and tiles are fewer than columns)
   if (f.tiles > MAX_BLOCKS || groups > MAX_BLOCKS || groups * f.splits > MAX_BLOCKS || (f.splits > 1 && all > MAX_BLOCKS))
     return JDOB_ERR_UNSUPPORTED;
   const int64_t blocks = groups * f.splits;
-  const int code = p.c.dim <= 64   ? paged<T, 64, BITS8>(p, f.columns, blocks, stream)
-                   : p.c.dim <= 96 ? paged<T, 96, BITS8>(p, f.columns, blocks, stream)
-                                   : paged<T, 128, BITS8>(p, f.columns, blocks, stream);
+  const int code = p.c.dim <= 64   ? paged<T, 64, BITS8>(p, f.columns, in, blocks, stream)
+                   : p.c.dim <= 96 ? paged<T, 96, BITS8>(p, f.columns, in, blocks, stream)
+                                   : paged<T, 128, BITS8>(p, f.columns, in, blocks, stream);
   if (code != JDOB_OK || f.splits == 1) return code;
   return launch(paged_join_kernel<T>, all, JOIN_THREADS, stream, p);
 }

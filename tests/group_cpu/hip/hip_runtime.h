@@ -307,6 +307,7 @@ inline V __shfl_up(V v, int d) {
 #define __builtin_amdgcn_exp2f(x) exp2f(x)
 #define __builtin_amdgcn_frexp_expf(x) group_cpu_exponent(x)
 #define __builtin_amdgcn_permlane32_swap(a, b, fi, bc) group_cpu_swap32(a, b)
+#define __builtin_amdgcn_permlane16_swap(a, b, fi, bc) group_cpu_swap16(a, b)
 #define __builtin_amdgcn_ds_read_tr16_b64_v4i16(p) group_cpu_transposed(p)
 #define __builtin_amdgcn_readfirstlane(v) group_cpu_first(v)
 #define __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, x, y, z) group_cpu_mfma<16, 8, __bf16, float>(a, b, c)
@@ -315,6 +316,29 @@ inline V __shfl_up(V v, int d) {
 #define __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, x, y, z) group_cpu_mfma<32, 8, _Float16, float>(a, b, c)
 #define __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, x, y, z) group_cpu_mfma<16, 16, signed char, unsigned>(a, b, c)
 #define __builtin_amdgcn_mfma_i32_32x32x32_i8(a, b, c, x, y, z) group_cpu_mfma<32, 16, signed char, unsigned>(a, b, c)
+
+// A window of memory: what is read from behind its end is zero, and nothing stands half behind it.
+struct group_cpu_window {
+  const char *at;
+  unsigned bytes;
+};
+#define __amdgpu_buffer_rsrc_t group_cpu_window
+#define __builtin_amdgcn_make_buffer_rsrc(p, stride, n, flags) (group_cpu_window{(const char *)(p), (unsigned)(n)})
+template <typename V>
+inline V group_cpu_window_load(group_cpu_window w, unsigned offset) {
+  V v;
+  memset(&v, 0, sizeof v);
+  if (offset >= w.bytes) return v;
+  if (w.bytes - offset < sizeof v) group_cpu::die("a load stands half behind a window's end");
+  memcpy(&v, w.at + offset, sizeof v);
+  return v;
+}
+typedef unsigned group_cpu_u2 __attribute__((ext_vector_type(2)));
+typedef unsigned group_cpu_u4 __attribute__((ext_vector_type(4)));
+#define __builtin_amdgcn_raw_buffer_load_b16(w, v, s, a) group_cpu_window_load<unsigned short>(w, (v) + (s))
+#define __builtin_amdgcn_raw_buffer_load_b32(w, v, s, a) group_cpu_window_load<unsigned>(w, (v) + (s))
+#define __builtin_amdgcn_raw_buffer_load_b64(w, v, s, a) group_cpu_window_load<group_cpu_u2>(w, (v) + (s))
+#define __builtin_amdgcn_raw_buffer_load_b128(w, v, s, a) group_cpu_window_load<group_cpu_u4>(w, (v) + (s))
 
 inline int group_cpu_exponent(float x) {
   int e = 0;
@@ -334,6 +358,11 @@ inline group_cpu_two group_cpu_swap32(unsigned a, unsigned b) {
   const int l = group_cpu::g().lane % 64;
   const unsigned lo = group_cpu::of_lane("permlane32", b, l & 31), hi = group_cpu::of_lane("permlane32", a, l | 32);
   return {{l < 32 ? a : lo, l < 32 ? hi : b}};
+}
+inline group_cpu_two group_cpu_swap16(unsigned a, unsigned b) {  // odd rows of 16 of a and even rows of b change places
+  const int l = group_cpu::g().lane % 64;
+  const unsigned lo = group_cpu::of_lane("permlane16", b, l & ~16), hi = group_cpu::of_lane("permlane16", a, l | 16);
+  return {{l & 16 ? lo : a, l & 16 ? b : hi}};
 }
 // Sixteen lanes' eight bytes are four rows of sixteen elements; a lane gets its column.
 template <typename V>
