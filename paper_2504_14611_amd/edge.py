@@ -381,47 +381,57 @@ def make_cache(pages: int, page_size: int, kv_heads: int, dim: int, dtype=torch.
     return cache
 
 
-def _strides4(t, where: str, name: str, shape, dtype, device):
-    """Pointer and strides of pages, heads and slots; of a dimension with one entry the stride is never used."""
+def _differs(t, where: str, name: str, shape, dtype, device):
     if t is None:
         _refuse(where, f"the cache has no {name}")
-    if t.dtype is not dtype or t.shape != shape or t.device != device:
-        _refuse(where, f"the cache's {name} is {tuple(t.shape)} {t.dtype} on {t.device}, "
-                       f"expected {tuple(shape)} {dtype} on {device}")
-    return (t.data_ptr(), *t.stride()[:3])
+    _refuse(where, f"the cache's {name} is {tuple(t.shape)} {t.dtype} on {t.device}, "
+                   f"expected {tuple(shape)} {dtype} on {device}")
 
 
-def _cache(cache: dict, where: str, dtype, table, row_start, key_count):
-    """The cache as the library takes it, and the sequences' part of the arguments."""
+def _cache(cache: dict, where: str, dtype, device, table, row_start, key_count):
+    """The cache as the library takes it, and the sequences' part of the arguments.  (Of a dimension with one entry the
+    library never uses the stride.)"""
     k, v = cache["k"], cache["v"]
-    if k.dim() != 4:
+    shape, kind = k.shape, k.dtype
+    if len(shape) != 4:
         _refuse(where, "the cache's k and v are [pages, heads, page size, columns]")
-    shape, kind, dev = k.shape, k.dtype, k.device
+    pages, g, size, d = shape
     bits8 = kind is torch.int8
     if not bits8 and kind is not dtype:
         _refuse(where, f"the cache is {kind}, expected {dtype} or int8")
-    pages, g, size, d = shape
+    if k.device != device:
+        _refuse(where, f"the cache is on {k.device}, expected {device}")
+    if v.shape != shape or v.dtype is not kind or v.device != device:
+        _differs(v, where, "v", shape, kind, device)
     if pages > _MAX_I32 or g > 1024 or size > MAX_PAGE_SIZE or d > MAX_HEAD_DIM or d % 8:
         _refuse(where, f"{pages} pages of {size} keys, {g} heads of {d}", jdob.JDOB_ERR_UNSUPPORTED)
-    if (k.stride(3) != 1 or v.stride(-1) != 1) and d > 1:
+    k_page, k_head, k_slot, k_one = k.stride()
+    v_page, v_head, v_slot, v_one = v.stride()
+    if k_one != 1 or v_one != 1:
         _refuse(where, "the cache's last dimension is not contiguous")
-    c = Cache(pages, size, g, d, _dtype(dtype, where), bits8, *_strides4(k, where, "k", shape, kind, dev),
-              *_strides4(v, where, "v", shape, kind, dev))
+    ks, vs = cache.get("k_scale"), cache.get("v_scale")
     if bits8:
-        c.k_scale, c.k_scale_page_stride, c.k_scale_head_stride, c.k_scale_slot_stride = \
-            _strides4(cache.get("k_scale"), where, "k_scale", shape[:3], torch.float32, dev)
-        c.v_scale, c.v_scale_page_stride, c.v_scale_head_stride, c.v_scale_slot_stride = \
-            _strides4(cache.get("v_scale"), where, "v_scale", shape[:3], torch.float32, dev)
-    elif cache.get("k_scale") is not None or cache.get("v_scale") is not None:
-        _refuse(where, "scales belong to an 8-bit cache")
-    if table.dim() != 2:
+        some = shape[:3]
+        if ks is None or ks.shape != some or ks.dtype is not torch.float32 or ks.device != device:
+            _differs(ks, where, "k_scale", some, torch.float32, device)
+        if vs is None or vs.shape != some or vs.dtype is not torch.float32 or vs.device != device:
+            _differs(vs, where, "v_scale", some, torch.float32, device)
+        c = Cache(pages, size, g, d, _dtype(dtype, where), 1, k.data_ptr(), k_page, k_head, k_slot, v.data_ptr(), v_page,
+                  v_head, v_slot, ks.data_ptr(), *ks.stride(), vs.data_ptr(), *vs.stride())
+    else:
+        if ks is not None or vs is not None:
+            _refuse(where, "scales belong to an 8-bit cache")
+        c = Cache(pages, size, g, d, _dtype(dtype, where), 0, k.data_ptr(), k_page, k_head, k_slot, v.data_ptr(), v_page,
+                  v_head, v_slot)
+    shape = table.shape
+    if len(shape) != 2:
         _refuse(where, "table is [sequences, pages]")
-    n, width = table.shape
+    n, width = shape
     if n > MAX_SEQUENCES or width > _MAX_I32:
         _refuse(where, f"{n} sequences of {width} pages", jdob.JDOB_ERR_UNSUPPORTED)
-    return (c, n, width, _array(table, where, "table", (n, width), torch.int32, dev), _row_stride(table, width),
-            _dense(row_start, where, "row_start", (n + 1,), torch.int32, dev),
-            _dense(key_count, where, "key_count", (n,), torch.int32, dev))
+    return (c, n, width, _array(table, where, "table", shape, torch.int32, device), _row_stride(table, width),
+            _dense(row_start, where, "row_start", (n + 1,), torch.int32, device),
+            _dense(key_count, where, "key_count", (n,), torch.int32, device))
 
 
 def cache_write(k, v, cache: dict, table, row_start, key_count, stream=None) -> None:
@@ -443,19 +453,20 @@ def cache_read(cache: dict, table, row_start, key_count, rows: Optional[int] = N
     were); else `rows` is how many to allocate, which row_start on the GPU says, too, but not without waiting for it:
     row_start's last entry (further ones stay unset)."""
     where = "jdob_edge_cache_read"
+    held = cache["k"]
     k, v = (into.get("k"), into.get("v")) if into else (None, None)
-    kind, dev = cache["k"].dtype, cache["k"].device
     if dtype is None:
-        dtype = k.dtype if k is not None else torch.bfloat16 if kind is torch.int8 else kind
+        dtype = k.dtype if k is not None else torch.bfloat16 if held.dtype is torch.int8 else held.dtype
     if k is None or v is None:
         given = v if k is None else k
-        if cache["k"].dim() != 4:
+        if len(held.shape) != 4:
             _refuse(where, "the cache's k and v are [pages, heads, page size, columns]")
         if given is None and (rows is None or rows < 0):
             _refuse(where, f"rows is {rows}, and no buffer is given")
-        shape = (rows if given is None else given.shape[0], cache["k"].shape[1], cache["k"].shape[3])
         _dtype(dtype, where)
-        with _allocating(dev, stream, where):
+        shape, dev = (rows if given is None else given.shape[0], held.shape[1], held.shape[3]), held.device
+        context = _enter(dev, stream, where)[1]
+        with context if context is not None else contextlib.nullcontext():
             k = torch.empty(shape, dtype=dtype, device=dev) if k is None else k
             v = torch.empty(shape, dtype=dtype, device=dev) if v is None else v
     if k.dim() != 3 or (rows is not None and k.shape[0] != rows):
@@ -464,22 +475,15 @@ def cache_read(cache: dict, table, row_start, key_count, rows: Optional[int] = N
     return k, v
 
 
-def _allocating(device, stream, where: str):
-    """The context in which a call's outputs are allocated."""
-    return _enter(device, stream, where)[1] or contextlib.nullcontext()
-
-
 def _rows(cache, where, dtype, k, v, table, row_start, key_count, stream):
     dev = k.device
     rows = k.shape[0]
     if rows > MAX_ROWS:
         _refuse(where, f"{rows} rows", jdob.JDOB_ERR_UNSUPPORTED)
-    part = _cache(cache, where, dtype, table, row_start, key_count)
+    part = _cache(cache, where, dtype, dev, table, row_start, key_count)
     shape = (rows, part[0].num_kv_heads, part[0].head_dim)
-    if cache["k"].device != dev:
-        _refuse(where, f"the cache is on {cache['k'].device}, expected {dev}")
-    a = CacheRowsArgs(*part, rows, _array(k, where, "k", shape, dtype, dev), k.stride(0), k.stride(1),
-                      _array(v, where, "v", shape, dtype, dev), v.stride(0), v.stride(1))
+    a = CacheRowsArgs(*part, rows, _array(k, where, "k", shape, dtype, dev), *k.stride()[:2],
+                      _array(v, where, "v", shape, dtype, dev), *v.stride()[:2])
     handle, context = _enter(dev, stream, where)
     lib = _lib or load()
     call = lib.jdob_edge_cache_write if where == "jdob_edge_cache_write" else lib.jdob_edge_cache_read
@@ -507,16 +511,16 @@ def attend_paged(q, cache: dict, table, query_start, key_count, scale: Optional[
     rows, h, d = shape
     if rows > MAX_ROWS:
         _refuse(where, f"{rows} rows", jdob.JDOB_ERR_UNSUPPORTED)
-    part = _cache(cache, where, dtype, table, query_start, key_count)
-    c, n, width = part[:3]
-    if cache["k"].device != dev or c.head_dim != d:
-        _refuse(where, f"the cache has heads of {c.head_dim} on {cache['k'].device}, expected {d} on {dev}")
+    part = _cache(cache, where, dtype, dev, table, query_start, key_count)
+    c = part[0]
+    if c.head_dim != d:
+        _refuse(where, f"the cache has heads of {c.head_dim}, expected {d}")
     most = rows if max_queries is None else max_queries
-    longest = width * c.page_size if max_keys is None else max_keys
+    longest = part[2] * c.page_size if max_keys is None else max_keys
     if most < 0 or longest < 0:
         _refuse(where, f"max_queries {most}, max_keys {longest}")
     a = AttendPagedArgs(*part, h, min(most, _MAX_I32), min(longest, _MAX_I32), d ** -0.5 if scale is None else scale,
-                        rows, _array(q, where, "q", shape, dtype, dev), q.stride(0), q.stride(1))
+                        rows, _array(q, where, "q", shape, dtype, dev), *q.stride()[:2])
     handle, context = _enter(dev, stream, where)
     if context is not None:
         with context:
@@ -530,7 +534,7 @@ def _attend_paged(a, where, shape, dtype, dev, out, workspace, handle):
         a.out = out.data_ptr()
     else:
         a.out = _array(out, where, "out", shape, dtype, dev)
-    a.out_stride, a.out_head_stride = out.stride(0), out.stride(1)
+    a.out_stride, a.out_head_stride = out.stride()[:2]
     lib = _lib or load()
     workspace = _workspace(a, workspace, lib.jdob_edge_attend_paged_workspace, dev, where)
     code = lib.jdob_edge_attend_paged(C.byref(a), handle)

@@ -4,6 +4,8 @@
 //
 // A key or a value of a row, up to 128 elements, belongs to 8 or 16 lanes of 8 elements each, so that the largest
 // |x| takes three or four lane exchanges and no LDS.
+#include <type_traits>
+
 #include "pages.h"
 
 namespace edge {
@@ -18,121 +20,197 @@ struct RowsParams {
 
 constexpr int CACHE_THREADS = 256;
 
-// Where a row's key stands; all L lanes of a group bring the same row.  page: -1 where it stands nowhere, -2 where
-// the row belongs to no sequence.
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+typedef int8_t Codes __attribute__((ext_vector_type(8)));
+
+// Where a row's key stands.  page: -1 where it stands nowhere, -2 where the row belongs to no sequence.
 struct Place {
   int page, slot;
 };
 
+// Looks up rows that a group of L lanes brings alike.  Rows in ascending order share a look at row_start as long as they
+// belong to one sequence.
 template <int L>
-__device__ inline Place place_of(const RowsParams &p, int row) {
-  const int n = p.c.sequences, lane = threadIdx.x % WAVE, in = lane % L;
-  // The last sequence that starts at or before the row: every step the group's lanes look at L starts.  The steps'
-  // sizes depend on the number of sequences alone, so that all groups of the wave take them together.
-  int u = 0;
-  for (int size = n; size > 1;) {
-    size = (size + L - 1) / L;
-    const int at = u + in * size;
-    const unsigned long long before = __ballot(at < n && p.c.row_start[at < n ? at : 0] <= row);
-    const int hits = __builtin_popcountll(before >> (lane / L * L) & ((1ull << L) - 1));
-    u += (hits > 0 ? hits - 1 : 0) * size;
+struct Places {
+  const RowsParams &p;
+  int u;
+  int64_t begin, end, keys;
+
+  __device__ Places(const RowsParams &p) : p(p), u(0), begin(0), end(-1), keys(0) {}
+
+  __device__ void search(int row) {
+    const int n = p.c.sequences, lane = threadIdx.x % WAVE, in = lane % L;
+    // The last sequence that starts at or before the row: every step the group's lanes look at L starts.  The steps'
+    // sizes depend on the number of sequences alone, so that all groups of the wave take them together.
+    u = 0;
+    for (int size = n; size > 1;) {
+      size = (size + L - 1) / L;
+      const int at = u + in * size;
+      const unsigned long long before = __ballot(at < n && p.c.row_start[at < n ? at : 0] <= row);
+      const int hits = __builtin_popcountll(before >> (lane / L * L) & ((1ull << L) - 1));
+      u += (hits > 0 ? hits - 1 : 0) * size;
+    }
+    begin = p.c.row_start[u], end = p.c.row_start[u + 1], keys = p.c.key_count[u];
+    end = end < p.rows ? end : p.rows;
+    keys = keys > 0 ? keys : 0;
   }
-  int64_t begin = p.c.row_start[u], end = p.c.row_start[u + 1], keys = p.c.key_count[u];
-  end = end < p.rows ? end : p.rows;
-  if (row < begin || row >= end) return {-2, 0};
-  const int64_t key = (keys > 0 ? keys : 0) - end + row;
-  Place at = {-1, 0};
-  if (key >= 0) at.page = page_of(p.c, u, (int)key, &at.slot);
-  return at;
+
+  __device__ Place find(int row) {
+    if (__any(row < begin || row >= end)) search(row);
+    if (row < begin || row >= end) return {-2, 0};
+    const int64_t key = keys - end + row;
+    Place at = {-1, 0};
+    if (key >= 0) at.page = page_of(p.c, u, (int)key, &at.slot);
+    return at;
+  }
+};
+
+// The codes of a row of which each of L lanes holds eight elements, and its scale.
+template <typename T, int L>
+__device__ inline u32x2 codes_of(const typename Raw<T, 8>::type &x, float *scale) {
+  // the largest |x| by its bit pattern, which orders like the value and puts NaN above all else
+  float f[8];
+  unsigned m = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    f[i] = (float)x[i];
+    const unsigned a = __float_as_uint(f[i]) & 0x7fffffffu;
+    m = a > m ? a : m;
+  }
+#pragma unroll
+  for (int d = L / 2; d > 0; d >>= 1) {
+    const unsigned a = __shfl_xor(m, d);
+    m = a > m ? a : m;
+  }
+  const bool finite = m < 0x7f800000u, some = finite && m > 0;
+  const float s = __uint_as_float(m) / 127.0f, r = some ? 1.0f / s : 0.0f;
+  *scale = finite ? s : __uint_as_float(0x7fc00000u);
+  // x / s is x r, put right by what it leaves of x: the same code as by a division for all values of 16 bits (every
+  // mantissa of x and of the largest value tried; below 1/256 of it x has code 0 either way) where what is left is a
+  // binary32 number.  A division takes ten instructions for the three: 32 prompts took 38 us to write.
+  u32x2 c = {0, 0};
+  const bool small = sizeof(T) == 2 && !__is_same(T, _Float16) && m < 0x12800000u;  // 2^-90
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float q = f[i] * r;
+    // adding 1.5 * 2^23 rounds to the nearest integer, ties to even, and leaves it in the low bits
+    const float y = __builtin_fmaf(__builtin_fmaf(-q, s, f[i]), r, q) + 0x1.8p23f;
+    c[i / 4] |= (__float_as_uint(y) & 0xffu) << (i % 4 * 8);
+  }
+  if (__any(small && some)) {
+    u32x2 d = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      d[i / 4] |= ((unsigned)(int)fminf(fmaxf(rintf(f[i] / s), -127.0f), 127.0f) & 0xffu) << (i % 4 * 8);
+    c[0] = small ? d[0] : c[0];
+    c[1] = small ? d[1] : c[1];
+  }
+  c[0] = some ? c[0] : 0;
+  c[1] = some ? c[1] : 0;
+  return c;
 }
 
-// A workgroup takes 256 / L rows of one head.
-template <typename T, bool BITS8, int L>
+// A workgroup takes B times 256 / L rows of one head.
+template <typename T, bool BITS8, int L, int B>
 __global__ __launch_bounds__(CACHE_THREADS) void write_kernel(RowsParams p) {
   constexpr int ROWS = CACHE_THREADS / L;
-  const int head = block_index() % p.c.kv_heads, e = threadIdx.x % L * 8;
-  const int64_t row = (int64_t)(block_index() / p.c.kv_heads) * ROWS + threadIdx.x / L;
-  if (block_index() / p.c.kv_heads * (int64_t)ROWS >= p.rows) return;
-  const bool in = row < p.rows && e < p.c.dim;
   typedef typename Raw<T, 8>::type Vec;
-  Vec k = {}, v = {};
-  if (in) {
-    k = *(const Vec *)((const T *)p.k + row * p.k_stride + head * p.k_head + e);
-    v = *(const Vec *)((const T *)p.v + row * p.v_stride + head * p.v_head + e);
+  const int head = block_index() % p.c.kv_heads, e = threadIdx.x % L * 8;
+  const int64_t row0 = (int64_t)(block_index() / p.c.kv_heads) * (B * ROWS) + threadIdx.x / L;
+  if (block_index() / p.c.kv_heads * (int64_t)(B * ROWS) >= p.rows) return;
+  Vec x[B][2];
+#pragma unroll
+  for (int b = 0; b < B; ++b) {
+    const int64_t row = row0 + b * ROWS;
+    const bool in = row < p.rows && e < p.c.dim;
+    x[b][0] = x[b][1] = Vec{};
+    if (in) {
+      x[b][0] = *(const Vec *)((const T *)p.k + row * p.k_stride + head * p.k_head + e);
+      x[b][1] = *(const Vec *)((const T *)p.v + row * p.v_stride + head * p.v_head + e);
+    }
   }
-  const Place at = place_of<L>(p, row < p.rows ? (int)row : 0);
-  const bool stands = in && at.page >= 0;
-  auto put = [&](const Vec &x, const Pool &to) {
-    const int64_t spot = at.page * to.page + head * to.head + at.slot * to.slot + e;
-    if constexpr (!BITS8) {
-      if (stands) *(Vec *)((T *)to.at + spot) = x;
-    } else {
-      // the largest |x| by its bit pattern, which orders like the value and puts NaN above all else
-      float f[8];
-      unsigned m = 0;
+  Places<L> places(p);
+  Place at[B];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        f[i] = (float)x[i];
-        const unsigned a = __float_as_uint(f[i]) & 0x7fffffffu;
-        m = a > m ? a : m;
-      }
+  for (int b = 0; b < B; ++b) at[b] = places.find(row0 + b * ROWS < p.rows ? (int)(row0 + b * ROWS) : p.rows - 1);
 #pragma unroll
-      for (int d = L / 2; d > 0; d >>= 1) {
-        const unsigned a = __shfl_xor(m, d);
-        m = a > m ? a : m;
-      }
-      const bool finite = m < 0x7f800000u;
-      const float scale = __uint_as_float(m) / 127.0f;
-      Raw<int8_t, 8>::type c;
+  for (int b = 0; b < B; ++b) {
+    const bool stands = row0 + b * ROWS < p.rows && e < p.c.dim && at[b].page >= 0;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float y = fminf(fmaxf(rintf(f[i] / scale), -127.0f), 127.0f);
-        c[i] = finite && scale > 0.0f ? (int8_t)(int)y : (int8_t)0;
-      }
-      if (stands) {
-        *(Raw<int8_t, 8>::type *)((int8_t *)to.at + spot) = c;
-        if (e == 0)
-          to.scale[at.page * to.scale_page + head * to.scale_head + at.slot * to.scale_slot] =
-              finite ? scale : __uint_as_float(0x7fc00000u);
+    for (int i = 0; i < 2; ++i) {
+      const Pool &to = i ? p.c.v : p.c.k;
+      const int64_t spot = at[b].page * to.page + head * to.head + at[b].slot * to.slot + e;
+      if constexpr (!BITS8) {
+        if (stands) *(Vec *)((T *)to.at + spot) = x[b][i];
+      } else {
+        float scale;
+        const u32x2 c = codes_of<T, L>(x[b][i], &scale);
+        if (stands) {
+          *(Raw<int8_t, 8>::type *)((int8_t *)to.at + spot) = __builtin_bit_cast(Codes, c);
+          if (e == 0) to.scale[at[b].page * to.scale_page + head * to.scale_head + at[b].slot * to.scale_slot] = scale;
+        }
       }
     }
-  };
-  put(k, p.c.k);
-  put(v, p.c.v);
+  }
 }
 
-template <typename T, bool BITS8, int L>
+template <typename T, bool BITS8, int L, int B>
 __global__ __launch_bounds__(CACHE_THREADS) void read_kernel(RowsParams p) {
   constexpr int ROWS = CACHE_THREADS / L;
-  const int head = block_index() % p.c.kv_heads, e = threadIdx.x % L * 8;
-  const int64_t row = (int64_t)(block_index() / p.c.kv_heads) * ROWS + threadIdx.x / L;
-  if (block_index() / p.c.kv_heads * (int64_t)ROWS >= p.rows) return;
-  const Place at = place_of<L>(p, row < p.rows ? (int)row : 0);
-  if (row >= p.rows || e >= p.c.dim || at.page == -2) return;
   typedef typename Raw<T, 8>::type Vec;
-  auto get = [&](const Pool &from, T *to) {
-    const int64_t spot = at.page * from.page + head * from.head + at.slot * from.slot + e;
-    Vec x = {};
-    if constexpr (!BITS8) {
-      if (at.page >= 0) x = *(const Vec *)((const T *)from.at + spot);
-    } else if (at.page >= 0) {
-      const Raw<int8_t, 8>::type c = *(const Raw<int8_t, 8>::type *)((const int8_t *)from.at + spot);
-      const float scale = from.scale[at.page * from.scale_page + head * from.scale_head + at.slot * from.scale_slot];
+  const int head = block_index() % p.c.kv_heads, e = threadIdx.x % L * 8;
+  const int64_t row0 = (int64_t)(block_index() / p.c.kv_heads) * (B * ROWS) + threadIdx.x / L;
+  if (block_index() / p.c.kv_heads * (int64_t)(B * ROWS) >= p.rows) return;
+  Places<L> places(p);
+  Place at[B];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = (T)((float)c[i] * scale);
+  for (int b = 0; b < B; ++b) at[b] = places.find(row0 + b * ROWS < p.rows ? (int)(row0 + b * ROWS) : p.rows - 1);
+  typedef typename std::conditional<BITS8, Codes, Vec>::type In;
+  In x[B][2];
+  float scale[B][2];
+#pragma unroll
+  for (int b = 0; b < B; ++b)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const Pool &from = i ? p.c.v : p.c.k;
+      const int64_t spot = at[b].page * from.page + head * from.head + at[b].slot * from.slot + e;
+      x[b][i] = In{};
+      if (at[b].page < 0 || e >= p.c.dim) continue;
+      if constexpr (BITS8) {
+        x[b][i] = __builtin_bit_cast(Codes, *(const Raw<int8_t, 8>::type *)((const int8_t *)from.at + spot));
+        scale[b][i] = from.scale[at[b].page * from.scale_page + head * from.scale_head + at[b].slot * from.scale_slot];
+      } else {
+        x[b][i] = *(const Vec *)((const T *)from.at + spot);
+      }
     }
-    *(Vec *)to = x;
-  };
-  get(p.c.k, (T *)p.k + row * p.k_stride + head * p.k_head + e);
-  get(p.c.v, (T *)p.v + row * p.v_stride + head * p.v_head + e);
+#pragma unroll
+  for (int b = 0; b < B; ++b) {
+    const int64_t row = row0 + b * ROWS;
+    if (row >= p.rows || e >= p.c.dim || at[b].page == -2) continue;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      T *const to = i ? (T *)p.v + row * p.v_stride + head * p.v_head : (T *)p.k + row * p.k_stride + head * p.k_head;
+      Vec y;
+      if constexpr (BITS8) {
+        const float s = at[b].page < 0 ? 0.0f : scale[b][i];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[j] = (T)((float)x[b][i][j] * s);
+      } else {
+        y = x[b][i];
+      }
+      *(Vec *)(to + e) = y;
+    }
+  }
 }
 
 template <typename T, bool BITS8, int L>
 int rows_launch(const RowsParams &p, bool write, hipStream_t stream) {
-  constexpr int ROWS = CACHE_THREADS / L;
-  const int64_t blocks = ((int64_t)p.rows + ROWS - 1) / ROWS * p.c.kv_heads;
-  if (blocks > MAX_BLOCKS) return JDOB_ERR_UNSUPPORTED;
-  return launch(write ? write_kernel<T, BITS8, L> : read_kernel<T, BITS8, L>, blocks, CACHE_THREADS, stream, p);
+  constexpr int ROWS = CACHE_THREADS / L, B = 4;
+  auto blocks = [&](int b) { return ((int64_t)p.rows + b * ROWS - 1) / (b * ROWS) * p.c.kv_heads; };
+  if (blocks(B) > MAX_BLOCKS) return JDOB_ERR_UNSUPPORTED;
+  if (blocks(B) >= 2048)
+    return launch(write ? write_kernel<T, BITS8, L, B> : read_kernel<T, BITS8, L, B>, blocks(B), CACHE_THREADS, stream, p);
+  return launch(write ? write_kernel<T, BITS8, L, 1> : read_kernel<T, BITS8, L, 1>, blocks(1), CACHE_THREADS, stream, p);
 }
 
 template <typename T>
