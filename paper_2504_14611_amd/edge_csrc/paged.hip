@@ -30,9 +30,10 @@ struct PagedParams {
   const char *q;
   char *out;
   int64_t q_stride, q_head, out_stride, out_head;  // elements
-  int splits, each;   // splits of the keys, keys of one
   int tiles;          // tiles of columns of a sequence
-  float *part;        // [sequence][key head][tile][split][columns of a tile][dim + 4]
+  int shares;         // of the keys, besides one for each sequence (0: keys are not split)
+  Divide by_heads, by_tiles, by_group;  // of key heads, tiles and the heads of a key head
+  float *part;        // [share][tile][key head][columns of a tile][dim + 4]
 };
 
 typedef short s16x8 __attribute__((ext_vector_type(8)));
@@ -53,18 +54,65 @@ struct Mma16<_Float16> {
 
 // A sequence's rows and keys, kept within the arrays whatever the index arrays hold.
 struct Newest {
-  int64_t row;
-  int rows, keys;  // the keys as counted
-  int last;        // keys that the table has room for
+  int row, rows, keys;  // the first row, rows, the keys as counted
+  int last;             // keys that the table has room for
 };
 
 __device__ inline Newest newest(const PagedParams &p, int u) {
-  int64_t at = p.c.row_start[u], end = p.c.row_start[u + 1];
-  at = at < 0 ? 0 : at < p.query_rows ? at : p.query_rows;
-  end = end < at ? at : end < p.query_rows ? end : p.query_rows;
+  const int most = (int)p.query_rows;
+  int at = p.c.row_start[u], end = p.c.row_start[u + 1];
+  at = at < 0 ? 0 : at < most ? at : most;
+  end = end < at ? at : end < most ? end : most;
   const int keys = p.c.key_count[u] > 0 ? p.c.key_count[u] : 0;
   const int64_t room = (int64_t)p.c.width * p.c.page_size;
-  return {at, (int)(end - at), keys, (int)(keys < room ? keys : room)};
+  return {at, end - at, keys, (int)(keys < room ? keys : room)};
+}
+
+// Sequences of very different lengths: each has a share for every so many keys, as few as p.shares and one more for each
+// sequence's end allow.  Every wave forms the shares' list from the lengths.
+struct Share {
+  Newest q;
+  int u, index, count;  // the sequence, which of its shares, how many it has
+  int first;            // the sequence's first share in the list
+};
+constexpr int SHARE_UNIT = 128, LEAST_KEYS = 256;
+
+__device__ inline int units_of(const Newest &q) { return (q.last >> 7) + ((q.last & 127) != 0); }
+
+// The share at place `at` of the list, or with `of_sequence` the first of sequence `at`; false where there is none.
+__device__ inline bool share_of(const PagedParams &p, int at, bool of_sequence, Share *s) {
+  const int lane = threadIdx.x % WAVE, n = p.c.sequences;
+  double units = 0.0;  // (exact)
+  for (int u = lane; u < n; u += WAVE) {
+    const Newest q = newest(p, u);
+    units += q.rows ? units_of(q) : 0;
+  }
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) units += __shfl_xor(units, d);
+  const int each = __builtin_amdgcn_readfirstlane((int)fmax(ceil(units / p.shares), (double)LEAST_KEYS / SHARE_UNIT));  // units, to 2^24
+  int before = 0;
+  for (int u0 = 0; u0 < n; u0 += WAVE) {
+    Newest q = {0, 0, 0, 0};
+    if (u0 + lane < n) q = newest(p, u0 + lane);
+    const int mine = !q.rows ? 0 : q.last ? (units_of(q) + each - 1) / each : 1;
+    int upto = mine;
+#pragma unroll
+    for (int d = 1; d < WAVE; d <<= 1) {
+      const int x = __shfl_up(upto, d);
+      if (lane >= d) upto += x;
+    }
+    const unsigned long long found = of_sequence ? at < u0 + WAVE ? 1ull << (at - u0) : 0 : __ballot(before + upto > at);
+    if (found) {
+      const int l = __builtin_ctzll(found);
+      *s = {{__builtin_amdgcn_readlane(q.row, l), __builtin_amdgcn_readlane(q.rows, l), __builtin_amdgcn_readlane(q.keys, l),
+             __builtin_amdgcn_readlane(q.last, l)},
+            u0 + l, 0, __builtin_amdgcn_readlane(mine, l), before + __builtin_amdgcn_readlane(upto - mine, l)};
+      s->index = of_sequence ? 0 : at - s->first;
+      return s->count > 0;
+    }
+    before += __builtin_amdgcn_readlane(upto, WAVE - 1);
+  }
+  return false;
 }
 
 // Which elements of a key's or value's row a lane holds, for heads padded to DP.
@@ -86,72 +134,134 @@ struct Tile {
   static constexpr int VW = BITS8 ? (DP == 128 ? 2 : DP == 96 ? 2 : 1) : DP / 32;  // words of a value
   unsigned k[2][KW], v[8][VW];
   f32x4 k_scale[2], v_scale[2];
-  unsigned gone;  // a bit for each of the lane's 8 keys that is absent
 };
 
-// A wave's keys of one head, and where the lane's are found: key by key, whatever the page's size and the arrays' alignment.
-template <typename T, int DP, bool BITS8>
+constexpr int TILE_KEYS = 32;
+constexpr int64_t NO_TILE = INT64_MAX / 2;  // behind any key
+
+__device__ const u32x4 paged_zeros = {0, 0, 0, 0};
+
+// A wave's keys of one head whatever the page's size and the arrays' alignment: every lane looks up its own keys' pages,
+// RUN keys from a multiple of RUN on at once (pages of a multiple of RUN keys).
+template <typename T, int DP, bool BITS8, int RUN>
 struct Anywhere {
+  typedef typename std::conditional<BITS8, int8_t, unsigned short>::type E;
   const PagedParams &p;
-  int u, head, until, lane_key, g;  // until: keys from there on are not read
+  int u, head, until, l16, g;  // until: keys from there on are not read
+  int64_t tile;                // to be looked up next
+  int step;
+  struct Spot {
+    int page, slot;  // page: -1 where there is none
+  };
+  struct Spots {  // of a tile: the lane's key of each half, and its runs of values
+    Spot key[2], run[2][4 / RUN];
+  } next, after;
 
-  __device__ Anywhere(const PagedParams &p, int u, int head, int until)
-      : p(p), u(u), head(head), until(until), lane_key(threadIdx.x % 16), g(threadIdx.x % WAVE / 16) {}
+  __device__ Anywhere(const PagedParams &p, int u, int head, int until, int tile, int step)
+      : p(p), u(u), head(head), until(until), l16(threadIdx.x % 16), g(threadIdx.x % WAVE / 16), tile(tile), step(step) {}
 
-  template <typename E, int N>
+  __device__ Spot spot(int64_t j) const {
+    const int i = divide(j < until ? (int)j : 0, p.c.by_page);  // (key 0 is there to be looked up if any is)
+    const int page = p.c.table[u * p.c.table_stride + i];
+    return {j < until && (unsigned)page < (unsigned)p.c.pages ? page : -1, (int)j - i * p.c.page_size};
+  }
+
+  // The tile that was looked up last is the next one to be loaded; looks up another and returns its first key.
+  __device__ int64_t find() {
+    next = after;
+    const int64_t first = tile * TILE_KEYS;
+    tile += step;
+    if (first >= until) return NO_TILE;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      after.key[h] = spot(first + h * 16 + l16);
+#pragma unroll
+      for (int r = 0; r < 4 / RUN; ++r) after.run[h][r] = spot(first + h * 16 + g * 4 + r * RUN);
+    }
+    return first;
+  }
+
+  // Whether the lane's value h, r of the next tile is there.  (The last keys of a run that the last key is part of are
+  // on its page, but not to be read.)
+  __device__ bool there(int64_t first, int h, int r) const {
+    return next.run[h][r / RUN].page >= 0 && (RUN == 1 || first + h * 16 + g * 4 + r < until);
+  }
+  __device__ unsigned gone(int64_t first) const {
+    unsigned bits = 0;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) bits |= there(first, h, r) ? 0 : 1u << (h * 4 + r);
+    return bits;
+  }
+
+  template <int N>
   __device__ static void piece(unsigned *to, const E *row, int e, bool have) {
-    typename Raw<E, N>::type x = {};
-    if (have) x = *(const typename Raw<E, N>::type *)(row + e);
+    typedef typename Raw<E, N>::type V;
+    const V x = *(const V *)(have ? (const void *)(row + e) : (const void *)&paged_zeros);
     if constexpr (sizeof x < sizeof(unsigned)) {
       *to = __builtin_bit_cast(unsigned short, x);
     } else {
       __builtin_memcpy(to, &x, sizeof x);
     }
   }
+  static constexpr int N = BITS8 ? 4 : 2;  // elements a word
 
-  __device__ void find(int64_t) {}
-  __device__ void load(Tile<DP, BITS8> &t, int64_t first) const {
-    typedef typename std::conditional<BITS8, int8_t, unsigned short>::type E;
-    constexpr int N = BITS8 ? 4 : 2;  // elements a word
-    const int dim = p.c.dim;
-    t.gone = 0;
+  __device__ void scales(f32x4 (&to)[2], const Pool &from, int64_t first) const {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const Spot at = next.run[h][r / RUN];
+        const float *const x =
+            from.scale + at.page * from.scale_page + head * from.scale_head + (at.slot + r % RUN) * from.scale_slot;
+        to[h][r] = *(there(first, h, r) ? x : (const float *)&paged_zeros);
+      }
+  }
+
+  __device__ void load_keys(Tile<DP, BITS8> &t, int64_t first) const {
+    if (first >= until) return;  // (it will not be taken)
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const int64_t key = first + h * 16 + lane_key;
-      int slot = 0;
-      const int page = key < until ? page_of(p.c, u, (int)key, &slot) : -1;
-      const E *const row = (const E *)p.c.k.at + page * p.c.k.page + head * p.c.k.head + slot * p.c.k.slot;
+      const Spot at = next.key[h];
+      const E *const row = (const E *)p.c.k.at + at.page * p.c.k.page + head * p.c.k.head + at.slot * p.c.k.slot;
 #pragma unroll
       for (int j = 0; j < DP / 32; ++j) {
         const int e = key_element<DP, BITS8>(j, g);
-        piece<E, 8>(t.k[h] + j * 8 / N, row, e, page >= 0 && e < dim);
+        piece<8>(t.k[h] + j * 8 / N, row, e, at.page >= 0 && e < p.c.dim);
       }
+      __builtin_amdgcn_sched_barrier(0);  // (all addresses at once would take more registers than there are)
+    }
+    if constexpr (BITS8) scales(t.k_scale, p.c.k, first);
+  }
+
+  __device__ void load_values(Tile<DP, BITS8> &t, int64_t first) const {
+    if (first >= until) return;
+    const int dim = p.c.dim;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const int64_t key = first + h * 16 + g * 4 + r;
-        int slot = 0;
-        const int page = key < until ? page_of(p.c, u, (int)key, &slot) : -1;
-        const E *const row = (const E *)p.c.v.at + page * p.c.v.page + head * p.c.v.head + slot * p.c.v.slot;
+        const Spot at = next.run[h][r / RUN];
+        const bool have = there(first, h, r);
+        const E *const row =
+            (const E *)p.c.v.at + at.page * p.c.v.page + head * p.c.v.head + (at.slot + r % RUN) * p.c.v.slot;
         unsigned *const to = t.v[h * 4 + r];
-        const int m = lane_key;
         if constexpr (DP == 96) {
-          piece<E, 4>(to, row, m * 4, page >= 0 && m * 4 < dim);
-          piece<E, 2>(to + 4 / N, row, 64 + m * 2, page >= 0 && 64 + m * 2 < dim);
+          piece<4>(to, row, l16 * 4, have && l16 * 4 < dim);
+          piece<2>(to + 4 / N, row, 64 + l16 * 2, have && 64 + l16 * 2 < dim);
         } else {
-          piece<E, DP / 16>(to, row, m * (DP / 16), page >= 0 && m * (DP / 16) < dim);
+          piece<DP / 16>(to, row, l16 * (DP / 16), have && l16 * (DP / 16) < dim);
         }
-        if constexpr (BITS8) {
-          t.k_scale[h][r] = t.v_scale[h][r] = 0.0f;
-          if (page >= 0) {
-            t.k_scale[h][r] = p.c.k.scale[page * p.c.k.scale_page + head * p.c.k.scale_head + slot * p.c.k.scale_slot];
-            t.v_scale[h][r] = p.c.v.scale[page * p.c.v.scale_page + head * p.c.v.scale_head + slot * p.c.v.scale_slot];
-          }
-        }
-        t.gone |= page < 0 ? 1u << (h * 4 + r) : 0;
+        __builtin_amdgcn_sched_barrier(0);
       }
-    }
+    if constexpr (BITS8) scales(t.v_scale, p.c.v, first);
   }
 };
+
+__device__ inline int64_t of_lane(int64_t x, int lane) {
+  return (int64_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32 | (unsigned)__builtin_amdgcn_readlane((int)x, lane);
+}
 
 // A stretch of memory from `at` on: what is read from behind its end is zero and does not touch memory.  Both are the
 // same for all lanes of the wave.
@@ -177,8 +287,9 @@ __device__ inline void window_load(unsigned *to, __amdgpu_buffer_rsrc_t w, unsig
 }
 
 // The same where 16 keys that start at a multiple of 16 stand side by side on one page, and their rows at multiples of
-// 16 bytes: the page is looked up once for all lanes, a lane's offsets within the 16 rows stay the same from tile to
-// tile, and rows behind the last key, or of a page that is not there, are kept out by the end of a window.
+// 16 bytes: the pages of 64 tiles are looked up at once, a tile a lane, and tiles without any are passed over; a lane's
+// offsets within the 16 rows stay the same from tile to tile, and rows behind the last key, or of a page that is not
+// there, are kept out by the end of a window.
 template <typename T, int DP, bool BITS8>
 struct InPages {
   typedef typename std::conditional<BITS8, int8_t, unsigned short>::type E;
@@ -187,11 +298,22 @@ struct InPages {
   const PagedParams &p;
   int u, head, until;
   unsigned k_at[NK], v_at[4][NV];
-  struct Spot {
-    int page[2], slot[2];
-  } spot;  // of the next tile
+  // Where the halves' 16 rows start, in bytes from the head's first; below zero: a page that is not there.
+  struct Spots {
+    int64_t k[2], v[2], k_scale[2], v_scale[2];
+  } next, after, lanes;  // lanes: of the tiles tile, tile + step, ...
+  int64_t tile;
+  int step;
+  unsigned long long left;  // those of them that are still to come
+  const char *k, *v, *k_scale, *v_scale;  // of the head
 
-  __device__ InPages(const PagedParams &p, int u, int head, int until) : p(p), u(u), head(head), until(until) {
+  __device__ InPages(const PagedParams &p, int u, int head, int until, int tile, int step)
+      : p(p), u(u), head(head), until(until), tile(tile), step(step) {
+    look();
+    k = p.c.k.at + head * p.c.k.head * SZ;
+    v = p.c.v.at + head * p.c.v.head * SZ;
+    k_scale = (const char *)(p.c.k.scale + head * p.c.k.scale_head);
+    v_scale = (const char *)(p.c.v.scale + head * p.c.v.scale_head);
     const int l16 = threadIdx.x % 16, g = threadIdx.x % WAVE / 16, dim = p.c.dim;
 #pragma unroll
     for (int i = 0; i < NK; ++i) {
@@ -210,60 +332,97 @@ struct InPages {
     }
   }
 
-  __device__ void find(int64_t first) {
+  __device__ void look() {
+    const int64_t first = (tile + (int64_t)(threadIdx.x % WAVE) * step) * TILE_KEYS;
+    bool any = false;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      spot.page[h] = -1;
-      spot.slot[h] = 0;
-      if (first + h * 16 < until)
-        spot.page[h] = __builtin_amdgcn_readfirstlane(page_of(p.c, u, (int)first + h * 16, &spot.slot[h]));
+      int page = -1, slot = 0;
+      if (first + h * 16 < until) page = page_of(p.c, u, (int)first + h * 16, &slot);
+      any |= page >= 0;
+      auto spot = [&](int64_t by_page, int64_t by_slot, int size) { return page < 0 ? -1 : (page * by_page + slot * by_slot) * size; };
+      lanes.k[h] = spot(p.c.k.page, p.c.k.slot, SZ);
+      lanes.v[h] = spot(p.c.v.page, p.c.v.slot, SZ);
+      if constexpr (BITS8) {
+        lanes.k_scale[h] = spot(p.c.k.scale_page, 1, 4);
+        lanes.v_scale[h] = spot(p.c.v.scale_page, 1, 4);
+      }
+    }
+    left = __ballot(any);
+  }
+
+  // The tile that was looked up last is the next one to be loaded; looks up another and returns its first key.
+  __device__ int64_t find() {
+    next = after;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) after.k[h] = after.v[h] = after.k_scale[h] = after.v_scale[h] = -1;
+    while (!left) {
+      if ((tile + (int64_t)WAVE * step) * TILE_KEYS >= until) return NO_TILE;
+      tile += (int64_t)WAVE * step;
+      look();
+    }
+    const int l = __builtin_ctzll(left);
+    left &= left - 1;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      after.k[h] = of_lane(lanes.k[h], l);
+      after.v[h] = of_lane(lanes.v[h], l);
+      if constexpr (BITS8) {
+        after.k_scale[h] = of_lane(lanes.k_scale[h], l);
+        after.v_scale[h] = of_lane(lanes.v_scale[h], l);
+      }
+    }
+    return (tile + (int64_t)l * step) * TILE_KEYS;
+  }
+
+  __device__ unsigned gone(int64_t) const { return (next.k[0] < 0 ? 0xfu : 0) | (next.k[1] < 0 ? 0xf0u : 0); }
+
+  // The 16 rows as far as there are any (the last key's tile ends with it).
+  __device__ __amdgpu_buffer_rsrc_t rows_of(const char *x, int64_t at, int slot, int64_t first, int h) const {
+    const int64_t behind = until - (first + h * 16);
+    const int rows = behind < 16 ? (int)behind : 16;
+    return window(x + at, at < 0 ? 0 : ((rows - 1) * slot + p.c.dim) * SZ);
+  }
+  // (all 16 scales are on the page, those behind the last key among them)
+  __device__ f32x4 scales_of(const char *x, int64_t at) const {
+    unsigned w[4];
+    window_load<16>(w, window(x + at, at < 0 ? 0 : 64), threadIdx.x % WAVE / 16 * 16);
+    return (f32x4){__uint_as_float(w[0]), __uint_as_float(w[1]), __uint_as_float(w[2]), __uint_as_float(w[3])};
+  }
+
+  __device__ void load_keys(Tile<DP, BITS8> &t, int64_t first) const {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const auto w = rows_of(k, next.k[h], (int)p.c.k.slot, first, h);
+#pragma unroll
+      for (int i = 0; i < NK; ++i) {
+        if constexpr (!BITS8) {
+          window_load<16>(t.k[h] + i * 4, w, k_at[i]);
+        } else if (i * 64 + 64 <= DP) {
+          window_load<16>(t.k[h] + i * 4, w, k_at[i]);
+        } else {
+          window_load<8>(t.k[h] + i * 4, w, k_at[i]);
+        }
+      }
+      if constexpr (BITS8) t.k_scale[h] = scales_of(k_scale, next.k_scale[h]);
     }
   }
 
-  __device__ void load(Tile<DP, BITS8> &t, int64_t first) const {
-    t.gone = 0;
+  __device__ void load_values(Tile<DP, BITS8> &t, int64_t first) const {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const int page = spot.page[h], slot = spot.slot[h];
-      const int64_t behind = until - (first + h * 16);
-      const int rows = page < 0 ? 0 : behind < 16 ? (int)behind : 16;  // (a page only where there are keys)
-      const E *const k = (const E *)p.c.k.at + page * p.c.k.page + head * p.c.k.head + slot * p.c.k.slot;
-      const E *const v = (const E *)p.c.v.at + page * p.c.v.page + head * p.c.v.head + slot * p.c.v.slot;
-      const auto kw = window(k, rows ? (int)((rows - 1) * p.c.k.slot + p.c.dim) * SZ : 0);
-      const auto vw = window(v, rows ? (int)((rows - 1) * p.c.v.slot + p.c.dim) * SZ : 0);
-#pragma unroll
-      for (int i = 0; i < NK; ++i) {
-        if constexpr (BITS8) {
-          if (i * 64 + 64 <= DP) {
-            window_load<16>(t.k[h] + i * 4, kw, k_at[i]);
-          } else {
-            window_load<8>(t.k[h] + i * 4, kw, k_at[i]);
-          }
-        } else {
-          window_load<16>(t.k[h] + i * 4, kw, k_at[i]);
-        }
-      }
+      const auto w = rows_of(v, next.v[h], (int)p.c.v.slot, first, h);
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         unsigned *const to = t.v[h * 4 + r];
         if constexpr (DP == 96) {
-          window_load<4 * SZ>(to, vw, v_at[r][0]);
-          window_load<2 * SZ>(to + SZ, vw, v_at[r][1]);
+          window_load<4 * SZ>(to, w, v_at[r][0]);
+          window_load<2 * SZ>(to + SZ, w, v_at[r][1]);
         } else {
-          window_load<DP / 16 * SZ>(to, vw, v_at[r][0]);
+          window_load<DP / 16 * SZ>(to, w, v_at[r][0]);
         }
       }
-      if constexpr (BITS8) {
-        // (all 16 are on the page, those behind the last key among them)
-        const float *const ks = p.c.k.scale + page * p.c.k.scale_page + head * p.c.k.scale_head + slot;
-        const float *const vs = p.c.v.scale + page * p.c.v.scale_page + head * p.c.v.scale_head + slot;
-        unsigned w[2][4];
-        window_load<16>(w[0], window(ks, rows ? 64 : 0), threadIdx.x % WAVE / 16 * 16);
-        window_load<16>(w[1], window(vs, rows ? 64 : 0), threadIdx.x % WAVE / 16 * 16);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) t.k_scale[h][r] = __uint_as_float(w[0][r]), t.v_scale[h][r] = __uint_as_float(w[1][r]);
-      }
-      t.gone |= page < 0 ? 0xfu << (h * 4) : 0;
+      if constexpr (BITS8) t.v_scale[h] = scales_of(v_scale, next.v_scale[h]);
     }
   }
 };
@@ -307,14 +466,14 @@ __device__ inline typename Mma16<T>::frag of_codes(unsigned lo, unsigned hi) {
   return f;
 }
 
-// Scores of the columns with 32 keys, softmax, and the values' sums.  Of the tile's keys the lane's column c sees
-// 0 .. sees[c] that are there; MASKED: some column of the tile does not see some key.
-template <typename T, int DP, bool BITS8, int CT, bool MASKED>
-__device__ inline void attend_tile(State16<DP> (&s)[CT], const typename Mma16<T>::frag (&q)[CT][DP / 32],
-                                   const Tile<DP, BITS8> &t, const int (&sees)[CT], float scale) {
+// p in the type of its product: with 8 bits in two bfloat16 parts, whose range holds p times any scale.
+template <typename T, bool BITS8>
+using Weight = typename std::conditional<BITS8, __bf16, T>::type;
+
+// Scores of the columns with 32 keys: column c's with key 16 h + 4 g + r in sc[c][h][r].
+template <typename T, int DP, bool BITS8, int CT>
+__device__ inline void scores(f32x4 (&sc)[CT][2], const typename Mma16<T>::frag (&q)[CT][DP / 32], const Tile<DP, BITS8> &t) {
   typedef typename Mma16<T>::frag frag;
-  const int g = threadIdx.x % WAVE / 16;
-  f32x4 sc[CT][2];
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
 #pragma unroll
@@ -335,159 +494,171 @@ __device__ inline void attend_tile(State16<DP> (&s)[CT], const typename Mma16<T>
       for (int c = 0; c < CT; ++c) sc[c][h] *= t.k_scale[h];
     }
   }
-  // p in the type of its product: with 8 bits in two bfloat16 parts, whose range holds p times any scale
-  typedef typename std::conditional<BITS8, __bf16, T>::type P;
-  typedef typename Mma16<P>::frag pfrag;
-  pfrag p[CT], rest[CT];
+}
+
+// p of a column's scores relative to its maximum, which is raised first where it lags; the sum goes on.
+template <int DP>
+__device__ inline void softmax(State16<DP> &s, f32x4 (&sc)[2], float scale) {
+  float top = -INFINITY;
 #pragma unroll
-  for (int c = 0; c < CT; ++c) {
-    auto seen = [&](int h, int r) { return h * 16 + g * 4 + r <= sees[c] && !(t.gone >> (h * 4 + r) & 1); };
-    float top = -INFINITY;
+  for (int h = 0; h < 2; ++h)
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int r = 0; r < 4; ++r) top = fmaxf(top, sc[h][r]);
+  top = column_max(top);
+  // (false where neither has seen anything: -inf - -inf is NaN)
+  const bool grows = (top - s.top) * scale > GROWTH;
+  if (__any(grows)) {
+    // a column's own scores decide for it: what other columns see does not change its roundings
+    const float next = grows ? top : s.top;
+    const float f = s.top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((s.top - next) * scale);
+    s.top = next;
+    s.sum *= f;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        if constexpr (MASKED) sc[c][h][r] = seen(h, r) ? sc[c][h][r] : -INFINITY;
-        top = fmaxf(top, sc[c][h][r]);
-      }
-    top = column_max(top);
-    // (false where neither has seen anything: -inf - -inf is NaN)
-    const bool grows = (top - s[c].top) * scale > GROWTH;
-    if (__any(grows)) {
-      // a column's own scores decide for it: what other columns see does not change its roundings
-      const float next = grows ? top : s[c].top;
-      const float f = s[c].top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((s[c].top - next) * scale);
-      s[c].top = next;
-      s[c].sum *= f;
-#pragma unroll
-      for (int i = 0; i < DP / 16; ++i) s[c].out[i] *= f;
-    }
-    const float base = base_of(s[c].top) * scale;
-    const bool far = !(fabsf(base) < NEAR);
-    if (__any(far)) {
-      // the difference first, again column by column
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) sc[c][h][r] = far ? (sc[c][h][r] - s[c].top) * scale : sc[c][h][r] * scale - base;
-    } else {
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) sc[c][h][r] = sc[c][h][r] * scale - base;
-    }
+    for (int i = 0; i < DP / 16; ++i) s.out[i] *= f;
+  }
+  const float base = base_of(s.top) * scale;
+  const bool far = !(fabsf(base) < NEAR);
+  if (__any(far)) {
+    // the difference first, again column by column
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        float x = __builtin_amdgcn_exp2f(sc[c][h][r]);
-        s[c].sum += x;
-        if constexpr (BITS8) {
-          // (what a column does not see may have any scale)
-          x *= MASKED && !seen(h, r) ? 0.0f : t.v_scale[h][r];
-        }
-        p[c][h * 4 + r] = (P)x;
-        if constexpr (BITS8) rest[c][h * 4 + r] = (P)(x - (float)p[c][h * 4 + r]);
-      }
+      for (int r = 0; r < 4; ++r) sc[h][r] = far ? (sc[h][r] - s.top) * scale : sc[h][r] * scale - base;
+  } else {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sc[h][r] = sc[h][r] * scale - base;
   }
 #pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      sc[h][r] = __builtin_amdgcn_exp2f(sc[h][r]);
+      s.sum += sc[h][r];
+    }
+}
+
+// Element i of the lane's piece of its eight 16-bit values.
+template <int DP>
+__device__ inline u32x4 value_words(const Tile<DP, false> &t, int i) {
+  u32x4 x;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const unsigned a = t.v[2 * e][i / 2], b = t.v[2 * e + 1][i / 2];
+    x[e] = i % 2 ? a >> 16 | (b & 0xffff0000u) : (a & 0xffffu) | b << 16;
+  }
+  return x;
+}
+
+// The values' sums with weights p.
+template <typename T, int DP, bool BITS8, int CT>
+__device__ inline void weighted(State16<DP> (&s)[CT], const f32x4 (&p)[CT][2], const Tile<DP, BITS8> &t) {
+  typedef Weight<T, BITS8> P;
+  typedef typename Mma16<P>::frag frag;
+  frag w[CT], rest[CT];
+#pragma unroll
+  for (int c = 0; c < CT; ++c)
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float x = BITS8 ? p[c][h][r] * t.v_scale[h][r] : p[c][h][r];
+        w[c][h * 4 + r] = (P)x;
+        if constexpr (BITS8) rest[c][h * 4 + r] = (P)(x - (float)w[c][h * 4 + r]);
+      }
+#pragma unroll
   for (int i = 0; i < DP / 16; ++i) {
-    pfrag v;
+    frag v;
     if constexpr (BITS8) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = (P)(float)(int8_t)(t.v[e][i / 4] >> 8 * (i % 4));
     } else {
-      u32x4 w;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const unsigned a = t.v[2 * e][i / 2], b = t.v[2 * e + 1][i / 2];
-        w[e] = i % 2 ? a >> 16 | (b & 0xffff0000u) : (a & 0xffffu) | b << 16;
-      }
-      v = __builtin_bit_cast(pfrag, w);
+      v = __builtin_bit_cast(frag, value_words(t, i));
     }
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
-      s[c].out[i] = Mma16<P>::m16(v, p[c], s[c].out[i]);
+      s[c].out[i] = Mma16<P>::m16(v, w[c], s[c].out[i]);
       if constexpr (BITS8) s[c].out[i] = Mma16<P>::m16(v, rest[c], s[c].out[i]);
     }
+    if (i % 2) __builtin_amdgcn_sched_barrier(0);  // (all operands at once would take more registers than there are)
   }
 }
 
-// Takes infinities and NaN out of the lane's 16-bit values, and says whether the wave had any.
-template <typename T, int DP>
-__device__ inline bool clear_non_finite(Tile<DP, false> &t) {
-  constexpr unsigned EXP = __is_same(T, __bf16) ? 0x7f80u : 0x7c00u;
-  bool bad = false;
+// Takes infinities and NaN out of 16-bit values; the elements of the columns that see them become NaN.  seen[c]: 1 for
+// each of the lane's keys that column c sees.
+template <typename T, int DP, int CT>
+__device__ inline void take_non_finite(State16<DP> (&s)[CT], Tile<DP, false> &t, const typename Mma16<T>::frag (&seen)[CT]) {
+  // two values a word: an exponent of ones carries into the sign's place
+  constexpr unsigned EXP = __is_same(T, __bf16) ? 0x7f807f80u : 0x7c007c00u, ONE = __is_same(T, __bf16) ? 0x00800080u : 0x04000400u;
+  constexpr unsigned UNIT = __is_same(T, __bf16) ? 0x3f80u : 0x3c00u;
+  unsigned bad = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+#pragma unroll
+    for (int w = 0; w < Tile<DP, false>::VW; ++w) bad |= ((t.v[e][w] & EXP) + ONE) & 0x80008000u;
+  if (!__any(bad != 0)) return;
+#pragma unroll
+  for (int i = 0; i < DP / 16; ++i) {
+    u32x4 x = value_words(t, i);  // (from here on: 1 where a value is not finite)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = ((((x[e] & EXP) + ONE) & 0x80008000u) >> 15) * UNIT;
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+      const f32x4 n = Mma16<T>::m16(__builtin_bit_cast(typename Mma16<T>::frag, x), seen[c], (f32x4){});
+#pragma unroll
+      for (int r = 0; r < 4; ++r) s[c].out[i][r] = n[r] > 0.0f ? __uint_as_float(0x7fc00000u) : s[c].out[i][r];
+    }
+  }
 #pragma unroll
   for (int e = 0; e < 8; ++e)
 #pragma unroll
     for (int w = 0; w < Tile<DP, false>::VW; ++w) {
-      unsigned &x = t.v[e][w];
-      const bool lo = (x & EXP) == EXP, hi = (x >> 16 & EXP) == EXP;
-      bad |= lo || hi;
-      x &= (lo ? 0xffff0000u : ~0u) & (hi ? 0xffffu : ~0u);
+      const unsigned m = ((t.v[e][w] & EXP) + ONE) & 0x80008000u;
+      t.v[e][w] &= ~((m << 1) - (m >> 15));
     }
-  return __any(bad);
 }
 
-// Adds the infinities and NaN of 16-bit values first .. first + 31 to the columns that see them.  Rare, and slow.
-template <typename T, int DP, int CT>
-__device__ inline void add_non_finite(const PagedParams &p, State16<DP> (&s)[CT], int u, int head, int first, int until,
-                                      const int (&sees)[CT]) {
-  constexpr unsigned EXP = __is_same(T, __bf16) ? 0x7f80u : 0x7c00u;
-  const int g = threadIdx.x % WAVE / 16;
-  for (int j = 0; j < 32 && first + j < until; ++j) {
-    int slot = 0;
-    const int page = page_of(p.c, u, first + j, &slot);
-    if (page < 0) continue;
-    const T *const row = (const T *)p.c.v.at + page * p.c.v.page + head * p.c.v.head + slot * p.c.v.slot;
-#pragma unroll
-    for (int i = 0; i < DP / 16; ++i)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int e = value_element<DP>(i, 4 * g + r);
-        const T x = e < p.c.dim ? row[e] : (T)0.0f;
-        const unsigned bits = __builtin_bit_cast(unsigned short, x);
-#pragma unroll
-        for (int c = 0; c < CT; ++c)
-          if ((bits & EXP) == EXP && j <= sees[c]) s[c].out[i][r] += (float)x;
-      }
-  }
+// Waves that a SIMD is to have room for: as many as leave them registers for all that a tile takes.
+constexpr int waves_a_simd(int dp, bool bits8, int ct, int aligned) {
+  if (aligned != 16) return ct == 2 || (bits8 && dp == 128) ? 1 : 2;
+  if (ct == 2) return dp == 64 ? 3 : 2;
+  return dp == 64 ? 4 : bits8 || dp == 96 ? 3 : 2;
 }
 
-constexpr int PAGED_WAVES = 4, TILE_KEYS = 32;
-
-template <typename T, int DP, bool BITS8, int CT, bool IN_PAGES>
-__global__ __launch_bounds__(PAGED_WAVES *WAVE, CT == 1 ? 2 : 1) void paged_kernel(PagedParams p) {
+// ALIGNED: 16 (InPages), 4 or 1 (Anywhere).
+template <typename T, int DP, bool BITS8, int CT, int ALIGNED, int WAVES>
+__global__ __launch_bounds__(WAVES *WAVE, waves_a_simd(DP, BITS8, CT, ALIGNED)) void paged_kernel(PagedParams p) {
   typedef typename Mma16<T>::frag frag;
-  constexpr int THREADS = PAGED_WAVES * WAVE, COLUMNS = 16 * CT, PITCH = DP + 4;
-  __shared__ __align__(16) float mix[PAGED_WAVES * COLUMNS * PITCH];
-  __shared__ float tops[PAGED_WAVES][COLUMNS], sums[PAGED_WAVES][COLUMNS];
+  constexpr int THREADS = WAVES * WAVE, COLUMNS = 16 * CT, PITCH = DP + 4;
+  __shared__ __align__(16) float mix[WAVES * COLUMNS * PITCH];
+  __shared__ float tops[WAVES][COLUMNS], sums[WAVES][COLUMNS];
   const int lane = threadIdx.x % WAVE, wave = wave_index(), l16 = lane % 16, g = lane / 16;
-  const int kv = block_index() % p.c.kv_heads, split = block_index() / p.c.kv_heads % p.splits;
-  const int tile = block_index() / p.c.kv_heads / p.splits % p.tiles, u = block_index() / p.c.kv_heads / p.splits / p.tiles;
-  if (u >= p.c.sequences) return;
-  const Newest q = newest(p, u);
-  const int rows = q.rows < p.max_queries ? q.rows : p.max_queries;
-  const int64_t columns = (int64_t)rows * p.group, column0 = (int64_t)tile * COLUMNS;
+  const int a = block_index(), b = divide(a, p.by_heads), c0 = divide(b, p.by_tiles);
+  const int kv = a - b * p.c.kv_heads, tile = b - c0 * p.tiles, column0 = tile * COLUMNS;
+  Share share;
+  if (p.shares) {
+    if (!share_of(p, c0, false, &share)) return;
+  } else {
+    if (c0 >= p.c.sequences) return;
+    share = {newest(p, c0), c0, 0, 1, 0};
+  }
+  const Newest &q = share.q;
+  const int u = share.u, rows = q.rows < p.max_queries ? q.rows : p.max_queries, columns = rows * p.group;
   if (column0 >= columns) return;
   const int shift = q.keys - q.rows;  // row i sees keys 0 .. shift + i
-  const int first_row = (int)(column0 / p.group);
-  const int last_row = (int)((column0 + COLUMNS < columns ? column0 + COLUMNS : columns) - 1) / p.group;
-  // this split's keys; the last split takes what the others leave (max_keys may be too small)
-  const int64_t from = (int64_t)split * p.each;
-  int64_t until = split + 1 < p.splits && from + p.each < q.last ? from + p.each : q.last;
-  if (from >= until && split > 0) return;
-  // what the tile's last row does not see is not read (and what it sees is there, or is no part of a column's output)
-  until = shift + last_row + 1 < until ? shift + last_row + 1 : until;
+  const int first_row = divide(column0, p.by_group);
+  const int last_row = divide((column0 + COLUMNS < columns ? column0 + COLUMNS : columns) - 1, p.by_group);
+  // what the tile's last row does not see is not read
+  const int until = shift + last_row + 1 < q.last ? shift + last_row + 1 : q.last;
   frag qf[CT][DP / 32];
   int limit[CT];
   State16<DP> s[CT];
 #pragma unroll
   for (int c = 0; c < CT; ++c) {
-    const int64_t column = column0 + c * 16 + l16;
+    const int column = column0 + c * 16 + l16;
     const bool have = column < columns;
-    const int row = have ? (int)(column / p.group) : 0, head = kv * p.group + (have ? (int)(column % p.group) : 0);
+    const int row = divide(have ? column : column0, p.by_group), head = kv * p.group + (have ? column : column0) - row * p.group;
     limit[c] = have ? shift + row : -1;
     const T *const qrow = (const T *)p.q + (q.row + row) * p.q_stride + head * p.q_head;
 #pragma unroll
@@ -502,37 +673,55 @@ __global__ __launch_bounds__(PAGED_WAVES *WAVE, CT == 1 ? 2 : 1) void paged_kern
     for (int i = 0; i < DP / 16; ++i) s[c].out[i] = (f32x4){};
   }
   const int first_limit = shift + first_row;
-  typedef typename std::conditional<IN_PAGES, InPages<T, DP, BITS8>, Anywhere<T, DP, BITS8>>::type Cache;
-  constexpr int STEP = PAGED_WAVES * TILE_KEYS;
-  Cache cache(p, u, kv, (int)until);
-  int64_t first = from + wave * TILE_KEYS;  // passes 2^31 behind the longest sequence's end
-  Tile<DP, BITS8> even, odd;
-  // Takes the tile at `first`, while the next one is loaded and the page of the one behind that is looked up.
-  auto take = [&](Tile<DP, BITS8> &now, Tile<DP, BITS8> &next) {
-    cache.load(next, first + STEP);
-    cache.find(first + 2 * STEP);
-    __builtin_amdgcn_sched_barrier(0);
-    int sees[CT];
-#pragma unroll
-    for (int c = 0; c < CT; ++c) sees[c] = (int)((limit[c] < until ? limit[c] : until - 1) - first);
-    if (first + TILE_KEYS - 1 <= first_limit && first + TILE_KEYS <= until && !__any(now.gone != 0)) {
-      attend_tile<T, DP, BITS8, CT, false>(s, qf, now, sees, p.scale);
-    } else {
-      if constexpr (!BITS8) {
-        // p = 0 of a column that does not see a value times an infinity would be NaN
-        if (clear_non_finite<T, DP>(now)) add_non_finite<T, DP, CT>(p, s, u, kv, (int)first, (int)until, sees);
-      }
-      attend_tile<T, DP, BITS8, CT, true>(s, qf, now, sees, p.scale);
-    }
-    first += STEP;
-  };
-  cache.find(first);
-  cache.load(even, first);
-  cache.find(first + STEP);
+  typedef typename std::conditional<ALIGNED == 16, InPages<T, DP, BITS8>, Anywhere<T, DP, BITS8, ALIGNED % 16>>::type Cache;
+  // A share's waves take every so many tiles, so that pages that are not there are missing from all shares alike.
+  Cache cache(p, u, kv, until, share.index * WAVES + wave, share.count * WAVES);
+  Tile<DP, BITS8> t;
+  int64_t first = cache.find(), second = cache.find();
+  cache.load_keys(t, first);
+  cache.load_values(t, first);
+  // A tile's registers are loaded again as soon as they have been read: the next keys come while p and the values' sums
+  // are formed, the next values while the next scores are, and the page of the tile behind them is looked up.
   while (first < until) {
-    take(even, odd);
-    if (first >= until) break;
-    take(odd, even);
+    const unsigned gone = cache.gone(first);
+    f32x4 sc[CT][2];
+    scores<T, DP, BITS8, CT>(sc, qf, t);
+    const int64_t third = cache.find();
+    cache.load_keys(t, second);
+    __builtin_amdgcn_sched_barrier(0);
+    if (first + TILE_KEYS - 1 > first_limit || first + TILE_KEYS > until || __any(gone != 0)) {
+      // some column does not see some key
+      frag saw[CT];
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int64_t key = first + h * 16 + g * 4 + r;
+          const bool there = key < until && !(gone >> (h * 4 + r) & 1);
+          bool good = true;
+          if constexpr (BITS8) {
+            // p = 0 of a column that does not see a value times a scale that is not finite would be NaN; whoever sees
+            // it has no finite output
+            good = fabsf(t.v_scale[h][r]) < INFINITY;
+            t.v_scale[h][r] = good ? t.v_scale[h][r] : 0.0f;
+          }
+#pragma unroll
+          for (int c = 0; c < CT; ++c) {
+            const bool seen = there && key <= limit[c];
+            sc[c][h][r] = seen ? sc[c][h][r] : -INFINITY;
+            saw[c][h * 4 + r] = (T)(seen ? 1.0f : 0.0f);
+            if (!good && seen) s[c].sum = __uint_as_float(0x7fc00000u);
+          }
+        }
+      if constexpr (!BITS8) take_non_finite<T, DP, CT>(s, t, saw);  // (likewise)
+    }
+#pragma unroll
+    for (int c = 0; c < CT; ++c) softmax<DP>(s[c], sc[c], p.scale);
+    weighted<T, DP, BITS8, CT>(s, sc, t);
+    cache.load_values(t, second);
+    __builtin_amdgcn_sched_barrier(0);
+    first = second;
+    second = third;
   }
   // the waves' results: each column's maximum, then sums and outputs relative to it
 #pragma unroll
@@ -548,7 +737,7 @@ __global__ __launch_bounds__(PAGED_WAVES *WAVE, CT == 1 ? 2 : 1) void paged_kern
   for (int c = 0; c < CT; ++c) {
     float top = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < PAGED_WAVES; ++w) top = fmaxf(top, tops[w][c * 16 + l16]);
+    for (int w = 0; w < WAVES; ++w) top = fmaxf(top, tops[w][c * 16 + l16]);
     const float f = __builtin_amdgcn_exp2f((s[c].top - base_of(top)) * p.scale);
 #pragma unroll
     for (int i = 0; i < DP / 16; ++i)
@@ -558,84 +747,107 @@ __global__ __launch_bounds__(PAGED_WAVES *WAVE, CT == 1 ? 2 : 1) void paged_kern
   }
   __syncthreads();
   for (int i = threadIdx.x; i < COLUMNS * (DP / 4); i += THREADS) {
-    const int c = i / (DP / 4), at = i % (DP / 4) * 4;
-    const int64_t col = column0 + c;
+    const int c = i / (DP / 4), at = i % (DP / 4) * 4, col = column0 + c;
     if (col >= columns || at >= p.c.dim) continue;
     float top = -INFINITY, sum = 0.0f;
 #pragma unroll
-    for (int w = 0; w < PAGED_WAVES; ++w) top = fmaxf(top, tops[w][c]);
+    for (int w = 0; w < WAVES; ++w) top = fmaxf(top, tops[w][c]);
     f32x4 y = {0, 0, 0, 0};
 #pragma unroll
-    for (int w = 0; w < PAGED_WAVES; ++w) {
+    for (int w = 0; w < WAVES; ++w) {
       sum += sums[w][c] * __builtin_amdgcn_exp2f((tops[w][c] - base_of(top)) * p.scale);
       y += *(const f32x4 *)(mix + (w * COLUMNS + c) * PITCH + at);
     }
-    if (p.splits == 1) {
+    if (share.count == 1) {
       const float f = sum > 0.0f ? 1.0f / sum : sum;
       const float z[4] = {y[0] * f, y[1] * f, y[2] * f, y[3] * f};
-      T *const out = (T *)p.out + (q.row + col / p.group) * p.out_stride + (kv * p.group + col % p.group) * p.out_head;
-      store_f32<T, 4>(out + at, z);
+      const int row = divide(col, p.by_group);
+      store_f32<T, 4>((T *)p.out + (q.row + row) * p.out_stride + (kv * p.group + col - row * p.group) * p.out_head + at, z);
     } else {
-      const int64_t group = ((int64_t)u * p.c.kv_heads + kv) * p.tiles + tile, pitch = p.c.dim + 4;
-      float *const part = p.part + ((group * p.splits + split) * COLUMNS + c) * pitch;
+      const int pitch = p.c.dim + 4;
+      float *const part = p.part + ((((int64_t)c0 * p.tiles + tile) * p.c.kv_heads + kv) * COLUMNS + c) * pitch;
       *(f32x4 *)(part + at) = y;
       if (at == 0) part[p.c.dim] = top, part[p.c.dim + 1] = sum;
     }
   }
 }
 
-constexpr int MAX_SPLITS = 256, JOIN_THREADS = 256;
-
-// A workgroup puts one column's partial results together.
-template <typename T>
-__global__ __launch_bounds__(JOIN_THREADS) void paged_join_kernel(PagedParams p) {
-  __shared__ float weight[MAX_SPLITS], mix[8][128];
-  const int columns_each = p.max_queries * p.group;
-  const int kv = block_index() % p.c.kv_heads, col = block_index() / p.c.kv_heads % columns_each;
-  const int u = block_index() / p.c.kv_heads / columns_each, tile = col / p.tile_columns;
-  if (u >= p.c.sequences) return;
-  const Newest q = newest(p, u);
-  const int rows = q.rows < p.max_queries ? q.rows : p.max_queries;
-  if (col >= rows * p.group) return;
-  const int64_t pitch = p.c.dim + 4, step = p.tile_columns * pitch;
-  const float *const part =
-      p.part + (((int64_t)u * p.c.kv_heads + kv) * p.tiles + tile) * p.splits * step + col % p.tile_columns * pitch;
-  const int used = q.last > 0 ? (q.last - 1) / p.each + 1 : 1, splits = used < p.splits ? used : p.splits;
-  const int t = threadIdx.x, lane = t % WAVE;
-  // every wave for itself: the maximum, the weights, their sum
-  float tops[MAX_SPLITS / WAVE], top = -INFINITY, sum = 0.0f;
-#pragma unroll
-  for (int i = 0; i < MAX_SPLITS / WAVE; ++i) {
-    tops[i] = i * WAVE + lane < splits ? part[(i * WAVE + lane) * step + p.c.dim] : -INFINITY;
-    top = fmaxf(top, tops[i]);
-  }
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-  const float base = base_of(top);
-#pragma unroll
-  for (int i = 0; i < MAX_SPLITS / WAVE; ++i)
-    if (i * WAVE + lane < splits) {
-      const float w = __builtin_amdgcn_exp2f((tops[i] - base) * p.scale);
-      sum += w * part[(i * WAVE + lane) * step + p.c.dim + 1];
-      if (t < WAVE) weight[i * WAVE + lane] = w;
-    }
-  sum = wave_sum(sum);
-  __syncthreads();
-  const int at = t % 32 * 4, g = t / 32;
+// EACH waves put one column's partial results together, in workgroups of four waves or EACH.  by_tiles stands for the
+// columns of a sequence here.
+template <typename T, int EACH>
+__global__ __launch_bounds__((EACH < 4 ? 4 : EACH) * WAVE) void paged_join_kernel(PagedParams p) {
+  // halves of 32 lanes, which hold four elements each, take shares in turn, MORE of them at once
+  constexpr int WAVES = EACH < 4 ? 4 : EACH, HALVES = 2 * EACH, MORE = 8;
+  __shared__ __align__(16) float mix[WAVES][128];
+  __shared__ float sums[WAVES];
+  const int lane = threadIdx.x % WAVE, wave = wave_index(), l32 = lane % 32;
+  const int64_t a0 = (int64_t)block_index() * (WAVES / EACH) + wave / EACH;
+  const int a = a0 < MAX_BLOCKS ? (int)a0 : MAX_BLOCKS;
+  const int b = divide(a, p.by_heads), u = divide(b, p.by_tiles);
+  const int kv = a - b * p.c.kv_heads, col = b - u * (p.max_queries * p.group), tile = col / p.tile_columns;
+  Share share = {};
+  // (whole waves, and with EACH > 1 whole workgroups, have nothing to do)
+  const bool some = u < p.c.sequences && share_of(p, u, true, &share) && share.count > 1 &&
+                    col < (share.q.rows < p.max_queries ? share.q.rows : p.max_queries) * p.group;
+  if (!some) return;
+  const int64_t pitch = p.c.dim + 4, step = (int64_t)p.tiles * p.c.kv_heads * p.tile_columns * pitch;
+  const float *const part = p.part + ((((int64_t)share.first * p.tiles + tile) * p.c.kv_heads + kv) * p.tile_columns + col % p.tile_columns) * pitch;
+  // a running maximum again: everything of a share is read at once
+  float top = -INFINITY, sum = 0.0f;
   f32x4 y = {0, 0, 0, 0};
-  if (at < p.c.dim) {
-#pragma unroll 4
-    for (int i = g; i < splits; i += 8) y += *(const f32x4 *)(part + i * step + at) * weight[i];
-    *(f32x4 *)(mix[g] + at) = y;
-  }
-  __syncthreads();
-  if (t < p.c.dim) {
-    float z = 0.0f;
+  const int at = l32 * 4 < p.c.dim ? l32 * 4 : 0;
+  for (int i0 = wave % EACH * 2 + lane / 32; __any(i0 < share.count); i0 += HALVES * MORE) {
+    f32x4 x[MORE];
+    float tops[MORE], parts[MORE], high = top;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) z += mix[i][t];
-    T *const out = (T *)p.out + (q.row + col / p.group) * p.out_stride + (kv * p.group + col % p.group) * p.out_head;
-    out[t] = (T)(z * (sum > 0.0f ? 1.0f / sum : sum));
+    for (int i = 0; i < MORE; ++i) {
+      const bool have = i0 + i * HALVES < share.count;
+      const float *const from = part + (have ? i0 + i * HALVES : 0) * step;
+      x[i] = *(const f32x4 *)(from + at);
+      tops[i] = have ? from[p.c.dim] : -INFINITY;
+      parts[i] = from[p.c.dim + 1];
+    }
+#pragma unroll
+    for (int i = 0; i < MORE; ++i) high = fmaxf(high, tops[i]);
+    const float base = base_of(high), f = __builtin_amdgcn_exp2f((top - base) * p.scale);
+    top = high;
+    sum *= f;
+    y *= f;
+#pragma unroll
+    for (int i = 0; i < MORE; ++i) {
+      const bool have = i0 + i * HALVES < share.count;  // (others are repeated, and may hold anything)
+      const float w = __builtin_amdgcn_exp2f((tops[i] - base) * p.scale);
+      sum += have ? w * parts[i] : 0.0f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) y[j] += have ? w * x[i][j] : 0.0f;
+    }
   }
+  // the two halves', then the waves' results
+  auto both = [&](float top2, float sum2, f32x4 y2) {
+    const float high = fmaxf(top, top2), base = base_of(high);
+    const float f = __builtin_amdgcn_exp2f((top - base) * p.scale), f2 = __builtin_amdgcn_exp2f((top2 - base) * p.scale);
+    top = high;
+    sum = sum * f + sum2 * f2;
+    y = y * f + y2 * f2;
+  };
+  f32x4 other;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) other[i] = __shfl_xor(y[i], 32);
+  both(__shfl_xor(top, 32), __shfl_xor(sum, 32), other);
+  if constexpr (EACH > 1) {
+    __shared__ float tops[WAVES];
+    if (lane < 32) *(f32x4 *)(mix[wave] + l32 * 4) = y;
+    if (lane == 0) tops[wave] = top, sums[wave] = sum;
+    __syncthreads();
+    if (wave) return;
+#pragma unroll
+    for (int w = 1; w < EACH; ++w) both(tops[w], sums[w], *(const f32x4 *)(mix[w] + l32 * 4));
+  }
+  if (lane >= 32 || l32 * 4 >= p.c.dim) return;
+  const float f = sum > 0.0f ? 1.0f / sum : sum;
+  const float z[4] = {y[0] * f, y[1] * f, y[2] * f, y[3] * f};
+  const int row = divide(col, p.by_group);
+  store_f32<T, 4>((T *)p.out + (share.q.row + row) * p.out_stride + (kv * p.group + col - row * p.group) * p.out_head + l32 * 4, z);
 }
 
 // ------------------------------------------------------------------ host side
@@ -657,35 +869,43 @@ bool has_work(const jdob_edge_attend_paged_args *a) {
 
 struct PagedPlan {
   int64_t tiles;
-  int queries, columns, splits, each;  // columns: of a tile
+  int queries, columns, shares;  // columns: of a tile
+  int64_t list;                  // of shares (or sequences) that there may be
 };
 
 PagedPlan paged_plan(const jdob_edge_attend_paged_args *a) {
   const int64_t queries = a->max_queries < a->query_rows ? a->max_queries : a->query_rows;  // no sequence has more
-  const int64_t room = (int64_t)a->table_width * a->cache.page_size;
+  const int64_t room = (int64_t)a->table_width * a->cache.page_size, n = a->num_sequences;
   const int64_t keys = a->max_keys < room ? a->max_keys : room;
   const int64_t all = queries * (a->num_heads / a->cache.num_kv_heads);
   const int columns = all <= 16 ? 16 : 32;
-  const int64_t tiles = (all + columns - 1) / columns, groups = tiles * a->cache.num_kv_heads * a->num_sequences;
-  // about four workgroups for each place that the chip has for one (two a compute unit), whose sequences may be
-  // of very different lengths, but no fewer than 512 keys each
-  int64_t each = groups < 2048 ? (keys * groups + 2047) / 2048 : keys;
-  each = each < 512 ? 512 : (each + 127) & ~127;
-  int64_t splits = (keys + each - 1) / each;
-  if (splits > MAX_SPLITS) {
-    each = ((keys + MAX_SPLITS - 1) / MAX_SPLITS + 127) & ~127;
-    splits = (keys + each - 1) / each;
-  }
-  return {tiles, (int)queries, columns, (int)(splits < 1 ? 1 : splits), (int)(each < INT32_MAX ? each : INT32_MAX)};
+  const int64_t tiles = (all + columns - 1) / columns, layers = tiles * a->cache.num_kv_heads;
+  const int64_t groups = layers * n, most = n * ((keys + LEAST_KEYS - 1) / LEAST_KEYS);
+  // How many shares: few sequences' fill the chip once, two workgroups a compute unit, with half a share a sequence lost
+  // at its end (one of 131,072 8-bit keys, 8 key heads: 53 us, with 128 shares a head 61); many, whose lengths may be
+  // anything, are dealt twice as finely (32 of 15 to 8191 keys: 98 us, 114 as for few; 64 of up to 8191: 121 and 134;
+  // but 64 of 2047 each 58 and 52).
+  int64_t shares = groups <= 128 ? (512 - groups / 2) / layers : 1024 / layers;
+  shares = shares < 1 ? 1 : shares < most ? shares : most;
+  // Not at all where the join, a launch of 5 us, costs more than it gives: 512 keys take 11 us in one workgroup and 14 in
+  // two; many sequences fill the chip, and one of 8192 keys among them ends 100 us after the others at most.  Forming the
+  // list takes two looks at every 64 sequences.
+  if (keys <= 512 || (groups >= 2048 && keys <= 8192) || n > 1024) shares = 0;
+  return {tiles, (int)queries, columns, (int)shares, n + shares};
+}
+
+template <typename T, int DP, bool BITS8, int CT>
+int paged(const PagedParams &p, int aligned, int64_t blocks, hipStream_t stream) {
+  constexpr int WAVES = 4;
+  return launch(aligned == 16  ? paged_kernel<T, DP, BITS8, CT, 16, WAVES>
+                : aligned == 4 ? paged_kernel<T, DP, BITS8, CT, 4, WAVES>
+                               : paged_kernel<T, DP, BITS8, CT, 1, WAVES>,
+                blocks, WAVES * WAVE, stream, p);
 }
 
 template <typename T, int DP, bool BITS8>
-int paged(const PagedParams &p, int columns, bool in_pages, int64_t blocks, hipStream_t stream) {
-  if (columns == 16)
-    return launch(in_pages ? paged_kernel<T, DP, BITS8, 1, true> : paged_kernel<T, DP, BITS8, 1, false>, blocks,
-                  PAGED_WAVES * WAVE, stream, p);
-  return launch(in_pages ? paged_kernel<T, DP, BITS8, 2, true> : paged_kernel<T, DP, BITS8, 2, false>, blocks,
-                PAGED_WAVES * WAVE, stream, p);
+int paged(const PagedParams &p, int columns, int aligned, int64_t blocks, hipStream_t stream) {
+  return columns == 16 ? paged<T, DP, BITS8, 1>(p, aligned, blocks, stream) : paged<T, DP, BITS8, 2>(p, aligned, blocks, stream);
 }
 
 // Whether a pool's rows can be read as InPages reads them; 16 rows have to stay within a window, whose offsets pass
@@ -697,21 +917,24 @@ bool in_pages(const Pool &x, bool bits8) {
 }
 
 template <typename T, bool BITS8>
-int paged(const PagedParams &p, const PagedPlan &f, hipStream_t stream) {
+int paged(PagedParams p, const PagedPlan &f, hipStream_t stream) {
   // (8-bit keys are read 16 elements at once up to 64, and beyond 96 to 128)
   const bool in = p.c.page_size % 16 == 0 && in_pages(p.c.k, BITS8) && in_pages(p.c.v, BITS8) &&
                   (!BITS8 || p.c.dim % 16 == 0 || (p.c.dim > 64 && p.c.dim <= 96));
-  const int64_t groups = (int64_t)p.c.sequences * p.c.kv_heads * f.tiles;
-  const int64_t all = (int64_t)p.c.sequences * p.c.kv_heads * f.queries * p.group;
-  // (each factor is below 2^31, and tiles are fewer than columns)
-  if (f.tiles > MAX_BLOCKS || groups > MAX_BLOCKS || groups * f.splits > MAX_BLOCKS || (f.splits > 1 && all > MAX_BLOCKS))
-    return JDOB_ERR_UNSUPPORTED;
-  const int64_t blocks = groups * f.splits;
-  const int code = p.c.dim <= 64   ? paged<T, 64, BITS8>(p, f.columns, in, blocks, stream)
-                   : p.c.dim <= 96 ? paged<T, 96, BITS8>(p, f.columns, in, blocks, stream)
-                                   : paged<T, 128, BITS8>(p, f.columns, in, blocks, stream);
-  if (code != JDOB_OK || f.splits == 1) return code;
-  return launch(paged_join_kernel<T>, all, JOIN_THREADS, stream, p);
+  const int aligned = in ? 16 : p.c.page_size % 4 == 0 ? 4 : 1;
+  const int64_t each = (int64_t)f.queries * p.group, all = each * p.c.sequences * p.c.kv_heads;
+  const int64_t blocks = f.list * p.c.kv_heads * f.tiles;
+  // (tiles are fewer than columns, whose numbers within a sequence are divided)
+  if (each >= 1 << 30 || blocks > MAX_BLOCKS || (f.shares && all > MAX_BLOCKS)) return JDOB_ERR_UNSUPPORTED;
+  p.by_heads = divide_by(p.c.kv_heads), p.by_tiles = divide_by((int)f.tiles), p.by_group = divide_by(p.group);
+  const int code = p.c.dim <= 64   ? paged<T, 64, BITS8>(p, f.columns, aligned, blocks, stream)
+                   : p.c.dim <= 96 ? paged<T, 96, BITS8>(p, f.columns, aligned, blocks, stream)
+                                   : paged<T, 128, BITS8>(p, f.columns, aligned, blocks, stream);
+  if (code != JDOB_OK || !f.shares) return code;
+  p.by_tiles = divide_by((int)each);
+  // few columns of many shares
+  if (f.shares >= 16 * p.c.sequences) return launch(paged_join_kernel<T, 8>, all, 8 * WAVE, stream, p);
+  return launch(paged_join_kernel<T, 1>, (all + 3) / 4, 4 * WAVE, stream, p);
 }
 
 }  // namespace
@@ -722,9 +945,8 @@ extern "C" int64_t jdob_edge_attend_paged_workspace(const jdob_edge_attend_paged
   if (paged_check_sizes(a) != JDOB_OK) return -1;
   if (!has_work(a)) return 0;
   const PagedPlan f = paged_plan(a);
-  if (f.splits == 1) return 0;
-  return (int64_t)a->num_sequences * a->cache.num_kv_heads * f.tiles * f.splits * f.columns * (a->cache.head_dim + 4) *
-         (int64_t)sizeof(float);
+  if (!f.shares) return 0;
+  return f.list * a->cache.num_kv_heads * f.tiles * f.columns * (a->cache.head_dim + 4) * (int64_t)sizeof(float);
 }
 
 extern "C" int jdob_edge_attend_paged(const jdob_edge_attend_paged_args *a, void *hip_stream) {
@@ -745,7 +967,7 @@ extern "C" int jdob_edge_attend_paged(const jdob_edge_attend_paged_args *a, void
                                   a->key_count),
                          a->num_heads, a->num_heads / a->cache.num_kv_heads, f.queries, f.columns,
                          a->scale * 1.44269504088896f, a->query_rows, (const char *)a->q, (char *)a->out, a->q_stride,
-                         a->q_head_stride, a->out_stride, a->out_head_stride, f.splits, f.each, (int)f.tiles,
+                         a->q_head_stride, a->out_stride, a->out_head_stride, (int)f.tiles, f.shares, {}, {}, {},
                          (float *)a->workspace};
   hipStream_t stream = (hipStream_t)hip_stream;
   if (a->cache.dtype == JDOB_EDGE_BF16)

@@ -5,8 +5,9 @@
 
 namespace edge {
 
-// x / by for 0 <= x < 2^31 and 1 <= by <= 2^16: with 2^(l-1) < by <= 2^l and mul = ceil(2^(31+l) / by) the error
-// mul * by - 2^(31+l) is below 2^l, so that x * mul / 2^(31+l) is never a whole number too large.
+// x / by for 0 <= x < 2^31 and 1 <= by <= 2^30: with 2^(l-1) < by <= 2^l and mul = ceil(2^(31+l) / by) the error
+// mul * by - 2^(31+l) is below 2^l, so that x * mul / 2^(31+l) is never a
+// whole number too large; mul is below 2^32, being at most 2^32 - 2^(33-l) + 1 or, of a power of two, 2^31.
 struct Divide {
   unsigned mul, shift;
 };

@@ -258,20 +258,25 @@ def test_nothing_to_do():
 
 @pytest.mark.parametrize("bits8", [False, True])
 def test_equal_calls_give_equal_bits_whatever_stands_beside(bits8):
-    """A sequence's rows do not depend on the batch, nor on the call."""
+    """What a sequence's rows become does not depend on the call, nor on what its neighbours' rows, keys and values are
+    (how the keys are split follows from all sequences' lengths)."""
     new, keys = [1, 1, 2], [5000, 77, 300]
     s = model.inputs(new, keys, 16, 2, 128, BF16, bits8, 4)
     want = call(s, new, keys)
     for _ in range(3):
         assert torch.equal(call(s, new, keys), want)
-    # alone, with the hints of the batch (they choose how keys are split)
     at = s["row_start"].tolist()
-    for u in (1, 2):
-        alone = {**s, "q": s["q"][at[u]:at[u + 1]], "table": s["table"][u:u + 1], "key_count": s["key_count"][u:u + 1],
-                 "row_start": torch.tensor([0, new[u]], dtype=torch.int32, device="cuda")}
-        got = edge.attend_paged(alone["q"], s["cache"], alone["table"], alone["row_start"], alone["key_count"], max_queries=2,
-                                max_keys=500)
-        assert torch.equal(got, want[at[u]:at[u + 1]]), u
+    for u in range(3):
+        mine = torch.zeros(s["cache"]["k"].shape[0], dtype=torch.bool, device="cuda")
+        mine[s["table"][u, :-(-keys[u] // 16)].long()] = True
+        cache = {n: None if t is None else t.clone() for n, t in s["cache"].items()}
+        for n in ("v_scale", "k_scale") if bits8 else ("k", "v"):
+            cache[n][~mine] *= 7
+        q = s["q"] * 3
+        q[at[u]:at[u + 1]] = s["q"][at[u]:at[u + 1]]
+        got = call({**s, "q": q, "cache": cache}, new, keys)
+        assert torch.equal(got[at[u]:at[u + 1]], want[at[u]:at[u + 1]]), u
+        assert not torch.equal(got, want)
 
 
 @pytest.mark.parametrize("bits8", [False, True])
