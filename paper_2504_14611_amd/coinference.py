@@ -8,7 +8,8 @@ sub-task; here the edge operators (edge.norm, edge.project, edge.attend) are tha
 2. `instance` puts them with the devices, uplinks and deadlines into a problem, which jdob.solve_batch decides:
    the partition point s, the GPU level, and which users offload,
 3. `Edge` computes blocks s+1..L for the offloaded users' rows in one batch, all users' rows packed one after the
-   other, and keeps their keys and values, so that it can go on with single tokens.
+   other, and keeps their keys and values, so that it can go on with single tokens: in a slab a user, or on pages that
+   all users share, 16-bit or in 8 bits (edge.cache_write, edge.cache_read, edge.attend_paged).
 
 A block:  h += x;  q, k, v = norm(h) Wqkv;  x = attend(q, k, v) Wo;  h += x;  x = gelu(norm(h) Wup) Wdown.
 Wqkv and Wup take the norm's 8-bit rows and have 8-bit weights; Wo and Wdown are 16-bit.  Weights and rows are
@@ -20,7 +21,7 @@ from __future__ import annotations
 import argparse
 import dataclasses
 import time
-from typing import Dict, List, Sequence
+from typing import Dict, List, Optional, Sequence
 
 import numpy as np
 
@@ -82,15 +83,50 @@ class Edge:
     """Blocks first..L of the chain for a batch of users, with their keys and values.
 
     Every user has a slab of `room` rows in each block's cache; new keys and values are written behind those that
-    stand there already."""
+    stand there already.  With `page` the cache is made of `pages` pages of so many keys (default: as many as all users
+    may fill), which users take as they grow; it holds 8-bit rows with bits8."""
 
-    def __init__(self, shape: Shape, chain: Sequence[dict], users: Sequence[int], first: int, room: int, device="cuda"):
+    FEW = 8  # rows a user that go over the pages as they are; more read them back first
+
+    def __init__(self, shape: Shape, chain: Sequence[dict], users: Sequence[int], first: int, room: int, device="cuda",
+                 page: int = 0, bits8: bool = False, pages: Optional[int] = None):
         import torch
         self.shape, self.chain, self.users, self.device = shape, list(chain[first:]), list(users), device
-        self.room, self.count = room, [0] * len(self.users)
+        self.room, self.count, self.page = room, [0] * len(self.users), page
+        if page:
+            each = -(-room // page)
+            pages = len(self.users) * each if pages is None else pages
+            self.free, self.held = list(range(pages))[::-1], [[] for _ in self.users]
+            self.cache = [edge.make_cache(pages, page, shape.kv_heads, shape.head_dim, bits8=bits8, device=device)
+                          for _ in self.chain]
+            return
+        if bits8 or pages is not None:
+            raise ValueError("slabs are 16-bit and have no pages")
         n = len(self.users) * room
         self.cache = [torch.zeros((n, 2, shape.kv_heads, shape.head_dim), dtype=torch.bfloat16, device=device)
                       for _ in self.chain]
+
+    def _take_pages(self, counts: Sequence[int]):
+        """Pages for so many keys of every user (the same ones in all blocks), and the table of all users' pages."""
+        import torch
+        need = [-(-m // self.page) - len(held) for m, held in zip(counts, self.held)]
+        if sum(max(0, n) for n in need) > len(self.free):
+            raise ValueError(f"the cache has {len(self.free)} pages left")
+        for n, held in zip(need, self.held):
+            held += [self.free.pop() for _ in range(n)]
+        width = max(map(len, self.held), default=0)
+        return torch.tensor([held + [-1] * (width - len(held)) for held in self.held], dtype=torch.int32,
+                            device=self.device).view(len(self.users), width)
+
+    def _attend_pages(self, q, k, v, cache, table, query_start, key_count, all_start, lengths, counts):
+        """The rows' keys and values into the cache, and their attention."""
+        edge.cache_write(k, v, cache, table, query_start, key_count)
+        most, longest = max(lengths), max(counts)
+        if most <= self.FEW:
+            return edge.attend_paged(q, cache, table, query_start, key_count, max_queries=most, max_keys=longest)
+        if any(c > m for c, m in zip(counts, lengths)):  # chunks after a history
+            k, v = edge.cache_read(cache, table, all_start, key_count, rows=sum(counts), dtype=q.dtype)
+        return edge.attend(q, k, v, query_start, all_start[:-1].long(), key_count, max_queries=most, max_keys=longest)
 
     def run(self, rows, lengths: Sequence[int]):
         """`rows` [sum of lengths, width]: each user's new rows behind each other, as they enter the first block.
@@ -110,8 +146,12 @@ class Edge:
         counts = [c + m for c, m in zip(self.count, lengths)]
         key_count = torch.tensor(counts, dtype=torch.int32, device=dev)
         row_adapter = torch.tensor(np.repeat(np.asarray(self.users, dtype=np.int32), lengths), device=dev)
-        slots = torch.tensor(np.concatenate([u * self.room + c + np.arange(m) for u, (c, m) in
-                                             enumerate(zip(self.count, lengths))]).astype(np.int64), device=dev)
+        if self.page:
+            table = self._take_pages(counts)
+            all_start = torch.tensor([sum(counts[:u]) for u in range(n + 1)], dtype=torch.int32, device=dev)
+        else:
+            slots = torch.tensor(np.concatenate([u * self.room + c + np.arange(m) for u, (c, m) in
+                                                 enumerate(zip(self.count, lengths))]).astype(np.int64), device=dev)
 
         def project(part, x, scale=None):
             return edge.project(x, part["weight"], x_scale=scale, weight_scale=part.get("weight_scale"),
@@ -122,9 +162,13 @@ class Edge:
             r = edge.norm(h if x is None else x, block["first"], residual=None if x is None else h, bits8=True)
             h = h if x is None else r["sum"]
             qkv = project(block["qkv"], r["q"], r["scale"]).view(-1, s.heads + 2 * s.kv_heads, s.head_dim)
-            cache[slots] = qkv[:, s.heads:].reshape(-1, 2, s.kv_heads, s.head_dim)
-            y = edge.attend(qkv[:, :s.heads], cache[:, 0], cache[:, 1], query_start, key_start, key_count,
-                            max_queries=max(lengths), max_keys=max(counts))
+            if self.page:
+                y = self._attend_pages(qkv[:, :s.heads], qkv[:, s.heads:s.heads + s.kv_heads], qkv[:, s.heads + s.kv_heads:],
+                                       cache, table, query_start, key_count, all_start, lengths, counts)
+            else:
+                cache[slots] = qkv[:, s.heads:].reshape(-1, 2, s.kv_heads, s.head_dim)
+                y = edge.attend(qkv[:, :s.heads], cache[:, 0], cache[:, 1], query_start, key_start, key_count,
+                                max_queries=max(lengths), max_keys=max(counts))
             r = edge.norm(project(block["o"], y.view(-1, s.width)), block["second"], residual=h, bits8=True)
             h = r["sum"]
             x = project(block["down"], F.gelu(project(block["up"], r["q"], r["scale"])))
@@ -182,14 +226,16 @@ def instance(shape: Shape, users: int, tokens: int, alpha: float, beta: float, s
 
 
 def carry_out(shape: Shape, chain: Sequence[dict], cut: int, offloaders: Sequence[int], rows: dict, more: int = 0,
-              device="cuda"):
+              device="cuda", page: int = 0, bits8: bool = False):
     """The offloaders' prompts (`rows`: user -> [tokens, width]) through the chain: blocks 1..cut each on their own
     device, the others in one batch on the edge, then `more` further single rows a user the same way, each the row
-    that left the last block before it.  Returns user -> the rows that left the last block."""
+    that left the last block before it.  `page` and `bits8` are the edge's cache.  Returns user -> the rows that left
+    the last block."""
     import torch
     lengths = [rows[u].shape[0] for u in offloaders]
     devices = [Edge(shape, chain[:cut], [u], 0, n + more, device) for u, n in zip(offloaders, lengths)]
-    e = Edge(shape, chain, offloaders, cut, max(lengths) + more, device)
+    e = Edge(shape, chain, offloaders, cut, max(lengths) + more, device, page, bits8,
+             sum(-(-(n + more) // page) for n in lengths) if page else None)
 
     def through(entering):
         sent = [d.run(x, [x.shape[0]]) for d, x in zip(devices, entering)]
@@ -208,6 +254,8 @@ def main(argv=None) -> Dict[str, object]:
     p.add_argument("--users", type=int, default=16)
     p.add_argument("--tokens", type=int, default=256, help="of the longest prompt")
     p.add_argument("--more", type=int, default=8, help="single tokens after the prompts")
+    p.add_argument("--page", type=int, default=0, help="keys on a page of the edge's cache (0: a slab a user)")
+    p.add_argument("--cache-bits", type=int, choices=(8, 16), default=16, help="of the keys and values on its pages")
     for field in dataclasses.fields(Shape):
         p.add_argument("--" + field.name.replace("_", "-"), type=int, default=field.default)
     a = p.parse_args(argv)
@@ -229,10 +277,11 @@ def main(argv=None) -> Dict[str, object]:
         r = np.random.RandomState(1)
         rows = {u: torch.randn(int(r.randint(max(1, a.tokens // 4), a.tokens + 1)), shape.width, device="cuda").bfloat16()
                 for u in offloaders}
-        carry_out(shape, chain, cut, offloaders, rows, 1)
+        kept = {"page": a.page, "bits8": a.cache_bits == 8}
+        carry_out(shape, chain, cut, offloaders, rows, 1, **kept)
         torch.cuda.synchronize()
         t = time.perf_counter()
-        out = carry_out(shape, chain, cut, offloaders, rows, a.more)
+        out = carry_out(shape, chain, cut, offloaders, rows, a.more, **kept)
         torch.cuda.synchronize()
         t = time.perf_counter() - t
         print(f"carried out: {sum(map(len, rows.values()))} rows and {a.more} further ones a user in {t * 1e3:.2f} ms; "
