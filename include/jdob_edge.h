@@ -230,8 +230,10 @@ int jdob_edge_cache_read(const jdob_edge_cache_rows_args *a, void *hip_stream);
  * query_start[u] .. query_start[u+1]-1 stand at the end of its key_count[u]
  * keys and see those of them that are there.  Made for few rows a sequence:
  * the keys are read once for every 32 rows times heads of a key head.  All
- * else is as in jdob_edge_attend; with an 8-bit cache p * scale of the value
- * keeps 16 bits in its product with the codes.                              */
+ * else is as in jdob_edge_attend, but that p (with an 8-bit cache p * scale of
+ * the value) goes into its product as two 16-bit parts: 16 bits of mantissa,
+ * or 22 with a binary16 cache.  How the keys are split, and with it the order
+ * of sums, follows from the lengths of all sequences.                       */
 typedef struct {
   jdob_edge_cache cache;
   int32_t num_sequences, table_width;
