@@ -624,7 +624,7 @@ __device__ inline void take_non_finite(State16<DP> (&s)[CT], Tile<DP, false> &t,
 
 // Waves that a SIMD is to have room for: as many as leave them registers for all that a tile takes.
 constexpr int waves_a_simd(int dp, bool bits8, int ct, int aligned) {
-  if (aligned != 16) return ct == 2 || (bits8 && dp == 128) ? 1 : 2;
+  if (aligned != 16) return aligned == 1 && bits8 && dp == 128 ? 1 : 2;
   if (ct == 2) return dp == 64 ? 3 : 2;
   return dp == 64 ? 4 : bits8 || dp == 96 ? 3 : 2;
 }
@@ -876,12 +876,17 @@ struct PagedPlan {
   int64_t list;                  // of shares (or sequences) that there may be
 };
 
-PagedPlan paged_plan(const jdob_edge_attend_paged_args *a) {
+// `in_pages`: InPages reads the cache.
+PagedPlan paged_plan(const jdob_edge_attend_paged_args *a, bool in_pages) {
   const int64_t queries = a->max_queries < a->query_rows ? a->max_queries : a->query_rows;  // no sequence has more
   const int64_t room = (int64_t)a->table_width * a->cache.page_size, n = a->num_sequences;
   const int64_t keys = a->max_keys < room ? a->max_keys : room;
   const int64_t all = queries * (a->num_heads / a->cache.num_kv_heads);
-  const int columns = all <= 16 ? 16 : 32;
+  // Keys that are read once for 32 columns, not twice: 16 users' 4 rows of 64 heads after up to 16,383 8-bit keys take 84 us
+  // so and 106 by 16 columns, after up to 4095 34 and 40.  By 16 columns, where waves need half the registers, if there
+  // are few keys (4 users, up to 1023 keys: 14 us and 17) or InPages does not read them (24 users' drafts on pages of
+  // 20 keys: 25 us and 32).
+  const int columns = all <= 16 || !in_pages || n * keys * a->cache.num_kv_heads <= 1 << 17 ? 16 : 32;
   const int64_t tiles = (all + columns - 1) / columns, layers = tiles * a->cache.num_kv_heads;
   const int64_t groups = layers * n, most = n * ((keys + LEAST_KEYS - 1) / LEAST_KEYS);
   // How many shares: few sequences' fill the chip once, two workgroups a compute unit, with half a share a sequence lost
@@ -897,42 +902,39 @@ PagedPlan paged_plan(const jdob_edge_attend_paged_args *a) {
   return {tiles, (int)queries, columns, (int)shares, n + shares};
 }
 
-template <typename T, int DP, bool BITS8, int CT>
+template <typename T, int DP, bool BITS8>
 int paged(const PagedParams &p, int aligned, int64_t blocks, hipStream_t stream) {
   constexpr int WAVES = 4;
-  return launch(aligned == 16  ? paged_kernel<T, DP, BITS8, CT, 16, WAVES>
-                : aligned == 4 ? paged_kernel<T, DP, BITS8, CT, 4, WAVES>
-                               : paged_kernel<T, DP, BITS8, CT, 1, WAVES>,
+  return launch(p.tile_columns == 32 ? paged_kernel<T, DP, BITS8, 2, 16, WAVES>
+                : aligned == 16      ? paged_kernel<T, DP, BITS8, 1, 16, WAVES>
+                : aligned == 4       ? paged_kernel<T, DP, BITS8, 1, 4, WAVES>
+                                     : paged_kernel<T, DP, BITS8, 1, 1, WAVES>,
                 blocks, WAVES * WAVE, stream, p);
 }
 
-template <typename T, int DP, bool BITS8>
-int paged(const PagedParams &p, int columns, int aligned, int64_t blocks, hipStream_t stream) {
-  return columns == 16 ? paged<T, DP, BITS8, 1>(p, aligned, blocks, stream) : paged<T, DP, BITS8, 2>(p, aligned, blocks, stream);
-}
-
-// Whether a pool's rows can be read as InPages reads them; 16 rows have to stay within a window, whose offsets pass
-// 2^31 nowhere.
-bool in_pages(const Pool &x, bool bits8) {
-  const int64_t unit = bits8 ? 16 : 8;
-  return (uintptr_t)x.at % 16 == 0 && x.page % unit == 0 && x.head % unit == 0 && x.slot % unit == 0 && x.slot < (1 << 24) &&
-         (!bits8 || x.scale_slot == 1);
+// Whether InPages can read the cache; 16 rows have to stay within a window, whose offsets pass 2^31 nowhere.
+bool in_pages(const jdob_edge_cache &c) {
+  const int64_t unit = c.bits8 ? 16 : 8;
+  auto pool = [&](const void *at, int64_t page, int64_t head, int64_t slot, int64_t scale_slot) {
+    return (uintptr_t)at % 16 == 0 && page % unit == 0 && head % unit == 0 && slot % unit == 0 && slot < (1 << 24) &&
+           (!c.bits8 || scale_slot == 1);
+  };
+  // (8-bit keys are read 16 elements at once up to 64, and beyond 96 to 128)
+  return c.page_size % 16 == 0 && pool(c.k, c.k_page_stride, c.k_head_stride, c.k_slot_stride, c.k_scale_slot_stride) &&
+         pool(c.v, c.v_page_stride, c.v_head_stride, c.v_slot_stride, c.v_scale_slot_stride) &&
+         (!c.bits8 || c.head_dim % 16 == 0 || (c.head_dim > 64 && c.head_dim <= 96));
 }
 
 template <typename T, bool BITS8>
-int paged(PagedParams p, const PagedPlan &f, hipStream_t stream) {
-  // (8-bit keys are read 16 elements at once up to 64, and beyond 96 to 128)
-  const bool in = p.c.page_size % 16 == 0 && in_pages(p.c.k, BITS8) && in_pages(p.c.v, BITS8) &&
-                  (!BITS8 || p.c.dim % 16 == 0 || (p.c.dim > 64 && p.c.dim <= 96));
-  const int aligned = in ? 16 : p.c.page_size % 4 == 0 ? 4 : 1;
+int paged(PagedParams p, const PagedPlan &f, int aligned, hipStream_t stream) {
   const int64_t each = (int64_t)f.queries * p.group, all = each * p.c.sequences * p.c.kv_heads;
   const int64_t blocks = f.list * p.c.kv_heads * f.tiles;
   // (tiles are fewer than columns, whose numbers within a sequence are divided)
   if (each >= 1 << 30 || blocks > MAX_BLOCKS || (f.shares && all > MAX_BLOCKS)) return JDOB_ERR_UNSUPPORTED;
   p.by_heads = divide_by(p.c.kv_heads), p.by_tiles = divide_by((int)f.tiles), p.by_group = divide_by(p.group);
-  const int code = p.c.dim <= 64   ? paged<T, 64, BITS8>(p, f.columns, aligned, blocks, stream)
-                   : p.c.dim <= 96 ? paged<T, 96, BITS8>(p, f.columns, aligned, blocks, stream)
-                                   : paged<T, 128, BITS8>(p, f.columns, aligned, blocks, stream);
+  const int code = p.c.dim <= 64   ? paged<T, 64, BITS8>(p, aligned, blocks, stream)
+                   : p.c.dim <= 96 ? paged<T, 96, BITS8>(p, aligned, blocks, stream)
+                                   : paged<T, 128, BITS8>(p, aligned, blocks, stream);
   if (code != JDOB_OK || !f.shares) return code;
   p.by_tiles = divide_by((int)each);
   // few columns of many shares
@@ -947,9 +949,14 @@ extern "C" int64_t jdob_edge_attend_paged_workspace(const jdob_edge_attend_paged
   using namespace edge;
   if (paged_check_sizes(a) != JDOB_OK) return -1;
   if (!has_work(a)) return 0;
-  const PagedPlan f = paged_plan(a);
-  if (!f.shares) return 0;
-  return f.list * a->cache.num_kv_heads * f.tiles * f.columns * (a->cache.head_dim + 4) * (int64_t)sizeof(float);
+  // (whether InPages reads the cache follows from its arrays, too)
+  int64_t most = 0;
+  for (bool in : {false, true}) {
+    const PagedPlan f = paged_plan(a, in);
+    const int64_t columns = f.shares ? f.list * a->cache.num_kv_heads * f.tiles * f.columns : 0;
+    most = columns > most ? columns : most;
+  }
+  return most * (a->cache.head_dim + 4) * (int64_t)sizeof(float);
 }
 
 extern "C" int jdob_edge_attend_paged(const jdob_edge_attend_paged_args *a, void *hip_stream) {
@@ -965,7 +972,9 @@ extern "C" int jdob_edge_attend_paged(const jdob_edge_attend_paged_args *a, void
     return JDOB_ERR_INVALID_ARG;
   const int64_t need = jdob_edge_attend_paged_workspace(a);
   if (need > 0 && (!a->workspace || (uintptr_t)a->workspace % 16 || a->workspace_bytes < need)) return JDOB_ERR_INVALID_ARG;
-  const PagedPlan f = paged_plan(a);
+  const bool in = in_pages(a->cache);
+  const int aligned = in ? 16 : a->cache.page_size % 4 == 0 ? 4 : 1;
+  const PagedPlan f = paged_plan(a, in);
   const PagedParams p = {pages_of(a->cache, a->num_sequences, a->table_width, a->table, a->table_stride, a->query_start,
                                   a->key_count),
                          a->num_heads, a->num_heads / a->cache.num_kv_heads, f.queries, f.columns,
@@ -974,6 +983,6 @@ extern "C" int jdob_edge_attend_paged(const jdob_edge_attend_paged_args *a, void
                          (float *)a->workspace};
   hipStream_t stream = (hipStream_t)hip_stream;
   if (a->cache.dtype == JDOB_EDGE_BF16)
-    return a->cache.bits8 ? paged<__bf16, true>(p, f, stream) : paged<__bf16, false>(p, f, stream);
-  return a->cache.bits8 ? paged<_Float16, true>(p, f, stream) : paged<_Float16, false>(p, f, stream);
+    return a->cache.bits8 ? paged<__bf16, true>(p, f, aligned, stream) : paged<__bf16, false>(p, f, aligned, stream);
+  return a->cache.bits8 ? paged<_Float16, true>(p, f, aligned, stream) : paged<_Float16, false>(p, f, aligned, stream);
 }

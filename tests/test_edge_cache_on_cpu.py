@@ -48,6 +48,11 @@ def run(c):
     gone = [tuple(x) for x in c.get("gone", ())]
     s = model.inputs(new, keys, page, g, d, dt, c["bits8"], c.get("group", 1), device="cpu", gone=gone, spare=c.get("spare", 1))
     kind, cache = cache_of(s, c, shift)
+    longest = max(keys)
+    if c.get("wide"):  # a table and a hint of many keys: 32 columns at once, keys split
+        more = torch.full((len(keys), 140000 // page), -1, dtype=torch.int32)
+        more[:, :s["table"].shape[1]] = s["table"]
+        s["table"], longest = more, 140000
     table, start, count = (guarded(s[n]) for n in ("table", "row_start", "key_count"))
     n, width, rows = len(keys), table.shape[1], sum(new)
     if c["op"] == "attend":
@@ -60,7 +65,7 @@ def run(c):
             else:
                 kind["v"][spot] = float("inf")
         q, out = guarded(s["q"], shift), guarded(torch.full((rows, h, d), 7.0, dtype=dt))
-        a = edge.AttendPagedArgs(cache, n, width, ptr(table), width, ptr(start), ptr(count), h, max(new), max(keys), d ** -0.5, rows,
+        a = edge.AttendPagedArgs(cache, n, width, ptr(table), width, ptr(start), ptr(count), h, max(new), longest, d ** -0.5, rows,
                                  ptr(q), h * d, d, ptr(out), h * d, d)
         need = lib.jdob_edge_attend_paged_workspace(C.byref(a))
         space = guarded(torch.full((max(need, 1),), 255, dtype=torch.uint8))
@@ -161,5 +166,6 @@ def test_attend(run, dim, page):
              for new, keys, g, group, gone in (([1], [1], 1, 2, ()), ([1, 0, 3], [70, 5, 2], 2, 3, [(0, 0)]),
                                                ([1, 1], [600, 33], 1, 4, [(0, 1), (0, 2)]), ([9, 3], [50, 0], 1, 4, ()))
              for dtype, bits8, shift in KINDS]
+    cases += [dict(c, new=[9, 2], keys=[700, 3], kv_heads=1, group=4, gone=[(0, 2)], wide=True) for c in cases[:4]]
     run(cases + [dict(c, unseen=True) for c in cases[:4]] +
         [dict(c, new=[3], keys=[60], kv_heads=2, group=4, gone=(), unseen=True) for c in cases[:4]])

@@ -205,6 +205,20 @@ def test_strides(order, shift, bits8):
 
 
 @pytest.mark.parametrize("bits8", [False, True])
+@pytest.mark.parametrize("dim,dtype", [(64, BF16), (88, F16), (128, BF16)])
+@pytest.mark.parametrize("page,shift", [(16, 0), (16, 1), (12, 0)])
+def test_many_columns_after_many_keys(page, shift, dim, dtype, bits8):
+    """More than 32 rows times heads of a key head, whose keys are read for 32 at once where the arrays allow."""
+    new, keys = [5, 1, 3], [20000, 1, 300]
+    s = model.inputs(new, keys, page, 8, dim, dtype, bits8, 8, seed=9)
+    for name in ("k", "v"):
+        old = s["cache"][name]
+        wide = torch.zeros(*old.shape[:3], dim + 16, dtype=old.dtype, device="cuda")[..., shift:shift + dim]
+        s["cache"][name] = wide.copy_(old)
+    check(s, new, keys, "columns")
+
+
+@pytest.mark.parametrize("bits8", [False, True])
 def test_a_cache_whose_offsets_pass_32_bits(bits8):
     """Pages behind 2^32 bytes and 2^31 elements of the cache."""
     page, d = 64, 64
