@@ -15,7 +15,6 @@ also where an input requires gradients.  Refused arguments raise jdob.JdobError 
 
 from __future__ import annotations
 
-import contextlib
 import ctypes as C
 from typing import Dict, Optional
 
@@ -442,7 +441,17 @@ def cache_write(k, v, cache: dict, table, row_start, key_count, stream=None) -> 
     where = "jdob_edge_cache_write"
     if k.dim() != 3:
         _refuse(where, "k and v have rows, heads and columns")
-    _rows(cache, where, k.dtype, k, v, table, row_start, key_count, stream)
+    dev = k.device
+    a = _rows(cache, where, k.dtype, dev, k, v, table, row_start, key_count)
+    handle, context = _enter(dev, stream, where)
+    lib = _lib or load()
+    if context is not None:
+        with context:
+            code = lib.jdob_edge_cache_write(C.byref(a), handle)
+    else:
+        code = lib.jdob_edge_cache_write(C.byref(a), handle)
+    if code:
+        jdob._check(code, where)
 
 
 def cache_read(cache: dict, table, row_start, key_count, rows: Optional[int] = None, dtype=None,
@@ -457,43 +466,48 @@ def cache_read(cache: dict, table, row_start, key_count, rows: Optional[int] = N
     k, v = (into.get("k"), into.get("v")) if into else (None, None)
     if dtype is None:
         dtype = k.dtype if k is not None else torch.bfloat16 if held.dtype is torch.int8 else held.dtype
+    dev = held.device
+    handle, context = _enter(dev, stream, where)
+    if context is not None:
+        with context:
+            return _cache_read(cache, where, held, dtype, dev, k, v, rows, table, row_start, key_count, handle)
+    return _cache_read(cache, where, held, dtype, dev, k, v, rows, table, row_start, key_count, handle)
+
+
+def _cache_read(cache, where, held, dtype, dev, k, v, rows, table, row_start, key_count, handle):
     if k is None or v is None:
         given = v if k is None else k
-        if len(held.shape) != 4:
+        shape = held.shape
+        if len(shape) != 4:
             _refuse(where, "the cache's k and v are [pages, heads, page size, columns]")
-        if given is None and (rows is None or rows < 0):
+        if given is not None:
+            rows = given.shape[0]
+        elif rows is None or rows < 0:
             _refuse(where, f"rows is {rows}, and no buffer is given")
         _dtype(dtype, where)
-        shape, dev = (rows if given is None else given.shape[0], held.shape[1], held.shape[3]), held.device
-        context = _enter(dev, stream, where)[1]
-        with context if context is not None else contextlib.nullcontext():
-            k = torch.empty(shape, dtype=dtype, device=dev) if k is None else k
-            v = torch.empty(shape, dtype=dtype, device=dev) if v is None else v
+        shape = (rows, shape[1], shape[3])
+        k = torch.empty(shape, dtype=dtype, device=dev) if k is None else k
+        v = torch.empty_like(k) if v is None and given is None else torch.empty(shape, dtype=dtype, device=dev) if v is None else v
     if k.dim() != 3 or (rows is not None and k.shape[0] != rows):
         _refuse(where, f"k is {tuple(k.shape)}, expected {rows} rows, heads and columns")
-    _rows(cache, where, dtype, k, v, table, row_start, key_count, stream)
+    a = _rows(cache, where, dtype, dev, k, v, table, row_start, key_count)
+    code = (_lib or load()).jdob_edge_cache_read(C.byref(a), handle)
+    if code:
+        jdob._check(code, where)
     return k, v
 
 
-def _rows(cache, where, dtype, k, v, table, row_start, key_count, stream):
-    dev = k.device
+def _rows(cache, where, dtype, dev, k, v, table, row_start, key_count):
     rows = k.shape[0]
     if rows > MAX_ROWS:
         _refuse(where, f"{rows} rows", jdob.JDOB_ERR_UNSUPPORTED)
     part = _cache(cache, where, dtype, dev, table, row_start, key_count)
-    shape = (rows, part[0].num_kv_heads, part[0].head_dim)
-    a = CacheRowsArgs(*part, rows, _array(k, where, "k", shape, dtype, dev), *k.stride()[:2],
-                      _array(v, where, "v", shape, dtype, dev), *v.stride()[:2])
-    handle, context = _enter(dev, stream, where)
-    lib = _lib or load()
-    call = lib.jdob_edge_cache_write if where == "jdob_edge_cache_write" else lib.jdob_edge_cache_read
-    if context is not None:
-        with context:
-            code = call(C.byref(a), handle)
-    else:
-        code = call(C.byref(a), handle)
-    if code:
-        jdob._check(code, where)
+    c = part[0]
+    shape = (rows, c.num_kv_heads, c.head_dim)
+    k_row, k_head, _ = k.stride()
+    v_at = _array(v, where, "v", shape, dtype, dev)
+    v_row, v_head, _ = v.stride()
+    return CacheRowsArgs(*part, rows, _array(k, where, "k", shape, dtype, dev), k_row, k_head, v_at, v_row, v_head)
 
 
 def attend_paged(q, cache: dict, table, query_start, key_count, scale: Optional[float] = None,

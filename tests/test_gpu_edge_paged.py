@@ -69,6 +69,17 @@ def test_many_sequences(seed):
 
 
 @pytest.mark.parametrize("bits8", [False, True])
+@pytest.mark.parametrize("n,page", [(70, 16), (150, 12), (200, 64)])
+def test_shares_of_many_sequences(n, page, bits8):
+    """More sequences than lanes whose keys are dealt over workgroups: none, few and many keys, with and without rows."""
+    r = random.Random(n)
+    new = [r.choice([0, 1, 1, 2]) for _ in range(n)]
+    keys = [r.choice([0, 3, 100, 700, 2000]) for _ in range(n)]
+    new[n // 2], keys[n // 2], keys[n - 1] = 1, 7000, 4000
+    check(model.inputs(new, keys, page, 2, 64, BF16, bits8, 3, seed=n), new, keys, (n, page))
+
+
+@pytest.mark.parametrize("bits8", [False, True])
 @pytest.mark.parametrize("page", [16, 48, 10])
 def test_pages_that_have_been_given_back(page, bits8):
     """Keys on pages that are not there are not seen: at the beginning, in the middle, all of them."""
@@ -202,6 +213,17 @@ def test_strides(order, shift, bits8):
     got = call({**s, "q": q, "cache": cache, "table": table[:, :-5]}, new, keys, out=wide[:, :, shift:shift + d])
     assert torch.equal(got, want)
     assert (wide[:, :, :shift] == 3).all() and (wide[:, :, shift + d:] == 3).all()
+
+
+def test_scales_with_gaps():
+    """Scales whose heads and pages start at any element, side by side within a page."""
+    new, keys = [1, 2, 1], [90, 300, 17]
+    s = model.inputs(new, keys, 16, 2, 64, BF16, True, 2, seed=7)
+    want = check(s, new, keys, "dense")
+    for name in ("k_scale", "v_scale"):
+        old = s["cache"][name]
+        s["cache"][name] = torch.full((old.shape[0], 2, 19), float("nan"), device="cuda")[:, :, 1:17].copy_(old)
+    assert torch.equal(call(s, new, keys), want)
 
 
 @pytest.mark.parametrize("bits8", [False, True])
