@@ -38,7 +38,8 @@
  * need the alignment of their element type only; rows whose starts are
  * multiples of 16 bytes are read faster.  Index arrays on the device are not
  * checked by the host: entries out of range never lead to an access out of
- * bounds (they are clamped, or the row counts as one without an adapter).
+ * bounds (they are clamped, the row counts as one without an adapter, or the
+ * key as absent).
  * Outputs must not overlap inputs unless an argument says that they may.
  * The operators are forward passes.
  */
