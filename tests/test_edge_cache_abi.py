@@ -31,6 +31,18 @@ def test_header_and_binding_agree():
     assert re.search(rf"#define JDOB_EDGE_MAX_PAGE_SIZE {edge.MAX_PAGE_SIZE}\b", src)
 
 
+@pytest.mark.parametrize("cls,packed", [(edge.CacheRowsArgs, edge._ROWS), (edge.AttendPagedArgs, edge._PAGED)])
+def test_what_is_packed_is_the_structure(cls, packed):
+    def flat(x):
+        for name, kind in x._fields_:
+            value = getattr(x, name)
+            yield from flat(value) if kind is edge.Cache else (value,)
+
+    numbers = list(range(1, 1 + len(list(flat(cls())))))
+    assert packed.size == C.sizeof(cls)
+    assert list(flat(cls.from_buffer_copy(packed.pack(*numbers)))) == numbers
+
+
 def cache(**kw):
     # [40 pages][2 heads][16 slots][64]
     c = edge.Cache(40, 16, 2, 64, edge.EDGE_BF16, 1, FAKE, 2048, 1024, 64, FAKE, 2048, 1024, 64, FAKE, 32, 16, 1, FAKE, 32, 16, 1)
@@ -157,6 +169,9 @@ def test_the_binding_refuses(bits8):
             edge.cache_read({**c, **bad}, rows=3, **where)
         with pytest.raises(jdob.JdobError):
             edge.attend_paged(k, {**c, **bad}, where["table"], where["row_start"], where["key_count"])
+    for kw in ({"scale": 0.0}, {"scale": float("nan")}, {"scale": 1e39}, {"max_queries": -1}, {"max_keys": -2}):
+        with pytest.raises(jdob.JdobError):
+            edge.attend_paged(k, c, where["table"], where["row_start"], where["key_count"], **kw)
     for kw in ({"pages": -1}, {"page_size": 0}, {"page_size": 65537}, {"kv_heads": 0}, {"dim": 12}, {"dim": 136}, {"dtype": torch.float32}):
         with pytest.raises(jdob.JdobError):
             edge.make_cache(**{"pages": 4, "page_size": 16, "kv_heads": 2, "dim": 64, "device": "cpu", **kw})
