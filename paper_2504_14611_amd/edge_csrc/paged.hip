@@ -143,14 +143,40 @@ struct Tile {
   f32x4 k_scale[2], v_scale[2];
 };
 
+// A stretch of memory from `at` on: what is read from behind its end is zero and does not touch memory.  Both are the
+// same for all lanes of the wave.
+__device__ inline __amdgpu_buffer_rsrc_t window(const void *at, int bytes) {
+  const uint64_t a = (uint64_t)at;
+  const uint64_t same = (uint64_t)__builtin_amdgcn_readfirstlane((unsigned)(a >> 32)) << 32 |
+                        (unsigned)__builtin_amdgcn_readfirstlane((unsigned)a);
+  return __builtin_amdgcn_make_buffer_rsrc((void *)same, 0, __builtin_amdgcn_readfirstlane(bytes), 0x00020000);
+}
+template <int BYTES>
+__device__ inline void window_load(unsigned *to, __amdgpu_buffer_rsrc_t w, unsigned offset) {
+  if constexpr (BYTES == 16) {
+    const u32x4 x = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(w, offset, 0, 0));
+    to[0] = x[0], to[1] = x[1], to[2] = x[2], to[3] = x[3];
+  } else if constexpr (BYTES == 8) {
+    const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(w, offset, 0, 0));
+    to[0] = x[0], to[1] = x[1];
+  } else if constexpr (BYTES == 4) {
+    *to = __builtin_amdgcn_raw_buffer_load_b32(w, offset, 0, 0);
+  } else {
+    *to = (unsigned short)__builtin_amdgcn_raw_buffer_load_b16(w, offset, 0, 0);
+  }
+}
+
 constexpr int TILE_KEYS = 32;
 constexpr int64_t NO_TILE = INT64_MAX / 2;  // behind any key
+constexpr unsigned FLAT = 0x70000000u;      // bytes from a head's first row or scale on that Anywhere's windows cover
 
 __device__ const u32x4 paged_zeros = {0, 0, 0, 0};
 
 // A wave's keys of one head whatever the page's size and the arrays' alignment: every lane looks up its own keys' pages,
-// RUN keys from a multiple of RUN on at once (pages of a multiple of RUN keys).
-template <typename T, int DP, bool BITS8, int RUN>
+// RUN keys from a multiple of RUN on at once (pages of a multiple of RUN keys).  WINDOW: through one window over each of
+// the arrays (FLAT: they are small enough), with offsets of 32 bits for addresses of 64 (32 users' tokens after up to 8191
+// 8-bit keys on pages of 20: 89 us and 106; three after 91,511 on pages of 7, a key at once: 118 and 342).
+template <typename T, int DP, bool BITS8, int RUN, bool WINDOW>
 struct Anywhere {
   typedef typename std::conditional<BITS8, int8_t, unsigned short>::type E;
   const PagedParams &p;
@@ -202,95 +228,95 @@ struct Anywhere {
     return bits;
   }
 
-  template <int N>
-  __device__ static void piece(unsigned *to, const E *row, int e, bool have) {
-    typedef typename Raw<E, N>::type V;
-    const V x = *(const V *)(have ? (const void *)(row + e) : (const void *)&paged_zeros);
-    if constexpr (sizeof x < sizeof(unsigned)) {
-      *to = __builtin_bit_cast(unsigned short, x);
+  static constexpr int N = BITS8 ? 4 : 2, SZ = sizeof(E);  // elements a word
+  // Offsets that lie behind an array's end, also when a row's and an element's are added.
+  static constexpr unsigned NO_ROW = 0x80000000u, NO_ELEMENT = FLAT;
+
+  __device__ static __amdgpu_buffer_rsrc_t all(const Pool &x, int head) {
+    return window(x.at + head * x.head * SZ, FLAT);
+  }
+
+  // A lane's row of keys or values: an address, or a distance from the head's first row.
+  struct Row {
+    const E *at;
+    unsigned offset;
+    bool have;
+  };
+  __device__ Row row(const Pool &x, Spot at, int more) const {
+    if constexpr (WINDOW)
+      return {nullptr, at.page < 0 ? NO_ROW : (unsigned)at.page * (unsigned)(x.page * SZ) + (unsigned)(at.slot + more) * (unsigned)(x.slot * SZ), true};
+    return {(const E *)x.at + at.page * x.page + head * x.head + (at.slot + more) * x.slot, 0, at.page >= 0};
+  }
+
+  template <int M>
+  __device__ void piece(unsigned *to, const Pool &x, const Row &row, int e) const {
+    if constexpr (WINDOW) {
+      window_load<M * SZ>(to, all(x, head), row.offset + (e < p.c.dim ? (unsigned)e * SZ : NO_ELEMENT));
     } else {
-      __builtin_memcpy(to, &x, sizeof x);
+      typedef typename Raw<E, M>::type V;
+      const V v = *(const V *)(row.have && e < p.c.dim ? (const void *)(row.at + e) : (const void *)&paged_zeros);
+      if constexpr (sizeof v < sizeof(unsigned)) {
+        *to = __builtin_bit_cast(unsigned short, v);
+      } else {
+        __builtin_memcpy(to, &v, sizeof v);
+      }
     }
   }
-  static constexpr int N = BITS8 ? 4 : 2;  // elements a word
 
-  __device__ void scales(f32x4 (&to)[2], const Pool &from, int64_t first) const {
+  __device__ void scales(f32x4 (&to)[2], const Pool &x) const {
+    const auto w = window(x.scale + head * x.scale_head, FLAT);
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const Spot at = next.run[h][r / RUN];
-        const float *const x =
-            from.scale + at.page * from.scale_page + head * from.scale_head + (at.slot + r % RUN) * from.scale_slot;
-        to[h][r] = *(there(first, h, r) ? x : (const float *)&paged_zeros);
+        const int slot = at.slot + r % RUN;
+        if constexpr (WINDOW) {
+          unsigned v;
+          window_load<4>(&v, w, at.page < 0 ? NO_ROW : (unsigned)at.page * (unsigned)(x.scale_page * 4) + (unsigned)slot * (unsigned)(x.scale_slot * 4));
+          to[h][r] = __uint_as_float(v);
+        } else {
+          const float *const v = x.scale + at.page * x.scale_page + head * x.scale_head + slot * x.scale_slot;
+          to[h][r] = *(at.page >= 0 ? v : (const float *)&paged_zeros);
+        }
       }
   }
 
+  // (The last keys of a run that the last key is part of are on its page: read, and seen by nobody.)
   __device__ void load_keys(Tile<DP, BITS8> &t, int64_t first) const {
     if (first >= until) return;  // (it will not be taken)
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const Spot at = next.key[h];
-      const E *const row = (const E *)p.c.k.at + at.page * p.c.k.page + head * p.c.k.head + at.slot * p.c.k.slot;
+      const Row k = row(p.c.k, next.key[h], 0);
 #pragma unroll
-      for (int j = 0; j < DP / 32; ++j) {
-        const int e = key_element<DP, BITS8>(j, g);
-        piece<8>(t.k[h] + j * 8 / N, row, e, at.page >= 0 && e < p.c.dim);
-      }
-      __builtin_amdgcn_sched_barrier(0);  // (all addresses at once would take more registers than there are)
+      for (int j = 0; j < DP / 32; ++j) piece<8>(t.k[h] + j * 8 / N, p.c.k, k, key_element<DP, BITS8>(j, g));
+      if constexpr (!WINDOW) __builtin_amdgcn_sched_barrier(0);  // (all addresses at once would take more registers than there are)
     }
-    if constexpr (BITS8) scales(t.k_scale, p.c.k, first);
+    if constexpr (BITS8) scales(t.k_scale, p.c.k);
   }
 
   __device__ void load_values(Tile<DP, BITS8> &t, int64_t first) const {
     if (first >= until) return;
-    const int dim = p.c.dim;
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const Spot at = next.run[h][r / RUN];
-        const bool have = there(first, h, r);
-        const E *const row =
-            (const E *)p.c.v.at + at.page * p.c.v.page + head * p.c.v.head + (at.slot + r % RUN) * p.c.v.slot;
+        const Row v = row(p.c.v, next.run[h][r / RUN], r % RUN);
         unsigned *const to = t.v[h * 4 + r];
         if constexpr (DP == 96) {
-          piece<4>(to, row, l16 * 4, have && l16 * 4 < dim);
-          piece<2>(to + 4 / N, row, 64 + l16 * 2, have && 64 + l16 * 2 < dim);
+          piece<4>(to, p.c.v, v, l16 * 4);
+          piece<2>(to + 4 / N, p.c.v, v, 64 + l16 * 2);
         } else {
-          piece<DP / 16>(to, row, l16 * (DP / 16), have && l16 * (DP / 16) < dim);
+          piece<DP / 16>(to, p.c.v, v, l16 * (DP / 16));
         }
-        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (!WINDOW) __builtin_amdgcn_sched_barrier(0);
       }
-    if constexpr (BITS8) scales(t.v_scale, p.c.v, first);
+    if constexpr (BITS8) scales(t.v_scale, p.c.v);
   }
 };
 
 __device__ inline int64_t of_lane(int64_t x, int lane) {
   return (int64_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32 | (unsigned)__builtin_amdgcn_readlane((int)x, lane);
-}
-
-// A stretch of memory from `at` on: what is read from behind its end is zero and does not touch memory.  Both are the
-// same for all lanes of the wave.
-__device__ inline __amdgpu_buffer_rsrc_t window(const void *at, int bytes) {
-  const uint64_t a = (uint64_t)at;
-  const uint64_t same = (uint64_t)__builtin_amdgcn_readfirstlane((unsigned)(a >> 32)) << 32 |
-                        (unsigned)__builtin_amdgcn_readfirstlane((unsigned)a);
-  return __builtin_amdgcn_make_buffer_rsrc((void *)same, 0, __builtin_amdgcn_readfirstlane(bytes), 0x00020000);
-}
-template <int BYTES>
-__device__ inline void window_load(unsigned *to, __amdgpu_buffer_rsrc_t w, unsigned offset) {
-  if constexpr (BYTES == 16) {
-    const u32x4 x = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(w, offset, 0, 0));
-    to[0] = x[0], to[1] = x[1], to[2] = x[2], to[3] = x[3];
-  } else if constexpr (BYTES == 8) {
-    const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(w, offset, 0, 0));
-    to[0] = x[0], to[1] = x[1];
-  } else if constexpr (BYTES == 4) {
-    *to = __builtin_amdgcn_raw_buffer_load_b32(w, offset, 0, 0);
-  } else {
-    *to = (unsigned short)__builtin_amdgcn_raw_buffer_load_b16(w, offset, 0, 0);
-  }
 }
 
 // The same where 16 keys that start at a multiple of 16 stand side by side on one page, and their rows at multiples of
@@ -631,12 +657,12 @@ __device__ inline void take_non_finite(State16<DP> (&s)[CT], Tile<DP, false> &t,
 
 // Waves that a SIMD is to have room for: as many as leave them registers for all that a tile takes.
 constexpr int waves_a_simd(int dp, bool bits8, int ct, int aligned) {
-  if (aligned != 16) return aligned == 1 && bits8 && dp == 128 ? 1 : 2;
+  if (aligned != 16) return aligned > 0 && bits8 && dp == 128 ? 1 : 2;
   if (ct == 2) return dp == 64 ? 3 : 2;
   return dp == 64 ? 4 : bits8 || dp == 96 ? 3 : 2;
 }
 
-// ALIGNED: 16 (InPages), 4 or 1 (Anywhere).
+// ALIGNED: 16 (InPages), 4 or 1 (Anywhere; negative: through windows).
 template <typename T, int DP, bool BITS8, int CT, int ALIGNED, int WAVES>
 __global__ __launch_bounds__(WAVES *WAVE, waves_a_simd(DP, BITS8, CT, ALIGNED)) void paged_kernel(PagedParams p) {
   typedef typename Mma16<T>::frag frag;
@@ -683,7 +709,7 @@ __global__ __launch_bounds__(WAVES *WAVE, waves_a_simd(DP, BITS8, CT, ALIGNED)) 
     for (int i = 0; i < DP / 16; ++i) s[c].out[i] = (f32x4){};
   }
   const int first_limit = shift + first_row;
-  typedef typename std::conditional<ALIGNED == 16, InPages<T, DP, BITS8>, Anywhere<T, DP, BITS8, ALIGNED % 16>>::type Cache;
+  typedef typename std::conditional<ALIGNED == 16, InPages<T, DP, BITS8>, Anywhere<T, DP, BITS8, ALIGNED % 4 ? 1 : 4, (ALIGNED < 0)>>::type Cache;
   // A share's waves take every so many tiles, so that pages that are not there are missing from all shares alike.
   Cache cache(p, u, kv, until, share.index * WAVES + wave, share.count * WAVES);
   Tile<DP, BITS8> t;
@@ -914,6 +940,8 @@ int paged(const PagedParams &p, int aligned, int64_t blocks, hipStream_t stream)
   constexpr int WAVES = 4;
   return launch(p.tile_columns == 32 ? paged_kernel<T, DP, BITS8, 2, 16, WAVES>
                 : aligned == 16      ? paged_kernel<T, DP, BITS8, 1, 16, WAVES>
+                : aligned == -4      ? paged_kernel<T, DP, BITS8, 1, -4, WAVES>
+                : aligned == -1      ? paged_kernel<T, DP, BITS8, 1, -1, WAVES>
                 : aligned == 4       ? paged_kernel<T, DP, BITS8, 1, 4, WAVES>
                                      : paged_kernel<T, DP, BITS8, 1, 1, WAVES>,
                 blocks, WAVES * WAVE, stream, p);
@@ -930,6 +958,21 @@ bool in_pages(const jdob_edge_cache &c) {
   return c.page_size % 16 == 0 && pool(c.k, c.k_page_stride, c.k_head_stride, c.k_slot_stride, c.k_scale_slot_stride) &&
          pool(c.v, c.v_page_stride, c.v_head_stride, c.v_slot_stride, c.v_scale_slot_stride) &&
          (!c.bits8 || c.head_dim % 16 == 0 || (c.head_dim > 64 && c.head_dim <= 96));
+}
+
+// Whether windows cover the cache's arrays, and rows start at multiples of four bytes: elements from a head's first row to
+// the last of its rows' ends, with strides as checked.
+bool flat(const jdob_edge_cache &c) {
+  const int64_t pages = c.num_pages > 0 ? c.num_pages - 1 : 0, slots = c.page_size - 1, unit = c.bits8 ? 4 : 2;
+  auto spans = [&](int64_t page, int64_t slot, int64_t size) {
+    return page < FLAT && slot < FLAT && pages * page + slots * slot + JDOB_EDGE_MAX_HEAD_DIM < FLAT / size;
+  };
+  auto rows = [&](const void *at, int64_t page, int64_t head, int64_t slot) {
+    return (uintptr_t)at % 4 == 0 && (page | head | slot) % unit == 0 && spans(page, slot, c.bits8 ? 1 : 2);
+  };
+  return rows(c.k, c.k_page_stride, c.k_head_stride, c.k_slot_stride) &&
+         rows(c.v, c.v_page_stride, c.v_head_stride, c.v_slot_stride) &&
+         (!c.bits8 || (spans(c.k_scale_page_stride, c.k_scale_slot_stride, 4) && spans(c.v_scale_page_stride, c.v_scale_slot_stride, 4)));
 }
 
 template <typename T, bool BITS8>
@@ -980,7 +1023,7 @@ extern "C" int jdob_edge_attend_paged(const jdob_edge_attend_paged_args *a, void
   const int64_t need = jdob_edge_attend_paged_workspace(a);
   if (need > 0 && (!a->workspace || (uintptr_t)a->workspace % 16 || a->workspace_bytes < need)) return JDOB_ERR_INVALID_ARG;
   const bool in = in_pages(a->cache);
-  const int aligned = in ? 16 : a->cache.page_size % 4 == 0 ? 4 : 1;
+  const int run = a->cache.page_size % 4 == 0 ? 4 : 1, aligned = in ? 16 : flat(a->cache) ? -run : run;
   const PagedPlan f = paged_plan(a, in);
   const PagedParams p = {pages_of(a->cache, a->num_sequences, a->table_width, a->table, a->table_stride, a->query_start,
                                   a->key_count),

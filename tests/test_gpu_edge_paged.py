@@ -241,9 +241,10 @@ def test_many_columns_after_many_keys(page, shift, dim, dtype, bits8):
 
 
 @pytest.mark.parametrize("bits8", [False, True])
-def test_a_cache_whose_offsets_pass_32_bits(bits8):
+@pytest.mark.parametrize("page", [64, 20, 9])
+def test_a_cache_whose_offsets_pass_32_bits(page, bits8):
     """Pages behind 2^32 bytes and 2^31 elements of the cache."""
-    page, d = 64, 64
+    d = 64
     pages = (1 << 33) // (page * d) // (1 if bits8 else 2) + 40
     s = model.inputs([1, 3], [300, 200], page, 1, d, BF16, bits8, 2)
     want = check(s, [1, 3], [300, 200], "near")
