@@ -31,7 +31,7 @@ namespace {
 
 struct PagedParams {
   Pages c;
-  int heads, group, max_queries, tile_columns;
+  int group, max_queries, tile_columns;  // group: heads of a key head
   float scale;  // times log2(e)
   int64_t query_rows;
   const char *q;
@@ -39,11 +39,10 @@ struct PagedParams {
   int64_t q_stride, q_head, out_stride, out_head;  // elements
   int tiles;          // tiles of columns of a sequence
   int shares;         // of the keys, besides one for each sequence (0: keys are not split)
-  Divide by_heads, by_tiles, by_group;  // of key heads, tiles and the heads of a key head
+  Divide by_heads, by_tiles, by_group;  // of key heads, tiles and heads of a key head
   float *part;        // [share][tile][key head][columns of a tile][dim + 4]
 };
 
-typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 
 template <typename T>
@@ -214,8 +213,7 @@ struct Anywhere {
     return first;
   }
 
-  // Whether the lane's value h, r of the next tile is there.  (The last keys of a run that the last key is part of are
-  // on its page, but not to be read.)
+  // Whether the lane's value h, r of the next tile is there.  (A run that the last key is part of may end behind it.)
   __device__ bool there(int64_t first, int h, int r) const {
     return next.run[h][r / RUN].page >= 0 && (RUN == 1 || first + h * 16 + g * 4 + r < until);
   }
@@ -282,7 +280,7 @@ struct Anywhere {
       }
   }
 
-  // (The last keys of a run that the last key is part of are on its page: read, and seen by nobody.)
+  // (What stands behind the last key in its run is on its page: read, and seen by nobody.)
   __device__ void load_keys(Tile<DP, BITS8> &t, int64_t first) const {
     if (first >= until) return;  // (it will not be taken)
 #pragma unroll
@@ -1027,7 +1025,7 @@ extern "C" int jdob_edge_attend_paged(const jdob_edge_attend_paged_args *a, void
   const PagedPlan f = paged_plan(a, in);
   const PagedParams p = {pages_of(a->cache, a->num_sequences, a->table_width, a->table, a->table_stride, a->query_start,
                                   a->key_count),
-                         a->num_heads, a->num_heads / a->cache.num_kv_heads, f.queries, f.columns,
+                         a->num_heads / a->cache.num_kv_heads, f.queries, f.columns,
                          a->scale * 1.44269504088896f, a->query_rows, (const char *)a->q, (char *)a->out, a->q_stride,
                          a->q_head_stride, a->out_stride, a->out_head_stride, (int)f.tiles, f.shares, {}, {}, {},
                          (float *)a->workspace};

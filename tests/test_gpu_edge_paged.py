@@ -350,6 +350,24 @@ def test_streams_graphs_and_workspaces(bits8):
             assert torch.equal(call(t, new, keys), want[1])
 
 
+@pytest.mark.parametrize("bits8", [False, True])
+def test_two_calls_at_once(bits8):
+    """Two batches over one cache on two streams, neither waiting for the other."""
+    new, keys = [1, 2], [6000, 300]
+    s = model.inputs(new, keys, 16, 4, 128, BF16, bits8, 4, seed=1)
+    t = {**s, "q": torch.randn_like(s["q"].float()).to(BF16)}
+    want = [call(x, new, keys) for x in (s, t)]
+    sides = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(5):
+        for x, side in zip((s, t), sides):
+            with torch.cuda.stream(side):
+                got.append(call(x, new, keys))
+    torch.cuda.synchronize()
+    assert all(torch.equal(g, want[i % 2]) for i, g in enumerate(got))
+
+
 def test_refusals():
     s = model.inputs([1], [90], 16, 2, 64, BF16, True, 2)
     none = {"k": s["cache"]["k"], "v": s["cache"]["v"]}
