@@ -481,9 +481,6 @@ __device__ inline float column_sum(float x) {
 }
 
 constexpr float GROWTH = 8.0f;  // the maximum may lag behind by this much (p up to 2^8) before out is rescaled
-// Up to here (log2 units) sc * scale - top * scale may be formed with one rounding of top * scale: it puts p
-// off by at most a factor of two, the same for all of a column, which its sum takes back.
-constexpr float NEAR = 0x1p24f;
 
 // Eight codes as elements of T, exactly.
 template <typename T>
@@ -550,25 +547,14 @@ __device__ inline void softmax(State16<DP> &s, f32x4 (&sc)[2], float scale) {
 #pragma unroll
     for (int i = 0; i < DP / 16; ++i) s.out[i] *= f;
   }
-  const float base = base_of(s.top) * scale;
-  const bool far = !(fabsf(base) < NEAR);
-  if (__any(far)) {
-    // the difference first, again column by column
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) sc[h][r] = far ? (sc[h][r] - s.top) * scale : sc[h][r] * scale - base;
-  } else {
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) sc[h][r] = sc[h][r] * scale - base;
-  }
+  // The difference first: sc * scale - top * scale with the product rounded puts all p of a wave off by the same factor, but
+  // another one in another wave, whose keys are weighed against these by exp(scale (top - top')).
+  const float base = base_of(s.top);
 #pragma unroll
   for (int h = 0; h < 2; ++h)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      sc[h][r] = __builtin_amdgcn_exp2f(sc[h][r]);
+      sc[h][r] = __builtin_amdgcn_exp2f((sc[h][r] - base) * scale);
       s.sum += sc[h][r];
     }
 }

@@ -1,0 +1,35 @@
+"""What the attentions' softmax and weighted sums lose, on inputs that show it (edge_precision_model)."""
+
+import pytest
+import torch
+
+from paper_2504_14611_amd import edge
+from tests import edge_precision_model as model
+
+pytestmark = pytest.mark.gpu
+BF16, F16 = torch.bfloat16, torch.float16
+
+
+def paged(scores, v, base, new, page, dtype, bits8, part, v_scale=None, kv_heads=2, group=2, label=None):
+    s = model.paged(scores, v, base, new, page, kv_heads, group, dtype, bits8, v_scale)
+    got = edge.attend_paged(s["q"], s["cache"], s["table"], s["row_start"], s["key_count"], scale=1.0, max_queries=new,
+                            max_keys=len(scores))
+    values = v if v_scale is None else v.double() * v_scale.double()[:, None]
+    over = model.over(got, scores, values, new, dtype, part)
+    assert over <= 0, (label, over)
+
+
+BASES = [0, 1 << 12, 1 << 20, 1 << 23, -(1 << 23)]
+
+
+@pytest.mark.parametrize("bits8", [False, True])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("page", [16, 20, 7])
+@pytest.mark.parametrize("dim", [64, 96, 128])
+def test_scores_far_from_zero_over_pages(dim, page, dtype, bits8):
+    """Waves and workgroups whose maxima differ, scores far from zero: weights are those of the differences."""
+    for base in BASES:
+        for keys, new, group in ((64, 1, 2), (600, 3, 2), (5000, 1, 4), (3000, 5, 8)):
+            for seed in (0, 1):
+                scores, v = model.far_scores(keys, seed, "cuda", dim)
+                paged(scores, v, base, new, page, dtype, bits8, 2.0 ** -16, group=group, label=(base, keys, new, seed))
