@@ -175,9 +175,11 @@ __device__ void State<DP>::clear() {
 }
 
 constexpr float GROWTH = 8.0f;  // the maximum may lag behind by this much (p up to 2^8) before out is rescaled
-// Up to here (log2 units) sc * scale - top * scale may be formed with one rounding of top * scale: it puts p
-// off by at most a factor of two, the same for all of a row, which its sum takes back.
-constexpr float NEAR = 0x1p24f;
+// Up to here (log2 units) sc * scale - top * scale may be formed with one rounding of top * scale: it puts all p of a
+// wave off by one factor, but another one for another maximum and in another wave, whose keys are weighed against these
+// by exp(scale (top - top')).  At 2^8 that is within 2^-17 log2 units, small beside p's rounding to 16 bits (2^-11 of
+// itself or more); at 2^24 it would be half of one.
+constexpr float NEAR = 0x1p8f;
 
 // Scores of 32 rows with KT * 32 staged keys, softmax, and the values' sums.  The lane's row sees the
 // tile's keys 0 .. sees; MASKED: some key of the tile lies behind that for some row.

@@ -91,3 +91,10 @@ def far_scores(keys, seed, device, dim=16):
     v = torch.randint(0, 3, (keys, dim), generator=gen).float()
     v[:, 0] = torch.arange(keys) >= keys // 2
     return r.to(device), v.to(device)
+
+
+def rising_scores(keys, seed, device, dim=16):
+    """Tiles of 64 keys each 7 above the one before, so that the maximum has to follow; values that show each tile's weight."""
+    tile = torch.arange(keys) // 64
+    v = (tile[:, None] % dim == torch.arange(dim)).float()
+    return (tile * 7).to(device), v.to(device)

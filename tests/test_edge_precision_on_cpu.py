@@ -65,6 +65,10 @@ def far(c):
     scores, v = model.far_scores(c["keys"], c["seed"], "cpu")
     return scores, v, None
 
+def rising(c):
+    scores, v = model.rising_scores(c["keys"], c["seed"], "cpu")
+    return scores, v, None
+
 for c in json.loads(sys.stdin.read()):
     print(c, flush=True)
     dt = TYPES[c["dtype"]]
@@ -113,3 +117,13 @@ def test_scores_far_from_zero_over_pages(run, base, bits8):
     run([dict(op="paged", what="far", keys=keys, seed=seed, new=new, page=page, kv_heads=1, group=2, dtype=dtype, bits8=bits8,
               base=base, part=2.0 ** -16)
          for keys, new, page in ((64, 1, 16), (64, 3, 20), (700, 1, 16)) for seed in (0, 1) for dtype in ("bf16", "f16")])
+
+
+@pytest.mark.parametrize("base", BASES)
+def test_scores_far_from_zero(run, base):
+    """Packed keys: few rows by two waves that take other keys, many rows whose maximum rises from tile to tile."""
+    run([dict(op="attend", what=what, keys=keys, seed=seed, new=new, kv_heads=1, group=2, dtype=dtype, base=base,
+              part=2.0 ** -8 if dtype == "bf16" else 2.0 ** -11)
+         for what, keys, new, seed in (("far", 64, 1, 0), ("far", 300, 3, 1), ("rising", 200, 2, 0), ("rising", 200, 70, 0),
+                                       ("far", 150, 70, 1))
+         for dtype in ("bf16", "f16")])

@@ -33,3 +33,18 @@ def test_scores_far_from_zero_over_pages(dim, page, dtype, bits8):
             for seed in (0, 1):
                 scores, v = model.far_scores(keys, seed, "cuda", dim)
                 paged(scores, v, base, new, page, dtype, bits8, 2.0 ** -16, group=group, label=(base, keys, new, seed))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("dim", [64, 96, 128])
+def test_scores_far_from_zero(dim, dtype):
+    """Packed keys: few rows, whose keys are split over waves and workgroups, and many."""
+    for base in BASES:
+        for what, keys, new in ((model.far_scores, 64, 1), (model.far_scores, 3000, 3), (model.rising_scores, 600, 2),
+                                (model.rising_scores, 600, 200), (model.far_scores, 700, 200)):
+            for seed in (0, 1):
+                scores, v = what(keys, seed, "cuda", dim)
+                q, k, v16, *where = model.packed(scores, v, base, new, 2, 2, dtype)
+                got = edge.attend(q, k, v16, *where, scale=1.0, max_queries=new, max_keys=keys)
+                over = model.over(got, scores, v, new, dtype, model.HALF[dtype])
+                assert over <= 0, (base, what, keys, new, seed, over)
