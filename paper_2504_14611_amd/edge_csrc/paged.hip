@@ -496,10 +496,20 @@ __device__ inline typename Mma16<T>::frag of_codes(unsigned lo, unsigned hi) {
 
 // p goes into its product as two parts of 16 bits, the rounded one and what it left: bounded by memory, the second
 // product costs nothing (32 users' tokens 95 us with one part or two), and the output's error against 64 bits is that
-// of its own rounding (1.6e-3 in bfloat16; 2.3e-3 with one part).  With 8 bits the parts are bfloat16, whose range holds
-// p times any scale.
+// of its own rounding (1.6e-3 in bfloat16; 2.3e-3 with one part).  With 8 bits the parts are bfloat16 ones of p times the
+// value's scale.
 template <typename T, bool BITS8>
 using Weight = typename std::conditional<BITS8, __bf16, T>::type;
+
+// Parts of binary16 end at 2^-25.  There p is made 2^LIFT times as large, below 2^16 still, and where some p of a tile is
+// below SMALL, so that its parts hold fewer than 16 bits, what they leave of p goes through the products again, 2^AGAIN
+// times as large, until they are 1 / END times as large: what is lost of a weight is then below 2^-25 2^-60 2^-7 of the largest, times values below
+// 2^16 and 2^31 keys far below what a binary16 output can show.  (Nothing at all would be left of p below 2^-25 otherwise,
+// while the sum has it.)  32 users' tokens take 96 us for 95 without, 104 where all tiles go through again; binary32
+// products, an eighth of the rate, took 100 for all (four rows of 64 heads of 16 users 135 for 130, one tile 6.8 for 5.7).
+template <typename T, bool BITS8>
+constexpr bool LIFTED = !BITS8 && __is_same(T, _Float16);
+constexpr float LIFT = 7.0f, SMALL = 0x1p-9f, AGAIN = 0x1p20f, END = 0x1p-60f;
 
 // Scores of the columns with 32 keys: column c's with key 16 h + 4 g + r in sc[c][h][r].
 template <typename T, int DP, bool BITS8, int CT>
@@ -527,9 +537,9 @@ __device__ inline void scores(f32x4 (&sc)[CT][2], const typename Mma16<T>::frag 
   }
 }
 
-// p of a column's scores relative to its maximum, which is raised first where it lags; the sum goes on.
+// p times 2^lift of a column's scores relative to its maximum, which is raised first where it lags; the sum goes on.
 template <int DP>
-__device__ inline void softmax(State16<DP> &s, f32x4 (&sc)[2], float scale) {
+__device__ inline void softmax(State16<DP> &s, f32x4 (&sc)[2], float scale, float lift) {
   float top = -INFINITY;
 #pragma unroll
   for (int h = 0; h < 2; ++h)
@@ -554,7 +564,7 @@ __device__ inline void softmax(State16<DP> &s, f32x4 (&sc)[2], float scale) {
   for (int h = 0; h < 2; ++h)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      sc[h][r] = __builtin_amdgcn_exp2f((sc[h][r] - base) * scale);
+      sc[h][r] = __builtin_amdgcn_exp2f((sc[h][r] - base) * scale + lift);
       s.sum += sc[h][r];
     }
 }
@@ -571,37 +581,69 @@ __device__ inline u32x4 value_words(const Tile<DP, false> &t, int i) {
   return x;
 }
 
-// The values' sums with weights p.
+// The values' sums with weights p, which are used up.
 template <typename T, int DP, bool BITS8, int CT>
-__device__ inline void weighted(State16<DP> (&s)[CT], const f32x4 (&p)[CT][2], const Tile<DP, BITS8> &t) {
+__device__ inline void weighted(State16<DP> (&s)[CT], f32x4 (&p)[CT][2], const Tile<DP, BITS8> &t) {
   typedef Weight<T, BITS8> P;
   typedef typename Mma16<P>::frag frag;
-  frag w[CT], rest[CT];
+  float least = 0.0f;  // of the lane's p that are not zero
+  if constexpr (LIFTED<T, BITS8>) {
+    unsigned x = ~0u;  // (the bits of 0 become the largest of all, those of a NaN)
 #pragma unroll
-  for (int c = 0; c < CT; ++c)
+    for (int c = 0; c < CT; ++c)
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const float x = BITS8 ? p[c][h][r] * t.v_scale[h][r] : p[c][h][r];
-        w[c][h * 4 + r] = (P)x;
-        rest[c][h * 4 + r] = (P)(x - (float)w[c][h * 4 + r]);
+        for (int r = 0; r < 4; ++r) {
+          const unsigned y = __float_as_uint(p[c][h][r]) - 1;
+          x = y < x ? y : x;
+        }
+    least = __uint_as_float(x);
+  }
+  float back = 1.0f;
+  for (;;) {
+    frag w[CT], rest[CT];
+#pragma unroll
+    for (int c = 0; c < CT; ++c)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float x = BITS8 ? p[c][h][r] * t.v_scale[h][r] : p[c][h][r], left = x - (float)(P)x;
+          w[c][h * 4 + r] = (P)x;
+          rest[c][h * 4 + r] = (P)left;
+          if constexpr (LIFTED<T, BITS8>) p[c][h][r] = (left - (float)(P)left) * AGAIN;
+        }
+#pragma unroll
+    for (int i = 0; i < DP / 16; ++i) {
+      frag v;
+      if constexpr (BITS8) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = (P)(float)(int8_t)(t.v[e][i / 4] >> 8 * (i % 4));
+      } else {
+        v = __builtin_bit_cast(frag, value_words(t, i));
       }
 #pragma unroll
-  for (int i = 0; i < DP / 16; ++i) {
-    frag v;
-    if constexpr (BITS8) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = (P)(float)(int8_t)(t.v[e][i / 4] >> 8 * (i % 4));
-    } else {
-      v = __builtin_bit_cast(frag, value_words(t, i));
+      for (int c = 0; c < CT; ++c) {
+        s[c].out[i] = Mma16<P>::m16(v, w[c], s[c].out[i]);
+        s[c].out[i] = Mma16<P>::m16(v, rest[c], s[c].out[i]);
+      }
+      if (i % 2) __builtin_amdgcn_sched_barrier(0);  // (all operands at once would take more registers than there are)
     }
+    if (!LIFTED<T, BITS8> || back == END || !__any(least < SMALL)) break;
+    // (out, at most 2^31 2^15 2^16, is enlarged with p: in a sum of its own it would take registers that are not there)
+    least *= AGAIN;
+    back *= 1.0f / AGAIN;
 #pragma unroll
-    for (int c = 0; c < CT; ++c) {
-      s[c].out[i] = Mma16<P>::m16(v, w[c], s[c].out[i]);
-      s[c].out[i] = Mma16<P>::m16(v, rest[c], s[c].out[i]);
-    }
-    if (i % 2) __builtin_amdgcn_sched_barrier(0);  // (all operands at once would take more registers than there are)
+    for (int c = 0; c < CT; ++c)
+#pragma unroll
+      for (int i = 0; i < DP / 16; ++i) s[c].out[i] *= AGAIN;
+  }
+  if (LIFTED<T, BITS8> && back < 1.0f) {
+#pragma unroll
+    for (int c = 0; c < CT; ++c)
+#pragma unroll
+      for (int i = 0; i < DP / 16; ++i) s[c].out[i] *= back;
   }
 }
 
@@ -639,10 +681,11 @@ __device__ inline void take_non_finite(State16<DP> (&s)[CT], Tile<DP, false> &t,
     }
 }
 
-// Waves that a SIMD is to have room for: as many as leave them registers for all that a tile takes.
+// Waves that a SIMD is to have room for: as many as leave them registers for all that a tile takes.  (Heads of 96 through
+// windows by binary16: 24 users' drafts on pages of 20 keys 22.4 us with three waves, 24.8 with two.)
 constexpr int waves_a_simd(int dp, bool bits8, int ct, int aligned) {
-  if (aligned != 16) return aligned > 0 && bits8 && dp == 128 ? 1 : 2;
-  if (ct == 2) return dp == 64 ? 3 : 2;
+  if (aligned != 16) return aligned == -4 && dp == 96 ? 3 : aligned > 0 && bits8 && dp == 128 ? 1 : 2;
+  if (ct == 2) return 2;
   return dp == 64 ? 4 : bits8 || dp == 96 ? 3 : 2;
 }
 
@@ -693,6 +736,7 @@ __global__ __launch_bounds__(WAVES *WAVE, waves_a_simd(DP, BITS8, CT, ALIGNED)) 
     for (int i = 0; i < DP / 16; ++i) s[c].out[i] = (f32x4){};
   }
   const int first_limit = shift + first_row;
+  const float lift = LIFTED<T, BITS8> ? LIFT : 0.0f;
   typedef typename std::conditional<ALIGNED == 16, InPages<T, DP, BITS8>, Anywhere<T, DP, BITS8, ALIGNED % 4 ? 1 : 4, (ALIGNED < 0)>>::type Cache;
   // A share's waves take every so many tiles, so that pages that are not there are missing from all shares alike.
   Cache cache(p, u, kv, until, share.index * WAVES + wave, share.count * WAVES);
@@ -736,7 +780,7 @@ __global__ __launch_bounds__(WAVES *WAVE, waves_a_simd(DP, BITS8, CT, ALIGNED)) 
       if constexpr (!BITS8) take_non_finite<T, DP, CT>(s, t, saw);  // (likewise)
     }
 #pragma unroll
-    for (int c = 0; c < CT; ++c) softmax<DP>(s[c], sc[c], p.scale);
+    for (int c = 0; c < CT; ++c) softmax<DP>(s[c], sc[c], p.scale, lift);
     weighted<T, DP, BITS8, CT>(s, sc, t);
     cache.load_values(t, second);
     __builtin_amdgcn_sched_barrier(0);

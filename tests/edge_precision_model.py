@@ -98,3 +98,11 @@ def rising_scores(keys, seed, device, dim=16):
     tile = torch.arange(keys) // 64
     v = (tile[:, None] % dim == torch.arange(dim)).float()
     return (tile * 7).to(device), v.to(device)
+
+
+def small_weights(keys, above, device, dim=16):
+    """The first key's value is zero and its score `above` the others', whose large values show what small weights are."""
+    gen = torch.Generator().manual_seed(above)
+    r = (torch.arange(keys) == 0).int() * above
+    v = torch.randint(64, 128, (keys, dim), generator=gen).float() * (r == 0)[:, None]
+    return r.to(device), v.to(device), torch.full((keys,), 256.0, device=device)

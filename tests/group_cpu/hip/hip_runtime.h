@@ -312,6 +312,7 @@ inline V __shfl_up(V v, int d) {
 #define __builtin_amdgcn_readfirstlane(v) group_cpu_first(v)
 #define __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, x, y, z) group_cpu_mfma<16, 8, __bf16, float>(a, b, c)
 #define __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, x, y, z) group_cpu_mfma<16, 8, _Float16, float>(a, b, c)
+#define __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, x, y, z) group_cpu_mfma<16, 1, float, float>(a, b, c)
 #define __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, x, y, z) group_cpu_mfma<32, 8, __bf16, float>(a, b, c)
 #define __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, x, y, z) group_cpu_mfma<32, 8, _Float16, float>(a, b, c)
 #define __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, x, y, z) group_cpu_mfma<16, 16, signed char, unsigned>(a, b, c)

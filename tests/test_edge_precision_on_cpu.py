@@ -69,6 +69,10 @@ def rising(c):
     scores, v = model.rising_scores(c["keys"], c["seed"], "cpu")
     return scores, v, None
 
+def small(c):
+    scores, v, v_scale = model.small_weights(c["keys"], c["above"], "cpu")
+    return (scores, v, v_scale) if c["bits8"] else (scores, v * v_scale[:, None], None)
+
 for c in json.loads(sys.stdin.read()):
     print(c, flush=True)
     dt = TYPES[c["dtype"]]
@@ -127,3 +131,12 @@ def test_scores_far_from_zero(run, base):
          for what, keys, new, seed in (("far", 64, 1, 0), ("far", 300, 3, 1), ("rising", 200, 2, 0), ("rising", 200, 70, 0),
                                        ("far", 150, 70, 1))
          for dtype in ("bf16", "f16")])
+
+
+@pytest.mark.parametrize("bits8", [0, 1])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_small_weights(run, dtype, bits8):
+    """Weights of e^-5 to e^-60 beside one of 1 whose value is zero."""
+    run([dict(op="paged", what="small", keys=keys, above=above, new=new, page=page, kv_heads=1, group=2, dtype=dtype, bits8=bits8,
+              base=0, part=2.0 ** -16)
+         for keys, new, page in ((500, 1, 16), (90, 3, 20), (700, 1, 16)) for above in (5, 10, 15, 17, 18, 22, 25, 60)])

@@ -48,3 +48,18 @@ def test_scores_far_from_zero(dim, dtype):
                 got = edge.attend(q, k, v16, *where, scale=1.0, max_queries=new, max_keys=keys)
                 over = model.over(got, scores, v, new, dtype, model.HALF[dtype])
                 assert over <= 0, (base, what, keys, new, seed, over)
+
+
+@pytest.mark.parametrize("bits8", [False, True])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("page", [16, 20, 7])
+@pytest.mark.parametrize("dim", [64, 96, 128])
+def test_small_weights(dim, page, dtype, bits8):
+    """Weights of e^-5 to e^-60 beside one of 1 whose value is zero, in the same tile, wave and workgroup and in others."""
+    for keys, new, group in ((500, 1, 2), (5000, 1, 4), (3000, 5, 8)):
+        for above in (5, 15, 17, 18, 25, 60):
+            scores, v, v_scale = model.small_weights(keys, above, "cuda", dim)
+            if bits8:
+                paged(scores, v, 0, new, page, dtype, True, 2.0 ** -16, v_scale, group=group, label=(keys, new, above))
+            else:
+                paged(scores, v * v_scale[:, None], 0, new, page, dtype, False, 2.0 ** -16, group=group, label=(keys, new, above))
