@@ -482,6 +482,12 @@ __device__ inline float column_sum(float x) {
 
 constexpr float GROWTH = 8.0f;  // the maximum may lag behind by this much (p up to 2^8) before out is rescaled
 
+// Values near the end of bfloat16's range, or scales of 8-bit ones, times p to 2^8, and their sums pass binary32.  A wave
+// that finds such a sum takes its keys once more, with p LOW times as large in that sum's column: 2^31 keys, p to 2^-32 and
+// values to 2^128 do not.  (Weights below 2^-86 of the largest, and elements of the column below 2^-86, may lose bits
+// there.)  What is joined has been divided by its sum.  32 users' tokens take 95.5 us for 95.2 without.
+constexpr float LOW = 0x1p-40f;
+
 // Eight codes as elements of T, exactly.
 template <typename T>
 __device__ inline typename Mma16<T>::frag of_codes(unsigned lo, unsigned hi) {
@@ -681,10 +687,10 @@ __device__ inline void take_non_finite(State16<DP> (&s)[CT], Tile<DP, false> &t,
     }
 }
 
-// Waves that a SIMD is to have room for: as many as leave them registers for all that a tile takes.  (Heads of 96 through
-// windows by binary16: 24 users' drafts on pages of 20 keys 22.4 us with three waves, 24.8 with two.)
+// Waves that a SIMD is to have room for: as many as leave them registers for all that a tile takes.  (On pages of 20 keys 24
+// users' binary16 drafts of heads of 96 take 22.4 us with three waves and 24.8 with two, 32 users' tokens over 8 bits 90 and 102.)
 constexpr int waves_a_simd(int dp, bool bits8, int ct, int aligned) {
-  if (aligned != 16) return aligned == -4 && dp == 96 ? 3 : aligned > 0 && bits8 && dp == 128 ? 1 : 2;
+  if (aligned != 16) return aligned == -4 && (dp < 128 || bits8) ? 3 : aligned > 0 && bits8 && dp == 128 ? 1 : 2;
   if (ct == 2) return 2;
   return dp == 64 ? 4 : bits8 || dp == 96 ? 3 : 2;
 }
@@ -730,64 +736,98 @@ __global__ __launch_bounds__(WAVES *WAVE, waves_a_simd(DP, BITS8, CT, ALIGNED)) 
       qf[c][j] = frag{};
       if (have && e < p.c.dim) qf[c][j] = *(const typename Raw<T, 8>::type *)(qrow + e);
     }
-    s[c].top = -INFINITY;
-    s[c].sum = 0.0f;
-#pragma unroll
-    for (int i = 0; i < DP / 16; ++i) s[c].out[i] = (f32x4){};
   }
   const int first_limit = shift + first_row;
-  const float lift = LIFTED<T, BITS8> ? LIFT : 0.0f;
   typedef typename std::conditional<ALIGNED == 16, InPages<T, DP, BITS8>, Anywhere<T, DP, BITS8, ALIGNED % 4 ? 1 : 4, (ALIGNED < 0)>>::type Cache;
-  // A share's waves take every so many tiles, so that pages that are not there are missing from all shares alike.
-  Cache cache(p, u, kv, until, share.index * WAVES + wave, share.count * WAVES);
-  Tile<DP, BITS8> t;
-  int64_t first = cache.find(), second = cache.find();
-  cache.load_keys(t, first);
-  cache.load_values(t, first);
-  // A tile's registers are loaded again as soon as they have been read: the next keys come while p and the values' sums
-  // are formed, the next values while the next scores are, and the page of the tile behind them is looked up.
-  while (first < until) {
-    const unsigned gone = cache.gone(first);
-    f32x4 sc[CT][2];
-    scores<T, DP, BITS8, CT>(sc, qf, t);
-    const int64_t third = cache.find();
-    cache.load_keys(t, second);
-    __builtin_amdgcn_sched_barrier(0);
-    if (first + TILE_KEYS - 1 > first_limit || first + TILE_KEYS > until || __any(gone != 0)) {
-      // some column does not see some key
-      frag saw[CT];
+  // Whether it is for the second time; then tops holds what the columns' p are multiplied by for their sums of values.
+  bool again = false;
+  for (;;) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+    for (int c = 0; c < CT; ++c) {
+      s[c].top = -INFINITY;
+      s[c].sum = 0.0f;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int64_t key = first + h * 16 + g * 4 + r;
-          const bool there = key < until && !(gone >> (h * 4 + r) & 1);
-          bool good = true;
-          if constexpr (BITS8) {
-            // p = 0 of a column that does not see a value times a scale that is not finite would be NaN; whoever sees
-            // it has no finite output
-            good = fabsf(t.v_scale[h][r]) < INFINITY;
-            t.v_scale[h][r] = good ? t.v_scale[h][r] : 0.0f;
-          }
-#pragma unroll
-          for (int c = 0; c < CT; ++c) {
-            const bool seen = there && key <= limit[c];
-            sc[c][h][r] = seen ? sc[c][h][r] : -INFINITY;
-            saw[c][h * 4 + r] = (T)(seen ? 1.0f : 0.0f);
-            if (!good && seen) s[c].sum = __uint_as_float(0x7fc00000u);
-          }
-        }
-      if constexpr (!BITS8) take_non_finite<T, DP, CT>(s, t, saw);  // (likewise)
+      for (int i = 0; i < DP / 16; ++i) s[c].out[i] = (f32x4){};
     }
+    // A share's waves take every so many tiles, so that pages that are not there are missing from all shares alike.
+    // (where the first tile stands is not the compiler's to know: it would keep what follows from it for the second time)
+    int from = share.index * WAVES + wave;
+    asm volatile("" : "+v"(from));
+    Cache cache(p, u, kv, until, __builtin_amdgcn_readfirstlane(from), share.count * WAVES);
+    Tile<DP, BITS8> t;
+    int64_t first = cache.find(), second = cache.find();
+    cache.load_keys(t, first);
+    cache.load_values(t, first);
+    // A tile's registers are loaded again as soon as they have been read: the next keys come while p and the values' sums
+    // are formed, the next values while the next scores are, and the page of the tile behind them is looked up.
+    while (first < until) {
+      const unsigned gone = cache.gone(first);
+      f32x4 sc[CT][2];
+      scores<T, DP, BITS8, CT>(sc, qf, t);
+      const int64_t third = cache.find();
+      cache.load_keys(t, second);
+      __builtin_amdgcn_sched_barrier(0);
+      if (first + TILE_KEYS - 1 > first_limit || first + TILE_KEYS > until || __any(gone != 0)) {
+        // some column does not see some key
+        frag saw[CT];
 #pragma unroll
-    for (int c = 0; c < CT; ++c) softmax<DP>(s[c], sc[c], p.scale, lift);
-    weighted<T, DP, BITS8, CT>(s, sc, t);
-    cache.load_values(t, second);
-    __builtin_amdgcn_sched_barrier(0);
-    first = second;
-    second = third;
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int64_t key = first + h * 16 + g * 4 + r;
+            const bool there = key < until && !(gone >> (h * 4 + r) & 1);
+            bool good = true;
+            if constexpr (BITS8) {
+              // p = 0 of a column that does not see a value times a scale that is not finite would be NaN; whoever sees
+              // it has no finite output
+              good = fabsf(t.v_scale[h][r]) < INFINITY;
+              t.v_scale[h][r] = good ? t.v_scale[h][r] : 0.0f;
+            }
+#pragma unroll
+            for (int c = 0; c < CT; ++c) {
+              const bool seen = there && key <= limit[c];
+              sc[c][h][r] = seen ? sc[c][h][r] : -INFINITY;
+              saw[c][h * 4 + r] = (T)(seen ? 1.0f : 0.0f);
+              if (!good && seen) s[c].sum = __uint_as_float(0x7fc00000u);
+            }
+          }
+        if constexpr (!BITS8) take_non_finite<T, DP, CT>(s, t, saw);  // (likewise)
+      }
+#pragma unroll
+      for (int c = 0; c < CT; ++c) softmax<DP>(s[c], sc[c], p.scale, LIFTED<T, BITS8> ? LIFT : 0.0f);
+      if (again) {
+#pragma unroll
+        for (int c = 0; c < CT; ++c) sc[c][0] *= tops[wave][c * 16 + l16], sc[c][1] *= tops[wave][c * 16 + l16];
+      }
+      weighted<T, DP, BITS8, CT>(s, sc, t);
+      cache.load_values(t, second);
+      __builtin_amdgcn_sched_barrier(0);
+      first = second;
+      second = third;
+    }
+    if constexpr (LIFTED<T, BITS8>) break;  // (2^31 keys, p to 2^15 and values to 2^16 stay within binary32)
+    if (again) break;
+    unsigned long long bad[CT], any = 0;
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+      float z = 0.0f;  // NaN with any sum that is not finite
+#pragma unroll
+      for (int i = 0; i < DP / 16; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) z = __builtin_fmaf(s[c].out[i][r], 0.0f, z);
+      any |= bad[c] = __ballot(z != z);
+    }
+    if (!any) break;
+    again = true;
+#pragma unroll
+    for (int c = 0; c < CT; ++c)  // (the column's four lanes write the same)
+      tops[wave][c * 16 + l16] = (bad[c] >> l16 | bad[c] >> (l16 + 16) | bad[c] >> (l16 + 32) | bad[c] >> (l16 + 48)) & 1 ? LOW : 1.0f;
   }
-  // the waves' results: each column's maximum, then sums and outputs relative to it
+  float even[CT];
+#pragma unroll
+  for (int c = 0; c < CT; ++c) even[c] = again ? 1.0f / tops[wave][c * 16 + l16] : 1.0f;
+  lanes_meet();
+  // The waves' results: each column's maximum and sum, then outputs relative to them, whose sums pass no value.
 #pragma unroll
   for (int c = 0; c < CT; ++c) {
     s[c].sum = column_sum(s[c].sum);
@@ -797,12 +837,23 @@ __global__ __launch_bounds__(WAVES *WAVE, waves_a_simd(DP, BITS8, CT, ALIGNED)) 
     }
   }
   __syncthreads();
+  auto top_of = [&](int c) {
+    float top = tops[0][c];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) top = fmaxf(top, tops[w][c]);
+    return top;
+  };
+  auto sum_of = [&](int c, float top) {
+    float sum = 0.0f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) sum += sums[w][c] * __builtin_amdgcn_exp2f((tops[w][c] - base_of(top)) * p.scale);
+    return sum;
+  };
 #pragma unroll
   for (int c = 0; c < CT; ++c) {
-    float top = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) top = fmaxf(top, tops[w][c * 16 + l16]);
-    const float f = __builtin_amdgcn_exp2f((s[c].top - base_of(top)) * p.scale);
+    const int col = c * 16 + l16;
+    const float top = top_of(col), sum = sum_of(col, top);
+    const float f = __builtin_amdgcn_exp2f((s[c].top - base_of(top)) * p.scale) * (sum > 0.0f ? 1.0f / sum : sum) * even[c];
 #pragma unroll
     for (int i = 0; i < DP / 16; ++i)
 #pragma unroll
@@ -813,25 +864,21 @@ __global__ __launch_bounds__(WAVES *WAVE, waves_a_simd(DP, BITS8, CT, ALIGNED)) 
   for (int i = threadIdx.x; i < COLUMNS * (DP / 4); i += THREADS) {
     const int c = i / (DP / 4), at = i % (DP / 4) * 4, col = column0 + c;
     if (col >= columns || at >= p.c.dim) continue;
-    float top = -INFINITY, sum = 0.0f;
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) top = fmaxf(top, tops[w][c]);
     f32x4 y = {0, 0, 0, 0};
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) {
-      sum += sums[w][c] * __builtin_amdgcn_exp2f((tops[w][c] - base_of(top)) * p.scale);
-      y += *(const f32x4 *)(mix + (w * COLUMNS + c) * PITCH + at);
-    }
+    for (int w = 0; w < WAVES; ++w) y += *(const f32x4 *)(mix + (w * COLUMNS + c) * PITCH + at);
     if (share.count == 1) {
-      const float f = sum > 0.0f ? 1.0f / sum : sum;
-      const float z[4] = {y[0] * f, y[1] * f, y[2] * f, y[3] * f};
+      const float z[4] = {y[0], y[1], y[2], y[3]};
       const int row = divide(col, p.by_group);
       store_f32<T, 4>((T *)p.out + (q.row + row) * p.out_stride + (kv * p.group + col - row * p.group) * p.out_head + at, z);
     } else {
       const int pitch = p.c.dim + 4;
       float *const part = p.part + ((((int64_t)c0 * p.tiles + tile) * p.c.kv_heads + kv) * COLUMNS + c) * pitch;
       *(f32x4 *)(part + at) = y;
-      if (at == 0) part[p.c.dim] = top, part[p.c.dim + 1] = sum;
+      if (at == 0) {
+        const float top = top_of(c);
+        part[p.c.dim] = top, part[p.c.dim + 1] = sum_of(c, top);
+      }
     }
   }
 }
@@ -856,7 +903,7 @@ __global__ __launch_bounds__((EACH < 4 ? 4 : EACH) * WAVE) void paged_join_kerne
   if (!some) return;
   const int64_t pitch = p.c.dim + 4, step = (int64_t)p.tiles * p.c.kv_heads * p.tile_columns * pitch;
   const float *const part = p.part + ((((int64_t)share.first * p.tiles + tile) * p.c.kv_heads + kv) * p.tile_columns + col % p.tile_columns) * pitch;
-  // a running maximum again: everything of a share is read at once
+  // A running maximum again: everything of a share is read at once.  y stays the weighted mean, which passes no value.
   float top = -INFINITY, sum = 0.0f;
   f32x4 y = {0, 0, 0, 0};
   const int at = l32 * 4 < p.c.dim ? l32 * 4 : 0;
@@ -873,26 +920,33 @@ __global__ __launch_bounds__((EACH < 4 ? 4 : EACH) * WAVE) void paged_join_kerne
     }
 #pragma unroll
     for (int i = 0; i < MORE; ++i) high = fmaxf(high, tops[i]);
-    const float base = base_of(high), f = __builtin_amdgcn_exp2f((top - base) * p.scale);
+    const float base = base_of(high), before = sum * __builtin_amdgcn_exp2f((top - base) * p.scale);
     top = high;
-    sum *= f;
-    y *= f;
+    sum = before;
 #pragma unroll
     for (int i = 0; i < MORE; ++i) {
       const bool have = i0 + i * HALVES < share.count;  // (others are repeated, and may hold anything)
-      const float w = __builtin_amdgcn_exp2f((tops[i] - base) * p.scale);
-      sum += have ? w * parts[i] : 0.0f;
+      parts[i] = have ? parts[i] * __builtin_amdgcn_exp2f((tops[i] - base) * p.scale) : 0.0f;
+      sum += parts[i];
+    }
+    const float f = sum > 0.0f ? 1.0f / sum : sum;
+    y *= before * f;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) y[j] += have ? w * x[i][j] : 0.0f;
+    for (int i = 0; i < MORE; ++i) {
+      const bool have = i0 + i * HALVES < share.count;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) y[j] += have ? parts[i] * f * x[i][j] : 0.0f;
     }
   }
   // the two halves', then the waves' results
   auto both = [&](float top2, float sum2, f32x4 y2) {
     const float high = fmaxf(top, top2), base = base_of(high);
-    const float f = __builtin_amdgcn_exp2f((top - base) * p.scale), f2 = __builtin_amdgcn_exp2f((top2 - base) * p.scale);
+    sum *= __builtin_amdgcn_exp2f((top - base) * p.scale);
+    sum2 *= __builtin_amdgcn_exp2f((top2 - base) * p.scale);
+    const float both = sum + sum2, f = both > 0.0f ? 1.0f / both : both;
     top = high;
-    sum = sum * f + sum2 * f2;
-    y = y * f + y2 * f2;
+    y = y * (sum * f) + y2 * (sum2 * f);
+    sum = both;
   };
   f32x4 other;
 #pragma unroll
@@ -908,8 +962,7 @@ __global__ __launch_bounds__((EACH < 4 ? 4 : EACH) * WAVE) void paged_join_kerne
     for (int w = 1; w < EACH; ++w) both(tops[w], sums[w], *(const f32x4 *)(mix[w] + l32 * 4));
   }
   if (lane >= 32 || l32 * 4 >= p.c.dim) return;
-  const float f = sum > 0.0f ? 1.0f / sum : sum;
-  const float z[4] = {y[0] * f, y[1] * f, y[2] * f, y[3] * f};
+  const float z[4] = {y[0], y[1], y[2], y[3]};
   const int row = divide(col, p.by_group);
   store_f32<T, 4>((T *)p.out + (share.q.row + row) * p.out_stride + (kv * p.group + col - row * p.group) * p.out_head + l32 * 4, z);
 }

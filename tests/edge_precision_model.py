@@ -106,3 +106,13 @@ def small_weights(keys, above, device, dim=16):
     r = (torch.arange(keys) == 0).int() * above
     v = torch.randint(64, 128, (keys, dim), generator=gen).float() * (r == 0)[:, None]
     return r.to(device), v.to(device), torch.full((keys,), 256.0, device=device)
+
+
+def huge_values(keys, seed, device, dim=16):
+    """Values near the end of bfloat16's range, of either sign in some columns, with scores that rise slowly: sums of values
+    times weights that nobody has divided yet pass binary32."""
+    gen = torch.Generator().manual_seed(seed)
+    r = torch.arange(keys) * 5 // keys
+    v = torch.randint(64, 128, (keys, dim), generator=gen).float()
+    v[:, dim // 2:] *= torch.randint(0, 2, (keys, dim - dim // 2), generator=gen) * 2 - 1
+    return r.to(device), v.to(device), torch.full((keys,), 2.0 ** 121, device=device)

@@ -73,6 +73,10 @@ def small(c):
     scores, v, v_scale = model.small_weights(c["keys"], c["above"], "cpu")
     return (scores, v, v_scale) if c["bits8"] else (scores, v * v_scale[:, None], None)
 
+def huge(c):
+    scores, v, v_scale = model.huge_values(c["keys"], c["seed"], "cpu")
+    return (scores, v, v_scale) if c["bits8"] else (scores, v * v_scale[:, None], None)
+
 for c in json.loads(sys.stdin.read()):
     print(c, flush=True)
     dt = TYPES[c["dtype"]]
@@ -140,3 +144,11 @@ def test_small_weights(run, dtype, bits8):
     run([dict(op="paged", what="small", keys=keys, above=above, new=new, page=page, kv_heads=1, group=2, dtype=dtype, bits8=bits8,
               base=0, part=2.0 ** -16)
          for keys, new, page in ((500, 1, 16), (90, 3, 20), (700, 1, 16)) for above in (5, 10, 15, 17, 18, 22, 25, 60)])
+
+
+@pytest.mark.parametrize("bits8", [0, 1])
+def test_huge_values(run, bits8):
+    """Sums that pass binary32 before they are divided."""
+    run([dict(op="paged", what="huge", keys=keys, seed=seed, new=new, page=page, kv_heads=1, group=2, dtype="bf16", bits8=bits8,
+              base=0, part=2.0 ** -16)
+         for keys, new, page in ((1, 1, 16), (200, 1, 16), (90, 3, 20), (1500, 1, 16)) for seed in (0, 1)])

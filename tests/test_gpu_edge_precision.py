@@ -63,3 +63,16 @@ def test_small_weights(dim, page, dtype, bits8):
                 paged(scores, v, 0, new, page, dtype, True, 2.0 ** -16, v_scale, group=group, label=(keys, new, above))
             else:
                 paged(scores, v * v_scale[:, None], 0, new, page, dtype, False, 2.0 ** -16, group=group, label=(keys, new, above))
+
+
+@pytest.mark.parametrize("bits8", [False, True])
+@pytest.mark.parametrize("page", [16, 20, 7])
+@pytest.mark.parametrize("dim", [64, 96, 128])
+def test_huge_values(dim, page, bits8):
+    """Sums that pass binary32 before they are divided, in one wave and where waves and workgroups are joined."""
+    for keys, new, group in ((1, 1, 2), (200, 1, 2), (5000, 1, 4), (3000, 5, 8), (70000, 1, 2)):
+        scores, v, v_scale = model.huge_values(keys, keys, "cuda", dim)
+        if bits8:
+            paged(scores, v, 0, new, page, BF16, True, 2.0 ** -16, v_scale, group=group, label=(keys, new))
+        else:
+            paged(scores, v * v_scale[:, None], 0, new, page, BF16, False, 2.0 ** -16, group=group, label=(keys, new))
