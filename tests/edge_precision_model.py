@@ -66,18 +66,18 @@ def outputs(scores, values, new):
     return torch.stack(out), torch.stack(mass)
 
 
-def bound(out, mass, keys, dtype, part):
+def bound(out, mass, keys, dtype, part, reach=128):
     """`part`: how far the weight that goes into the product may be from p, relative.  A difference of two scores, exact,
-    is multiplied by log2(e), which is rounded and rounds: 2 * 2^-24 of an exponent to 2^7, 0.7 of that of p; the joins of
-    waves and workgroups do it again, the exponential adds a little: 2^-15 covers four of them for exponents to 2^7
-    (2 * 2^-17 * 0.7 * 4 < 2^-15).  Sums are binary32, numerator and denominator."""
-    return out.abs() * HALF[dtype] * 1.01 + LEAST[dtype] + mass * (part + 2.0 ** -15 + 2 * (keys + 64) * U32)
+    is multiplied by scale * log2(e), which has been rounded, and rounds: an exponent to `reach` is off by reach * 2^-23, p
+    by 0.7 of that, relative.  Waves and workgroups are joined by three more such factors: 4 * 0.7 * reach * 2^-23, and
+    reach * 2^-21 stands for it and the exponentials' own steps.  Sums are binary32, numerator and denominator."""
+    return out.abs() * HALF[dtype] * 1.01 + LEAST[dtype] + mass * (part + reach * 2.0 ** -21 + 2 * (keys + 64) * U32)
 
 
-def over(got, scores, values, new, dtype, part):
+def over(got, scores, values, new, dtype, part, reach=128):
     """By how much the worst element of got [new, heads, dim] passes its bound (not above 0: none)."""
     out, mass = outputs(scores, values, new)
-    off = (got.double() - out[:, None]).abs() - bound(out, mass, len(scores), dtype, part)[:, None]
+    off = (got.double() - out[:, None]).abs() - bound(out, mass, len(scores), dtype, part, reach)[:, None]
     assert not got.isnan().any() and not off.isnan().any()
     return off.max().item()
 
@@ -116,3 +116,22 @@ def huge_values(keys, seed, device, dim=16):
     v = torch.randint(64, 128, (keys, dim), generator=gen).float()
     v[:, dim // 2:] *= torch.randint(0, 2, (keys, dim - dim // 2), generator=gen) * 2 - 1
     return r.to(device), v.to(device), torch.full((keys,), 2.0 ** 121, device=device)
+
+
+def cancelling_values(keys, seed, dtype, bits8, device, dim=16):
+    """The last key's values are chosen so that the output is next to nothing beside what is summed: it shows each weight's
+    own rounding, not the output's.  For one row."""
+    gen = torch.Generator().manual_seed(seed)
+    r = torch.randint(0, 7, (keys,), generator=gen)
+    r[0], r[-1] = 6, 5
+    v = (torch.rand(keys, dim, generator=gen) * 254 - 127).round()
+    v[-1] = 0
+    p = torch.softmax(r.double(), dim=0)
+    last = -(p @ v.double()) / p[-1]
+    scale = torch.ones(keys)
+    if bits8:
+        scale[-1] = last.abs().max() / 127
+        v[-1] = (last / scale[-1].double()).round()
+    else:
+        v[-1] = last.to(dtype).float()
+    return r.to(device), v.to(device), scale.to(device)

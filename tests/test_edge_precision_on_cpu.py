@@ -77,13 +77,17 @@ def huge(c):
     scores, v, v_scale = model.huge_values(c["keys"], c["seed"], "cpu")
     return (scores, v, v_scale) if c["bits8"] else (scores, v * v_scale[:, None], None)
 
+def cancelling(c):
+    scores, v, v_scale = model.cancelling_values(c["keys"], c["seed"], TYPES[c["dtype"]], c["bits8"], "cpu")
+    return scores, v, v_scale if c["bits8"] else None
+
 for c in json.loads(sys.stdin.read()):
     print(c, flush=True)
     dt = TYPES[c["dtype"]]
     scores, v, v_scale = globals()[c["what"]](c)
     values = v if v_scale is None else v.double() * v_scale.double()[:, None]
     got = packed(c, scores, v) if c["op"] == "attend" else paged(c, scores, v, v_scale)
-    over = model.over(got, scores, values, c["new"], dt, c["part"])
+    over = model.over(got, scores, values, c["new"], dt, c["part"], c.get("reach", 128))
     assert over <= 0, (c, over)
 print("RUN COMPLETE", flush=True)
 """
@@ -152,3 +156,12 @@ def test_huge_values(run, bits8):
     run([dict(op="paged", what="huge", keys=keys, seed=seed, new=new, page=page, kv_heads=1, group=2, dtype="bf16", bits8=bits8,
               base=0, part=2.0 ** -16)
          for keys, new, page in ((1, 1, 16), (200, 1, 16), (90, 3, 20), (1500, 1, 16)) for seed in (0, 1)])
+
+
+@pytest.mark.parametrize("bits8", [0, 1])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_weights_keep_16_bits(run, dtype, bits8):
+    """Sums of terms that cancel: a weight of one part, 8 or 11 bits, would show."""
+    run([dict(op="paged", what="cancelling", keys=keys, seed=seed, new=1, page=page, kv_heads=1, group=2, dtype=dtype, bits8=bits8,
+              base=0, part=2.0 ** -16, reach=9)
+         for keys, page in ((2, 16), (5, 16), (20, 16), (60, 20), (300, 16)) for seed in range(3)])

@@ -10,12 +10,13 @@ pytestmark = pytest.mark.gpu
 BF16, F16 = torch.bfloat16, torch.float16
 
 
-def paged(scores, v, base, new, page, dtype, bits8, part, v_scale=None, kv_heads=2, group=2, label=None):
+def paged(scores, v, base, new, page, dtype, bits8, part, v_scale=None, kv_heads=2, group=2, label=None,
+          reach=128):
     s = model.paged(scores, v, base, new, page, kv_heads, group, dtype, bits8, v_scale)
     got = edge.attend_paged(s["q"], s["cache"], s["table"], s["row_start"], s["key_count"], scale=1.0, max_queries=new,
                             max_keys=len(scores))
     values = v if v_scale is None else v.double() * v_scale.double()[:, None]
-    over = model.over(got, scores, values, new, dtype, part)
+    over = model.over(got, scores, values, new, dtype, part, reach)
     assert over <= 0, (label, over)
 
 
@@ -76,3 +77,17 @@ def test_huge_values(dim, page, bits8):
             paged(scores, v, 0, new, page, BF16, True, 2.0 ** -16, v_scale, group=group, label=(keys, new))
         else:
             paged(scores, v * v_scale[:, None], 0, new, page, BF16, False, 2.0 ** -16, group=group, label=(keys, new))
+
+
+@pytest.mark.parametrize("bits8", [False, True])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("page", [16, 20, 7])
+@pytest.mark.parametrize("dim", [64, 96, 128])
+def test_weights_keep_16_bits(dim, page, dtype, bits8):
+    """Sums of terms that cancel: a weight of one part, 8 or 11 bits, would show."""
+    for keys in (2, 5, 20, 60, 300, 2000):
+        for seed in range(2):
+            scores, v, v_scale = model.cancelling_values(keys, seed, dtype, bits8, "cuda", dim)
+            for group in (2, 8):
+                paged(scores, v, 0, 1, page, dtype, bits8, 2.0 ** -16, v_scale if bits8 else None, group=group, reach=9,
+                      label=(keys, seed))
