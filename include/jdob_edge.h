@@ -160,7 +160,7 @@ typedef struct {
   const int64_t *key_start;       /* [num_sequences]                         */
   const int32_t *key_count;       /* [num_sequences]                         */
   void *out;                      /* [query_rows][num_heads][head_dim]       */
-  int64_t out_stride, out_head_stride; /* >= head_dim, where there is more than one */
+  int64_t out_stride, out_head_stride; /* no two rows or heads share elements  */
   void *workspace;                /* jdob_edge_attend_workspace bytes        */
   int64_t workspace_bytes;
 } jdob_edge_attend_args;
@@ -208,7 +208,8 @@ typedef struct {
  * nothing else of the cache changes.  At most one row may be written to a
  * slot.  jdob_edge_cache_read does the reverse with the same arguments:
  * 8-bit rows become code * scale rounded to dtype, a row whose key is absent
- * or negative becomes zeros, a row of no sequence is left as it was.        */
+ * or negative becomes zeros, a row of no sequence is left as it was; there no
+ * two rows or heads of k or of v may share elements.                        */
 typedef struct {
   jdob_edge_cache cache;
   int32_t num_sequences;          /* 0 .. JDOB_EDGE_MAX_SEQUENCES            */
@@ -252,7 +253,7 @@ typedef struct {
   const void *q;                  /* [query_rows][num_heads][head_dim]       */
   int64_t q_stride, q_head_stride;
   void *out;                      /* [query_rows][num_heads][head_dim]       */
-  int64_t out_stride, out_head_stride; /* >= head_dim, where there is more than one */
+  int64_t out_stride, out_head_stride; /* no two rows or heads share elements  */
   void *workspace;                /* jdob_edge_attend_paged_workspace bytes  */
   int64_t workspace_bytes;
 } jdob_edge_attend_paged_args;

@@ -680,9 +680,6 @@ int attend_check(const jdob_edge_attend_args *a, bool sizes_only) {
   if (a->q_stride < 0 || a->q_head_stride < 0 || a->k_stride < 0 || a->k_head_stride < 0 || a->v_stride < 0 ||
       a->v_head_stride < 0 || a->out_stride < 0 || a->out_head_stride < 0)
     return JDOB_ERR_INVALID_ARG;
-  // rows and heads of out that are written at once must not share elements
-  if ((a->query_rows > 1 && a->out_stride < a->head_dim) || (a->num_heads > 1 && a->out_head_stride < a->head_dim))
-    return JDOB_ERR_INVALID_ARG;
   const int64_t need = jdob_edge_attend_workspace(a);
   if (need > 0 && (!a->workspace || (uintptr_t)a->workspace % 16 || a->workspace_bytes < need))
     return JDOB_ERR_INVALID_ARG;
@@ -717,12 +714,14 @@ FewPlan few_plan(const jdob_edge_attend_args *a) {
   return {true, (int)tiles, (int)(splits < 1 ? 1 : splits), (int)(each < INT32_MAX ? each : INT32_MAX)};
 }
 
+// `clash`: rows or heads of out share elements (looked at behind the sizes).
 template <typename T, int DP>
-int attend(AttendParams p, bool few, bool direct, hipStream_t stream) {
+int attend(AttendParams p, bool few, bool direct, bool clash, hipStream_t stream) {
   if (few) {
     const int64_t groups = (int64_t)p.sequences * p.kv_heads * p.tiles;
     const int64_t columns = (int64_t)p.sequences * p.kv_heads * p.max_queries * p.group;
     if (groups * p.splits > MAX_BLOCKS || columns > MAX_BLOCKS) return JDOB_ERR_UNSUPPORTED;
+    if (clash) return JDOB_ERR_INVALID_ARG;
     const int code = direct ? launch(few_kernel<T, DP, true>, groups * p.splits, FEW_WAVES * WAVE, stream, p)
                             : launch(few_kernel<T, DP, false>, groups * p.splits, FEW_WAVES * WAVE, stream, p);
     if (code != JDOB_OK || p.splits == 1) return code;
@@ -730,14 +729,15 @@ int attend(AttendParams p, bool few, bool direct, hipStream_t stream) {
   }
   const int64_t blocks = (int64_t)p.tiles * p.heads;
   if (blocks > MAX_BLOCKS) return JDOB_ERR_UNSUPPORTED;
+  if (clash) return JDOB_ERR_INVALID_ARG;
   return direct ? launch(prompt_kernel<T, DP, true>, blocks, PROMPT_WAVES * WAVE, stream, p)
                 : launch(prompt_kernel<T, DP, false>, blocks, PROMPT_WAVES * WAVE, stream, p);
 }
 
 template <typename T>
-int attend(const AttendParams &p, bool few, bool direct, hipStream_t stream) {
-  if (p.dim <= 64) return attend<T, 64>(p, few, direct, stream);
-  return p.dim <= 96 ? attend<T, 96>(p, few, direct, stream) : attend<T, 128>(p, few, direct, stream);
+int attend(const AttendParams &p, bool few, bool direct, bool clash, hipStream_t stream) {
+  if (p.dim <= 64) return attend<T, 64>(p, few, direct, clash, stream);
+  return p.dim <= 96 ? attend<T, 96>(p, few, direct, clash, stream) : attend<T, 128>(p, few, direct, clash, stream);
 }
 
 }  // namespace
@@ -769,5 +769,8 @@ extern "C" int jdob_edge_attend(const jdob_edge_attend_args *a, void *hip_stream
                       (uintptr_t)a->k % 16 == 0 && (uintptr_t)a->v % 16 == 0 && a->k_stride % 8 == 0 &&
                     a->k_head_stride % 8 == 0 && a->v_stride % 8 == 0 && a->v_head_stride % 8 == 0 && a->k_stride < (1 << 24) && a->v_stride < (1 << 24);
   hipStream_t stream = (hipStream_t)hip_stream;
-  return a->dtype == JDOB_EDGE_BF16 ? attend<__bf16>(p, f.few, direct, stream) : attend<_Float16>(p, f.few, direct, stream);
+  // rows and heads of out that are written at once must not share elements
+  const bool clash = pieces_overlap(a->query_rows, a->out_stride, a->num_heads, a->out_head_stride, a->head_dim);
+  return a->dtype == JDOB_EDGE_BF16 ? attend<__bf16>(p, f.few, direct, clash, stream)
+                                    : attend<_Float16>(p, f.few, direct, clash, stream);
 }

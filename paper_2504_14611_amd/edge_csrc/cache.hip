@@ -239,8 +239,8 @@ int cache_rows(const jdob_edge_cache_rows_args *a, bool write, void *hip_stream)
   const int64_t d = a->cache.head_dim, g = a->cache.num_kv_heads;
   if (a->k_stride < 0 || a->k_head_stride < 0 || a->v_stride < 0 || a->v_head_stride < 0) return JDOB_ERR_INVALID_ARG;
   // rows and heads that are written at once must not share elements
-  if (!write && ((a->rows > 1 && (a->k_stride < d || a->v_stride < d)) ||
-                 (g > 1 && (a->k_head_stride < d || a->v_head_stride < d))))
+  if (!write && (pieces_overlap(a->rows, a->k_stride, g, a->k_head_stride, d) ||
+                 pieces_overlap(a->rows, a->v_stride, g, a->v_head_stride, d)))
     return JDOB_ERR_INVALID_ARG;
   const RowsParams p = {pages_of(a->cache, a->num_sequences, a->table_width, a->table, a->table_stride, a->row_start,
                                  a->key_count),

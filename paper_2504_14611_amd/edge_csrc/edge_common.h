@@ -102,6 +102,21 @@ __device__ inline void barrier() {
   asm volatile("" ::: "memory");
 }
 
+// Whether two of rows x heads pieces of `width` elements, whose rows and heads start so many elements from each other, share
+// an element.  (Strides are not below zero.  One of two strides that no memory has room for counts as shared.)
+inline bool pieces_overlap(int64_t rows, int64_t row, int64_t heads, int64_t head, int64_t width) {
+  if ((rows > 1 && row < width) || (heads > 1 && head < width)) return true;
+  if (rows < 2 || heads < 2) return false;
+  if ((row - width) / (heads - 1) >= head || (head - width) / (rows - 1) >= row) return false;  // one within the other
+  if (head > INT64_MAX / 4096 || row > INT64_MAX / 4096) return true;
+  // h heads against the rows next to them
+  for (int64_t h = 1; h < heads; ++h) {
+    const int64_t r = h * head / row, past = h * head - r * row;
+    if ((r < rows && past < width) || (r + 1 < rows && row - past < width)) return true;
+  }
+  return false;
+}
+
 // A dimension of a grid takes fewer than 2^32 threads: more than FOLD workgroups stand in rows of FOLD, and
 // those behind the last one, in the last row, have nothing to do.
 constexpr int FOLD = 1 << 21, MAX_BLOCKS = 0x7fffffff - FOLD;

@@ -1098,8 +1098,8 @@ extern "C" int jdob_edge_attend_paged(const jdob_edge_attend_paged_args *a, void
   if (code != JDOB_OK) return code;
   if (!a->q || !a->out || a->q_stride < 0 || a->q_head_stride < 0) return JDOB_ERR_INVALID_ARG;
   // rows and heads of out that are written at once must not share elements
-  if ((a->query_rows > 1 && a->out_stride < a->cache.head_dim) || (a->num_heads > 1 && a->out_head_stride < a->cache.head_dim) ||
-      a->out_stride < 0 || a->out_head_stride < 0)
+  if (a->out_stride < 0 || a->out_head_stride < 0 ||
+      pieces_overlap(a->query_rows, a->out_stride, a->num_heads, a->out_head_stride, a->cache.head_dim))
     return JDOB_ERR_INVALID_ARG;
   const int64_t need = jdob_edge_attend_paged_workspace(a);
   if (need > 0 && (!a->workspace || (uintptr_t)a->workspace % 16 || a->workspace_bytes < need)) return JDOB_ERR_INVALID_ARG;
