@@ -20,6 +20,7 @@ from __future__ import annotations
 
 import argparse
 import dataclasses
+import itertools
 import time
 from typing import Dict, List, Optional, Sequence
 
@@ -84,15 +85,18 @@ class Edge:
 
     Every user has a slab of `room` rows in each block's cache; new keys and values are written behind those that
     stand there already.  With `page` the cache is made of `pages` pages of so many keys (default: as many as all users
-    may fill), which users take as they grow; it holds 8-bit rows with bits8."""
+    may fill), which users take as they grow; it holds 8-bit rows with bits8, and then all rows attend to what the cache
+    stands for, their own and the other new ones' keys and values among it.  Users with up to FEW new rows attend over the
+    pages as they are, the others to rows that are read back, each user for itself: what a user's rows see does not depend on
+    who else is in the batch."""
 
-    FEW = 8  # rows a user that go over the pages as they are; more read them back first
+    FEW = 8
 
     def __init__(self, shape: Shape, chain: Sequence[dict], users: Sequence[int], first: int, room: int, device="cuda",
                  page: int = 0, bits8: bool = False, pages: Optional[int] = None):
         import torch
         self.shape, self.chain, self.users, self.device = shape, list(chain[first:]), list(users), device
-        self.room, self.count, self.page = room, [0] * len(self.users), page
+        self.room, self.count, self.page, self.bits8 = room, [0] * len(self.users), page, bits8
         if page:
             each = -(-room // page)
             pages = len(self.users) * each if pages is None else pages
@@ -118,15 +122,56 @@ class Edge:
         return torch.tensor([held + [-1] * (width - len(held)) for held in self.held], dtype=torch.int32,
                             device=self.device).view(len(self.users), width)
 
-    def _attend_pages(self, q, k, v, cache, table, query_start, key_count, all_start, lengths, counts):
+    def _plan(self, lengths: Sequence[int], counts: Sequence[int]) -> dict:
+        """Where the new rows go, and for the users with few and with many of them: their rows (None: all there are),
+        tables, starts of their rows and of all their keys."""
+        import torch
+
+        def on_device(x, dtype=torch.int32):
+            return torch.tensor(x, dtype=dtype, device=self.device)
+
+        def starts(x):
+            return [0, *itertools.accumulate(x)]
+
+        table, first, groups = self._take_pages(counts), starts(lengths), []
+        query_start, key_count = on_device(first), on_device(counts)
+        for few in (True, False):
+            users = [u for u, m in enumerate(lengths) if m and (m <= self.FEW) == few]
+            if not users:
+                continue
+            new, keys = [lengths[u] for u in users], [counts[u] for u in users]
+            g = {"rows": None, "table": table, "query_start": query_start, "key_count": key_count}
+            if sum(new) < first[-1]:
+                g["rows"] = on_device([first[u] + i for u in users for i in range(lengths[u])], torch.int64)
+            if len(users) < len(lengths):
+                g.update(table=table[on_device(users, torch.int64)], query_start=on_device(starts(new)), key_count=on_device(keys))
+            key_start = None if few else on_device(starts(keys))
+            # (rows without a history are read back as they are out of 16 bits)
+            groups.append({**g, "few": few, "read": not few and (self.bits8 or new != keys), "key_start": key_start,
+                           "most": max(new), "longest": max(keys), "keys": sum(keys)})
+        return {"table": table, "query_start": query_start, "key_count": key_count, "groups": groups}
+
+    def _attend_pages(self, q, k, v, cache, plan):
         """The rows' keys and values into the cache, and their attention."""
-        edge.cache_write(k, v, cache, table, query_start, key_count)
-        most, longest = max(lengths), max(counts)
-        if most <= self.FEW:
-            return edge.attend_paged(q, cache, table, query_start, key_count, max_queries=most, max_keys=longest)
-        if any(c > m for c, m in zip(counts, lengths)):  # chunks after a history
-            k, v = edge.cache_read(cache, table, all_start, key_count, rows=sum(counts), dtype=q.dtype)
-        return edge.attend(q, k, v, query_start, all_start[:-1].long(), key_count, max_queries=most, max_keys=longest)
+        import torch
+        edge.cache_write(k, v, cache, plan["table"], plan["query_start"], plan["key_count"])
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if len(plan["groups"]) > 1 else None
+        for g in plan["groups"]:
+            rows, where = g["rows"], (g["table"], g["query_start"], g["key_count"])
+            qg = q if rows is None else q[rows]
+            most = {"max_queries": g["most"], "max_keys": g["longest"]}
+            if g["few"]:
+                y = edge.attend_paged(qg, cache, *where, **most)
+            else:
+                if g["read"]:
+                    kg, vg = edge.cache_read(cache, g["table"], g["key_start"], g["key_count"], rows=g["keys"], dtype=q.dtype)
+                else:
+                    kg, vg = (k, v) if rows is None else (k[rows], v[rows])
+                y = edge.attend(qg, kg, vg, g["query_start"], g["key_start"][:-1].long(), g["key_count"], **most)
+            if out is None:
+                return y
+            out[rows] = y
+        return torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
 
     def run(self, rows, lengths: Sequence[int]):
         """`rows` [sum of lengths, width]: each user's new rows behind each other, as they enter the first block.
@@ -140,16 +185,14 @@ class Edge:
             raise ValueError(f"the cache has room for {self.room} rows a user")
         if not self.chain:
             return rows
-        starts = [sum(lengths[:u]) for u in range(n + 1)]
-        query_start = torch.tensor(starts, dtype=torch.int32, device=dev)
-        key_start = torch.arange(n, device=dev) * self.room
         counts = [c + m for c, m in zip(self.count, lengths)]
-        key_count = torch.tensor(counts, dtype=torch.int32, device=dev)
         row_adapter = torch.tensor(np.repeat(np.asarray(self.users, dtype=np.int32), lengths), device=dev)
         if self.page:
-            table = self._take_pages(counts)
-            all_start = torch.tensor([sum(counts[:u]) for u in range(n + 1)], dtype=torch.int32, device=dev)
+            plan = self._plan(lengths, counts)
         else:
+            query_start = torch.tensor([0, *itertools.accumulate(lengths)], dtype=torch.int32, device=dev)
+            key_start = torch.arange(n, device=dev) * self.room
+            key_count = torch.tensor(counts, dtype=torch.int32, device=dev)
             slots = torch.tensor(np.concatenate([u * self.room + c + np.arange(m) for u, (c, m) in
                                                  enumerate(zip(self.count, lengths))]).astype(np.int64), device=dev)
 
@@ -164,7 +207,7 @@ class Edge:
             qkv = project(block["qkv"], r["q"], r["scale"]).view(-1, s.heads + 2 * s.kv_heads, s.head_dim)
             if self.page:
                 y = self._attend_pages(qkv[:, :s.heads], qkv[:, s.heads:s.heads + s.kv_heads], qkv[:, s.heads + s.kv_heads:],
-                                       cache, table, query_start, key_count, all_start, lengths, counts)
+                                       cache, plan)
             else:
                 cache[slots] = qkv[:, s.heads:].reshape(-1, 2, s.kv_heads, s.head_dim)
                 y = edge.attend(qkv[:, :s.heads], cache[:, 0], cache[:, 1], query_start, key_start, key_count,
