@@ -97,6 +97,8 @@ class Edge:
         import torch
         self.shape, self.chain, self.users, self.device = shape, list(chain[first:]), list(users), device
         self.room, self.count, self.page, self.bits8 = room, [0] * len(self.users), page, bits8
+        if page < 0:
+            raise ValueError(f"pages of {page} keys")
         if page:
             each = -(-room // page)
             pages = len(self.users) * each if pages is None else pages
@@ -302,6 +304,10 @@ def main(argv=None) -> Dict[str, object]:
     for field in dataclasses.fields(Shape):
         p.add_argument("--" + field.name.replace("_", "-"), type=int, default=field.default)
     a = p.parse_args(argv)
+    if not 0 <= a.page <= edge.MAX_PAGE_SIZE:
+        p.error(f"--page: 0 to {edge.MAX_PAGE_SIZE} keys")
+    if a.cache_bits == 8 and not a.page:
+        p.error("--cache-bits 8: 8-bit keys and values stand on pages (--page)")
     shape = Shape(*[getattr(a, field.name) for field in dataclasses.fields(Shape)])
     chain = make_chain(shape, a.users)
     alpha, beta = profile(shape, chain, a.users, a.tokens)
