@@ -8,7 +8,7 @@
 //
 // Bound: HBM.  131,072 8-bit rows of 8 heads of 128 read back in 162 us (805 MB, 5.0 TB/s; a large copy moves 4.9; with
 // one block of rows a workgroup 198); 16,192 rows written in 8 bits in 26 us (101 MB, 3.9 TB/s; lane exchanges without
-// LDS and four blocks a workgroup change nothing there) and read back in 19; 32 rows written in 3.5 us, a launch.
+// LDS change nothing there) and read back in 19; 32 rows written in 3.5 us, a launch.
 #include <type_traits>
 
 #include "pages.h"
@@ -115,50 +115,41 @@ __device__ inline u32x2 codes_of(const typename Raw<T, 8>::type &x, float *scale
   return c;
 }
 
-// A workgroup takes B times 256 / L rows of one head.
-template <typename T, bool BITS8, int L, int B>
+// A workgroup takes 256 / L rows of one head.
+template <typename T, bool BITS8, int L>
 __global__ __launch_bounds__(CACHE_THREADS) void write_kernel(RowsParams p) {
   constexpr int ROWS = CACHE_THREADS / L;
   typedef typename Raw<T, 8>::type Vec;
   const int head = block_index() % p.c.kv_heads, e = threadIdx.x % L * 8;
-  const int64_t row0 = (int64_t)(block_index() / p.c.kv_heads) * (B * ROWS) + threadIdx.x / L;
-  if (block_index() / p.c.kv_heads * (int64_t)(B * ROWS) >= p.rows) return;
-  Vec x[B][2];
-#pragma unroll
-  for (int b = 0; b < B; ++b) {
-    const int64_t row = row0 + b * ROWS;
-    const bool in = row < p.rows && e < p.c.dim;
-    x[b][0] = x[b][1] = Vec{};
-    if (in) {
-      x[b][0] = *(const Vec *)((const T *)p.k + row * p.k_stride + head * p.k_head + e);
-      x[b][1] = *(const Vec *)((const T *)p.v + row * p.v_stride + head * p.v_head + e);
-    }
+  const int64_t first = (int64_t)(block_index() / p.c.kv_heads) * ROWS, row = first + threadIdx.x / L;
+  if (first >= p.rows) return;
+  const bool in = row < p.rows && e < p.c.dim;
+  Vec x[2] = {};
+  if (in) {
+    x[0] = *(const Vec *)((const T *)p.k + row * p.k_stride + head * p.k_head + e);
+    x[1] = *(const Vec *)((const T *)p.v + row * p.v_stride + head * p.v_head + e);
   }
   Places<L> places(p);
-  Place at[B];
+  const Place at = places.find(row < p.rows ? (int)row : p.rows - 1);
+  const bool stands = in && at.page >= 0;
 #pragma unroll
-  for (int b = 0; b < B; ++b) at[b] = places.find(row0 + b * ROWS < p.rows ? (int)(row0 + b * ROWS) : p.rows - 1);
-#pragma unroll
-  for (int b = 0; b < B; ++b) {
-    const bool stands = row0 + b * ROWS < p.rows && e < p.c.dim && at[b].page >= 0;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const Pool &to = i ? p.c.v : p.c.k;
-      const int64_t spot = at[b].page * to.page + head * to.head + at[b].slot * to.slot + e;
-      if constexpr (!BITS8) {
-        if (stands) *(Vec *)((T *)to.at + spot) = x[b][i];
-      } else {
-        float scale;
-        const u32x2 c = codes_of<T, L>(x[b][i], &scale);
-        if (stands) {
-          *(Raw<int8_t, 8>::type *)((int8_t *)to.at + spot) = __builtin_bit_cast(Codes, c);
-          if (e == 0) to.scale[at[b].page * to.scale_page + head * to.scale_head + at[b].slot * to.scale_slot] = scale;
-        }
+  for (int i = 0; i < 2; ++i) {
+    const Pool &to = i ? p.c.v : p.c.k;
+    const int64_t spot = at.page * to.page + head * to.head + at.slot * to.slot + e;
+    if constexpr (!BITS8) {
+      if (stands) *(Vec *)((T *)to.at + spot) = x[i];
+    } else {
+      float scale;
+      const u32x2 c = codes_of<T, L>(x[i], &scale);
+      if (stands) {
+        *(Raw<int8_t, 8>::type *)((int8_t *)to.at + spot) = __builtin_bit_cast(Codes, c);
+        if (e == 0) to.scale[at.page * to.scale_page + head * to.scale_head + at.slot * to.scale_slot] = scale;
       }
     }
   }
 }
 
+// A workgroup takes B times 256 / L rows of one head.
 template <typename T, bool BITS8, int L, int B>
 __global__ __launch_bounds__(CACHE_THREADS) void read_kernel(RowsParams p) {
   constexpr int ROWS = CACHE_THREADS / L;
@@ -212,11 +203,15 @@ template <typename T, bool BITS8, int L>
 int rows_launch(const RowsParams &p, bool write, hipStream_t stream) {
   constexpr int ROWS = CACHE_THREADS / L, B = 4;
   auto blocks = [&](int b) { return ((int64_t)p.rows + b * ROWS - 1) / (b * ROWS) * p.c.kv_heads; };
-  if (blocks(B) > MAX_BLOCKS) return JDOB_ERR_UNSUPPORTED;
-  // (more rows a workgroup keep more loads under way, but leave few workgroups for few rows: 131,072 rows as above)
-  if (blocks(B) >= 2048)
-    return launch(write ? write_kernel<T, BITS8, L, B> : read_kernel<T, BITS8, L, B>, blocks(B), CACHE_THREADS, stream, p);
-  return launch(write ? write_kernel<T, BITS8, L, 1> : read_kernel<T, BITS8, L, 1>, blocks(1), CACHE_THREADS, stream, p);
+  // More rows a workgroup keep more loads of a read under way, but leave few workgroups for few rows (131,072 rows as above).
+  // A write has no use for them: 131,072 8-bit rows of one sequence took 190 us for 178, of 256 sequences 190 for 201.
+  const bool more = !write && blocks(B) >= 2048;
+  const int64_t n = blocks(more ? B : 1);
+  if (n > MAX_BLOCKS) return JDOB_ERR_UNSUPPORTED;
+  return launch(write  ? write_kernel<T, BITS8, L>
+                : more ? read_kernel<T, BITS8, L, B>
+                       : read_kernel<T, BITS8, L, 1>,
+                n, CACHE_THREADS, stream, p);
 }
 
 template <typename T>
