@@ -397,7 +397,9 @@ def _differs(t, where: str, name: str, shape, dtype, device):
 def _cache(cache: dict, where: str, dtype, device, table, row_start, key_count):
     """The cache and the sequences as the first fields of CacheRowsArgs and AttendPagedArgs.  (Of a dimension with one
     entry the library never uses the stride.)"""
-    k, v = cache["k"], cache["v"]
+    k, v = cache.get("k"), cache.get("v")
+    if k is None or v is None:
+        _refuse(where, "the cache has no " + ("k" if k is None else "v"))
     shape, kind = k.shape, k.dtype
     if len(shape) != 4:
         _refuse(where, "the cache's k and v are [pages, heads, page size, columns]")
@@ -471,7 +473,9 @@ def cache_read(cache: dict, table, row_start, key_count, rows: Optional[int] = N
     were); else `rows` is how many to allocate, which row_start on the GPU says, too, but not without waiting for it:
     row_start's last entry (further ones stay unset)."""
     where = "jdob_edge_cache_read"
-    held = cache["k"]
+    held = cache.get("k")
+    if held is None:
+        _refuse(where, "the cache has no k")
     k, v = (into.get("k"), into.get("v")) if into else (None, None)
     if dtype is None:
         dtype = k.dtype if k is not None else torch.bfloat16 if held.dtype is torch.int8 else held.dtype
