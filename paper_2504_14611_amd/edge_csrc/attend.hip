@@ -758,7 +758,7 @@ extern "C" int jdob_edge_attend(const jdob_edge_attend_args *a, void *hip_stream
   if (code != JDOB_OK || a->num_sequences == 0 || a->query_rows == 0 || a->max_queries == 0) return code;
   const FewPlan f = few_plan(a);
   AttendParams p = {a->num_sequences, a->num_heads, a->num_kv_heads, a->num_heads / a->num_kv_heads, a->head_dim,
-                    a->max_queries, a->scale * 1.44269504088896f, a->query_rows, a->key_rows,
+                    a->max_queries, log2_scale(a->scale), a->query_rows, a->key_rows,
                     (const char *)a->q, (const char *)a->k, (const char *)a->v, (char *)a->out,
                     a->q_stride, a->q_head_stride, a->k_stride, a->k_head_stride, a->v_stride, a->v_head_stride,
                     a->out_stride, a->out_head_stride, a->query_start, a->key_start, a->key_count,

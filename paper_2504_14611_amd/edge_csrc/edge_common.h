@@ -117,6 +117,9 @@ inline bool pieces_overlap(int64_t rows, int64_t row, int64_t heads, int64_t hea
   return false;
 }
 
+// A softmax's scale for powers of two; an infinity would make NaN of equal scores.
+inline float log2_scale(float scale) { return fminf(scale * 1.44269504088896f, 0x1.fffffep127f); }
+
 // A dimension of a grid takes fewer than 2^32 threads: more than FOLD workgroups stand in rows of FOLD, and
 // those behind the last one, in the last row, have nothing to do.
 constexpr int FOLD = 1 << 21, MAX_BLOCKS = 0x7fffffff - FOLD;

@@ -1109,7 +1109,7 @@ extern "C" int jdob_edge_attend_paged(const jdob_edge_attend_paged_args *a, void
   const PagedParams p = {pages_of(a->cache, a->num_sequences, a->table_width, a->table, a->table_stride, a->query_start,
                                   a->key_count),
                          a->num_heads / a->cache.num_kv_heads, f.queries, f.columns,
-                         a->scale * 1.44269504088896f, a->query_rows, (const char *)a->q, (char *)a->out, a->q_stride,
+                         log2_scale(a->scale), a->query_rows, (const char *)a->q, (char *)a->out, a->q_stride,
                          a->q_head_stride, a->out_stride, a->out_head_stride, (int)f.tiles, f.shares, {}, {}, {},
                          (float *)a->workspace};
   hipStream_t stream = (hipStream_t)hip_stream;

@@ -91,3 +91,18 @@ def test_weights_keep_16_bits(dim, page, dtype, bits8):
             for group in (2, 8):
                 paged(scores, v, 0, 1, page, dtype, bits8, 2.0 ** -16, v_scale if bits8 else None, group=group, reach=9,
                       label=(keys, seed))
+
+
+@pytest.mark.parametrize("bits8", [False, True])
+@pytest.mark.parametrize("scale", [1e30, 2.9e38])
+def test_scales_near_the_end_of_binary32(scale, bits8):
+    """Every row is the value of the key with its largest score."""
+    scores = (torch.arange(100, device="cuda") * 37) % 101
+    v = torch.randint(-100, 100, (100, 64), generator=torch.Generator().manual_seed(1)).float().cuda()
+    want = torch.stack([v[scores[:97 + i + 1].argmax()] for i in range(3)])[:, None].expand(3, 4, 64)
+    s = model.paged(scores, v, 0, 3, 16, 2, 2, BF16, bits8)
+    got = edge.attend_paged(s["q"], s["cache"], s["table"], s["row_start"], s["key_count"], scale=scale, max_queries=3, max_keys=100)
+    assert torch.equal(got.float(), want)
+    q, k, v16, *where = model.packed(scores, v, 0, 3, 2, 2, BF16)
+    for most in (3, 200):
+        assert torch.equal(edge.attend(q, k, v16, *where, scale=scale, max_queries=most, max_keys=100).float(), want), most
