@@ -138,7 +138,10 @@ int jdob_edge_project(const jdob_edge_project_args *a, void *hip_stream);
  * change it, infinities and NaN among them; an infinite value that it does
  * see makes its column an infinity or a NaN.  Scores, maxima, sums and the
  * output are binary32; p is rounded to dtype before it is multiplied with v
- * (relative error 2^-8 or 2^-11 of each term, the size of out's own rounding).
+ * (relative error 2^-8 or 2^-11 of each term, the size of out's own rounding;
+ * binary16 has fewer bits of p below 2^-14 of the largest and nothing of it
+ * below 2^-25, which the sum that divides has).  Division comes last: sums of
+ * values beyond 2^119 / m may pass binary32.
  * max_queries and max_keys are at least the largest n and m (both only size
  * the launch and choose the kernel for all of the call's sequences); rows
  * beyond max_queries may be left unwritten.                                */
@@ -236,9 +239,9 @@ int jdob_edge_cache_read(const jdob_edge_cache_rows_args *a, void *hip_stream);
  * the value) goes into its product as 16-bit parts that hold 16 bits of its
  * mantissa, however small it is beside the largest (with a binary16 cache down
  * to 2^-76 of it: what less weight adds, such an output cannot show), and that
- * sums of values pass binary32 nowhere: a mean of finite values is finite.
- * How the keys are split, and with it the order of sums, follows from the
- * lengths of all sequences.                                                 */
+ * sums of values pass binary32 nowhere: a mean of finite values is finite, and
+ * then rounded to dtype.  How the keys are split, and with it the order of
+ * sums, follows from the lengths of all sequences.                          */
 typedef struct {
   jdob_edge_cache cache;
   int32_t num_sequences, table_width;

@@ -17,8 +17,8 @@
 // element a lane, is cut out of 8 rows' pieces that the lane loads side by side.
 //
 // Bound: HBM, at 5 to 5.8 TB/s where there are keys enough (a large copy moves 4.9; what the last cache keeps from pass
-// to pass helps).  Kernels alone: 32 rows of 32 heads after 15 to 8191 keys 89 us, one after 131,071 8-bit keys 47,
-// 256 rows of 64 heads after 511 to 4095 8-bit keys 246; the join 5 to 6.  A tile of 32 8-bit keys of 128 takes 390
+// to pass helps).  Kernels alone: 32 rows of 32 heads after 15 to 8191 keys 89 us, one after 131,071 8-bit keys 48,
+// 256 rows of 64 heads after 511 to 4095 8-bit keys 248; the join 5 to 6.  A tile of 32 8-bit keys of 128 takes 390
 // vector and 110 scalar instructions a wave (half of them turn codes into bfloat16) and 24 products, 1.4 us where a wave
 // has a SIMD to itself: few keys are bound by that and by the launch (one key 6.4 us, 512 keys 10.7).  Tiles of 64 keys
 // took more registers and as long a key; eight waves a workgroup took 0.8 us off 512 keys and put 0.4 on one.
@@ -998,8 +998,9 @@ PagedPlan paged_plan(const jdob_edge_attend_paged_args *a, bool in_pages) {
   const int64_t all = queries * (a->num_heads / a->cache.num_kv_heads);
   // Keys that are read once for 32 columns, not twice: 16 users' 4 rows of 64 heads after up to 16,383 8-bit keys take 84 us
   // so and 106 by 16 columns, after up to 4095 34 and 40.  By 16 columns, where waves need half the registers, if there
-  // are few keys (4 users, up to 1023 keys: 14 us and 17) or InPages does not read them (24 users' drafts on pages of
-  // 20 keys: 25 us and 32).
+  // are few keys (4 users, up to 1023 keys: 14 us and 17) or InPages does not read them: there are no kernels for 32 of
+  // those (through windows 24 users' drafts on pages of 20 keys would take the same 23 us, 16 users' 4 rows of 64 heads after
+  // up to 4095 8-bit keys 44 for 57).
   const int columns = all <= 16 || !in_pages || n * keys * a->cache.num_kv_heads <= 1 << 17 ? 16 : 32;
   const int64_t tiles = (all + columns - 1) / columns, layers = tiles * a->cache.num_kv_heads;
   const int64_t groups = layers * n, most = n * ((keys + LEAST_KEYS - 1) / LEAST_KEYS);

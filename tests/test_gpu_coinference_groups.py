@@ -39,3 +39,13 @@ def test_alone_and_beside_others(page, bits8):
         if NEW[u]:
             alone = attended(chain, [u], runs, rows, page, bits8)
             assert torch.equal(together[u], alone[0]), u
+
+
+@pytest.mark.parametrize("bits8", [False, True])
+def test_a_batch_without_rows(bits8):
+    chain = co.make_chain(SHAPE, 2)
+    e = co.Edge(SHAPE, chain, [0, 1], 0, 40, page=16, bits8=bits8)
+    none = torch.empty(0, SHAPE.width, dtype=torch.bfloat16, device="cuda")
+    assert e.run(none, [0, 0]).shape == (0, SHAPE.width)
+    e.run(torch.randn(21, SHAPE.width, device="cuda").bfloat16(), [20, 1])
+    assert e.run(none, [0, 0]).shape == (0, SHAPE.width) and e.count == [20, 1]
