@@ -178,7 +178,7 @@ constexpr float GROWTH = 8.0f;  // the maximum may lag behind by this much (p up
 // Up to here (log2 units) sc * scale - top * scale may be formed with one rounding of top * scale: it puts all p of a
 // wave off by one factor, but another one for another maximum and in another wave, whose keys are weighed against these
 // by exp(scale (top - top')).  At 2^8 that is within 2^-17 log2 units, small beside p's rounding to 16 bits (2^-11 of
-// itself or more); at 2^24 it would be half of one.
+// itself or more); at 2^24 it would be half of one.  (The difference costs a prompt of 16,384 rows 1.09 ms for 0.98.)
 constexpr float NEAR = 0x1p8f;
 
 // Scores of 32 rows with KT * 32 staged keys, softmax, and the values' sums.  The lane's row sees the
