@@ -237,11 +237,11 @@ int jdob_edge_cache_read(const jdob_edge_cache_rows_args *a, void *hip_stream);
  * the keys are read once for every 32 rows times heads of a key head.  All
  * else is as in jdob_edge_attend, but that p (with an 8-bit cache p * scale of
  * the value) goes into its product as 16-bit parts that hold 16 bits of its
- * mantissa, however small it is beside the largest (with a binary16 cache down
- * to 2^-76 of it: what less weight adds, such an output cannot show), and that
- * sums of values pass binary32 nowhere: a mean of finite values is finite, and
- * then rounded to dtype.  How the keys are split, and with it the order of
- * sums, follows from the lengths of all sequences.                          */
+ * mantissa from 2^-118 on (with a binary16 cache from 2^-76 on: what less
+ * weight adds, such an output cannot show), and that sums of values pass
+ * binary32 nowhere: a mean of finite values is finite, and then rounded to
+ * dtype.  How the keys are split, and with it the order of sums, follows from
+ * the lengths of all sequences.                                             */
 typedef struct {
   jdob_edge_cache cache;
   int32_t num_sequences, table_width;

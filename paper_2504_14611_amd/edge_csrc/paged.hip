@@ -508,11 +508,12 @@ template <typename T, bool BITS8>
 using Weight = typename std::conditional<BITS8, __bf16, T>::type;
 
 // Parts of binary16 end at 2^-25.  There p is made 2^LIFT times as large, below 2^16 still, and where some p of a tile is
-// below SMALL, so that its parts hold fewer than 16 bits, what they leave of p goes through the products again, 2^AGAIN
-// times as large, until they are 1 / END times as large: what is lost of a weight is then below 2^-25 2^-60 2^-7 of the largest, times values below
-// 2^16 and 2^31 keys far below what a binary16 output can show.  (Nothing at all would be left of p below 2^-25 otherwise,
-// while the sum has it.)  32 users' tokens take 96 us for 95 without, 104 where all tiles go through again; binary32
-// products, an eighth of the rate, took 100 for all (four rows of 64 heads of 16 users 135 for 130, one tile 6.8 for 5.7).
+// below SMALL, so that its parts hold fewer than 16 bits, what they leave of p goes through the products again, AGAIN
+// times as large, until that is 1 / END: what is lost of a weight is then below 2^-25 2^-60 2^-7 of the largest, which
+// 2^31 keys with values to 2^16 cannot make a binary16 output show.  (Nothing at all would be left of p below 2^-25
+// otherwise, while the sum has it.)  32 users' tokens take 96 us for 95 without, 104 where all tiles go through again;
+// binary32 products, an eighth of the rate, took 100 for all (four rows of 64 heads of 16 users 135 for 130, one tile 6.8
+// for 5.7).
 template <typename T, bool BITS8>
 constexpr bool LIFTED = !BITS8 && __is_same(T, _Float16);
 constexpr float LIFT = 7.0f, SMALL = 0x1p-9f, AGAIN = 0x1p20f, END = 0x1p-60f;
